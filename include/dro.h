@@ -407,6 +407,132 @@ int dro_bcd_solve(dro_ctx *ctx, const dro_problem *p, const float *eps, const dr
                   int32_t max_outer, int32_t max_inner, int32_t *z, int32_t *k, double *pi,
                   uint8_t *delta, double *objective, int32_t *info, dro_stream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The paged cache that the reservations are for.  A pool of `num_blocks` blocks
+ * of `block` tokens holds the keys and values of every request; a request's
+ * table row names its blocks in order, so token p of the request lies in slot
+ *   table[r][p / block] * block + p % block
+ * of the pool.  One step of a serving loop is kv_block_tables (blocks for the
+ * step's new tokens and for the reservations r = L_in + eta of this library),
+ * then per layer kv_store (the new tokens' keys and values into their slots)
+ * and kv_attention (the new tokens' attention over the cache).
+ *
+ * Strides and lengths are in elements.  Limits (DRO_ELIMIT): blocks of 16 to
+ * 1024 tokens, a power of two; head dimension a multiple of 8 up to 256; R up
+ * to 2^20 requests, T up to 2^24 tokens a call, T * heads up to 2^30,
+ * R * max_blocks and num_blocks * block up to 2^31 - 1 (the byte offsets into
+ * the cache are 64-bit), a head's tokens within a block closer than 2^31 bytes.
+ * Device data steers no read or write outside the arrays given: a block
+ * outside the pool is read as the nearest one of the pool, a slot outside it
+ * is not written, lengths and offsets are cut to the table and to T.
+ * ---------------------------------------------------------------------- */
+enum { DRO_BF16 = 0, DRO_F16 = 1, DRO_FP8_E4M3 = 2 };
+
+/* Block tables and slots of one step.  Request r holds len[r] tokens in
+ * held[r] blocks and brings add[r] new ones (0: none; < 0: it ends and gives
+ * its blocks back); reserve[r] (NULL: none) is the number of tokens that it is
+ * to have blocks for.  With B = block, per request
+ *   n = max(add, 0), after = len + n, blocks = ceil(max(after, reserve) / B),
+ *   grow = max(0, blocks - held)
+ * the step is, exactly:
+ *   the blocks of ended requests go on top of the free stack free_list[0 .. free),
+ *   in the order of the requests and of their rows, F tokens in all then;
+ *   a request is granted if it has not ended, blocks <= max_blocks, and grow = 0
+ *   or the sum of grow up to and with it (over the requests that have neither
+ *   ended nor too wide a row) is at most F: first come, first served, so that
+ *   after the first request that has to wait no later one grows;
+ *   granted requests take their blocks from the top of the stack, in order.
+ * Outputs: table and free_list in place (rows change in [held, blocks) only),
+ *   held_out [R], free_out [1], context [R] = after if granted, else 0,
+ *   granted [R] = 1 or 0, start [R+1] = the exclusive sums of n, and for token
+ *   t = start[r] + i < T of a granted request pos[t] = len[r] + i and its slot
+ *   slot[t]; -1 in both for tokens that were not granted and for t >= start[R].
+ * held_out and free_out may be held and free_count themselves (in place); as
+ * they may be others, a step can be tried: called again with the same inputs
+ * it gives the same outputs.  Negative lengths count as 0, held as cut to
+ * [0, max_blocks], free_count to [0, num_blocks]. */
+typedef struct {
+    int32_t R;             /* requests                                                */
+    int32_t block;         /* tokens a block                                          */
+    int32_t num_blocks;    /* blocks of the pool                                      */
+    int32_t max_blocks;    /* blocks that a table row can name                        */
+    int64_t table_stride;  /* entries from row to row, >= max_blocks                  */
+    int32_t *table;        /* [R] rows, in and out                                    */
+    int32_t *free_list;    /* [num_blocks] free blocks (a stack), in and out          */
+    const int32_t *held;   /* [R] blocks held                                         */
+    const int32_t *free_count; /* [1] blocks free                                     */
+} dro_kv_pool;
+
+int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *pool, const int32_t *len, const int32_t *add,
+                    const int32_t *reserve, int64_t T, int32_t *held_out, int32_t *free_out,
+                    int32_t *context, int32_t *start, int64_t *slot, int32_t *pos,
+                    uint8_t *granted, dro_stream_t stream);
+
+/* One layer's cache: element (block b, token i, head h, component d) of the keys
+ * is k[b k_block + i k_token + h k_head + d], so blocks may hold their tokens
+ * or their heads together.  Components are contiguous; every stride is a multiple
+ * of 8 elements, and k and v are aligned to 8 elements.  dtype DRO_FP8_E4M3 holds key / k_scale[h] and value /
+ * v_scale[h], rounded to nearest even and saturated at +-448 (NaN stays NaN);
+ * the scales ([heads], > 0) are NULL for the other types. */
+typedef struct {
+    int32_t dtype;
+    int32_t heads, dim, block, num_blocks;
+    void *k, *v;
+    int64_t k_block, k_token, k_head;
+    int64_t v_block, v_token, v_head;
+    const float *k_scale, *v_scale;
+} dro_kv_cache;
+
+/* The keys and values of T tokens into their slots: token t, head h, component d
+ * at k[t k_token + h k_head + d] (strides of this call, multiples of 8, k and v
+ * aligned to 16 bytes) of type `dtype`, DRO_BF16 or DRO_F16, which the cache's
+ * type is unless that is DRO_FP8_E4M3.  Slots outside [0, num_blocks * block)
+ * (-1: no slot) are skipped; of two tokens with one slot either may remain. */
+int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, const void *k,
+             int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
+             const int64_t *slot, dro_stream_t stream);
+
+/* Attention of each request's last tokens over the cache.  Request r has
+ * context[r] tokens in the cache, the last n = start[r+1] - start[r] of which
+ * are the rows q[start[r] ..] (kv_store puts their keys and values there
+ * first); query head h reads key head h / (Hq / heads).  Row i is at
+ * position p = context[r] - n + i and sees key j < context[r] if
+ *   (j <= p or j < prefix[r])  and  (window = 0 or p - j < window);
+ *   s_j = scale q . k_j, then cap tanh(s_j / cap) if cap > 0,
+ *   then s_j + slope_h (j - p) with slopes
+ *   out = sum_j softmax(s)_j v_j,  lse = log sum_j exp s_j  over the keys seen.
+ * A row that sees no key (or whose s are all -infinity) has out = 0 and lse =
+ * -infinity; keys and values that a row does not see do not enter it, whatever
+ * they hold.  Rows of no request (t outside [start[0], start[R])) are zero with
+ * lse -infinity.  Products, sums and the softmax are kept in fp32; the weights
+ * are rounded to q's type for the product with the values.
+ * max_new bounds the rows of one request and picks the kernels (a larger request
+ * is computed all the same). */
+typedef struct {
+    int32_t dtype;              /* of q and out: DRO_BF16 or DRO_F16                      */
+    int32_t R, Hq;              /* requests; query heads, a multiple of the cache's heads */
+    int64_t T;                  /* rows of q, out and lse                                 */
+    const void *q;              /* row t, head h at q[t q_token + h q_head], aligned as k */
+    int64_t q_token, q_head;
+    void *out;                  /* as q                                                   */
+    int64_t out_token, out_head;
+    float *lse;                 /* [T][Hq], may be NULL                                   */
+    const int32_t *start;       /* [R+1] ascending                                        */
+    const int32_t *context;     /* [R]                                                    */
+    const int32_t *table;       /* [R][max_blocks]                                        */
+    int64_t table_stride;
+    int32_t max_blocks;
+    int32_t max_new;
+    float scale;                /* finite                                                 */
+    float softcap;              /* 0: none                                                */
+    int32_t window;             /* 0: none                                                */
+    const float *slopes;        /* [Hq], NULL: none                                       */
+    const int32_t *prefix;      /* [R], NULL: none                                        */
+} dro_kv_rows;
+
+int kv_attention(dro_ctx *ctx, const dro_kv_cache *cache, const dro_kv_rows *rows,
+                 dro_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

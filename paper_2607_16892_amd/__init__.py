@@ -9,6 +9,7 @@ from .api import (Context, Problem, Groups, DroError, dro_validate, dro_cost_eva
                   dro_argmin_reservation, dro_exact_table, dro_continuous_dual, class_quantile,
                   class_moments, dro_reservation_cost, dro_baseline_reservations, bcd_init_state,
                   bcd_block_step)
+from .kv import BlockPool, KvCache, kv_attention, kv_block_tables, kv_store
 from ._native import LIB_PATH, NativeMissing, load as load_native
 
 __all__ = ["Context", "Problem", "Groups", "DroError", "dro_validate", "dro_cost_eval",
@@ -16,5 +17,6 @@ __all__ = ["Context", "Problem", "Groups", "DroError", "dro_validate", "dro_cost
            "dro_argmin_reservation", "dro_exact_table", "dro_continuous_dual", "class_quantile",
            "class_moments", "dro_reservation_cost", "dro_baseline_reservations", "bcd_init_state",
            "bcd_block_step",
+           "BlockPool", "KvCache", "kv_block_tables", "kv_store", "kv_attention",
            "LIB_PATH", "NativeMissing",
            "load_native"]

@@ -13,6 +13,7 @@ _lib = None
 
 P = ct.c_void_p
 i32 = ct.c_int32
+i64 = ct.c_int64
 
 
 class ProblemStruct(ct.Structure):
@@ -35,6 +36,27 @@ class ServiceStruct(ct.Structure):
 
 class StepOutStruct(ct.Structure):
     _fields_ = [("k_next", P), ("W_star", P), ("q_value", P), ("usage", P), ("feasible", P)]
+
+
+class KvPoolStruct(ct.Structure):
+    _fields_ = [("R", i32), ("block", i32), ("num_blocks", i32), ("max_blocks", i32),
+                ("table_stride", i64), ("table", P), ("free_list", P), ("held", P),
+                ("free_count", P)]
+
+
+class KvCacheStruct(ct.Structure):
+    _fields_ = [("dtype", i32), ("heads", i32), ("dim", i32), ("block", i32), ("num_blocks", i32),
+                ("k", P), ("v", P), ("k_block", i64), ("k_token", i64), ("k_head", i64),
+                ("v_block", i64), ("v_token", i64), ("v_head", i64), ("k_scale", P),
+                ("v_scale", P)]
+
+
+class KvRowsStruct(ct.Structure):
+    _fields_ = [("dtype", i32), ("R", i32), ("Hq", i32), ("T", i64), ("q", P), ("q_token", i64),
+                ("q_head", i64), ("out", P), ("out_token", i64), ("out_head", i64), ("lse", P),
+                ("start", P), ("context", P), ("table", P), ("table_stride", i64),
+                ("max_blocks", i32), ("max_new", i32), ("scale", ct.c_float),
+                ("softcap", ct.c_float), ("window", i32), ("slopes", P), ("prefix", P)]
 
 
 EXPORTS = {
@@ -67,6 +89,10 @@ EXPORTS = {
                                  i32, P, P, P, P, P, P, P]),
     "bcd_block_step": (ct.c_int, [P, ct.POINTER(ProblemStruct), P, ct.POINTER(GroupsStruct), P,
                                   ct.POINTER(StepOutStruct), P]),
+    "kv_block_tables": (ct.c_int, [P, ct.POINTER(KvPoolStruct), P, P, P, i64, P, P, P, P, P, P, P,
+                                   P]),
+    "kv_store": (ct.c_int, [P, ct.POINTER(KvCacheStruct), i32, i64, P, i64, i64, P, i64, i64, P, P]),
+    "kv_attention": (ct.c_int, [P, ct.POINTER(KvCacheStruct), ct.POINTER(KvRowsStruct), P]),
 }
 
 

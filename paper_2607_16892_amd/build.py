@@ -30,6 +30,9 @@ UNITS = {
     "exact.hip": ["-ffp-contract=off"],
     "serving.hip": ["-ffp-contract=off"],
     "api.hip": ["-ffp-contract=off"],
+    "kv_api.hip": [],
+    "kv_cache.hip": ["-ffp-contract=off"],
+    "kv_attention.hip": [],
 }
 
 
