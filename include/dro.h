@@ -420,8 +420,8 @@ int dro_bcd_solve(dro_ctx *ctx, const dro_problem *p, const float *eps, const dr
  * Strides and lengths are in elements.  Limits (DRO_ELIMIT): blocks of 16 to
  * 1024 tokens, a power of two; head dimension a multiple of 8 up to 256; R up
  * to 2^20 requests, T up to 2^24 tokens a call, T * heads up to 2^30,
- * R * max_blocks and num_blocks * block up to 2^31 - 1 (the byte offsets into
- * the cache are 64-bit), a head's tokens within a block closer than 2^31 bytes.
+ * max_blocks * block up to 2^30 tokens a request, R * max_blocks and
+ * num_blocks * block up to 2^31 - 1 (byte offsets into the cache are 64-bit), a head's tokens within a block closer than 2^31 bytes.
  * Device data steers no read or write outside the arrays given: a block
  * outside the pool is read as the nearest one of the pool, a slot outside it
  * is not written, lengths and offsets are cut to the table and to T.

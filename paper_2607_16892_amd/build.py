@@ -33,6 +33,8 @@ UNITS = {
     "kv_api.hip": [],
     "kv_cache.hip": ["-ffp-contract=off"],
     "kv_attention.hip": [],
+    "kv_decode_bf16.hip": [],
+    "kv_decode_f16.hip": [],
 }
 
 

@@ -33,7 +33,7 @@ int check_pool_size(dro_ctx *ctx, int block, int num_blocks)
     return DRO_OK;
 }
 
-int check_table(dro_ctx *ctx, const int32_t *table, int R, int max_blocks, int64_t stride)
+int check_table(dro_ctx *ctx, const int32_t *table, int R, int max_blocks, int64_t stride, int block)
 {
     if (R <= 0 || max_blocks <= 0)
         return fail(ctx, DRO_EINVAL, "R and max_blocks must be positive (R=%d max_blocks=%d)", R,
@@ -42,6 +42,9 @@ int check_table(dro_ctx *ctx, const int32_t *table, int R, int max_blocks, int64
     if (stride < max_blocks)
         return fail(ctx, DRO_EINVAL, "table_stride=%lld is less than max_blocks=%d",
                     (long long)stride, max_blocks);
+    if ((int64_t)max_blocks * block > 1LL << 30)
+        return fail(ctx, DRO_ELIMIT, "max_blocks * block = %lld exceeds 2^30 tokens a request",
+                    (long long)max_blocks * block);
     if (R > kMaxRequests) return fail(ctx, DRO_ELIMIT, "R=%d exceeds 2^20 requests", R);
     if ((int64_t)R * max_blocks > 0x7fffffffLL || stride > (1LL << 40))
         return fail(ctx, DRO_ELIMIT, "R * max_blocks = %lld exceeds 2^31 - 1 table entries",
@@ -128,15 +131,12 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *p, const int32_t *len, cons
     if (!p) return fail(ctx, DRO_EINVAL, "pool is NULL");
     int rc = check_pool_size(ctx, p->block, p->num_blocks);
     if (rc) return rc;
-    if ((rc = check_table(ctx, p->table, p->R, p->max_blocks, p->table_stride))) return rc;
+    if ((rc = check_table(ctx, p->table, p->R, p->max_blocks, p->table_stride, p->block))) return rc;
     if ((rc = check_tokens(ctx, T, 1))) return rc;
     if (!p->free_list || !p->held || !p->free_count || !len || !add)
         return fail(ctx, DRO_EINVAL, "free_list, held, free_count, len or add is NULL");
     if (!held_out || !free_out || !context || !start || !granted || (T && (!slot || !pos)))
         return fail(ctx, DRO_EINVAL, "a required output is NULL");
-    if ((int64_t)p->max_blocks * p->block > 0x7fffffffLL)
-        return fail(ctx, DRO_ELIMIT, "max_blocks * block = %lld exceeds 2^31 - 1 tokens",
-                    (long long)p->max_blocks * p->block);
     ENTER_DEVICE(ctx);
     hipStream_t st = (hipStream_t)stream;
     if ((rc = ensure_ws(ctx, rup((size_t)p->R * sizeof(int4)) + rup(8), st))) return rc;
@@ -216,11 +216,8 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     if ((rc = check_dtype(ctx, q->dtype, c))) return rc;
     if (q->Hq <= 0 || q->Hq % c->heads)
         return fail(ctx, DRO_EINVAL, "Hq=%d is not a multiple of the cache's %d heads", q->Hq, c->heads);
-    if ((rc = check_table(ctx, q->table, q->R, q->max_blocks, q->table_stride))) return rc;
+    if ((rc = check_table(ctx, q->table, q->R, q->max_blocks, q->table_stride, c->block))) return rc;
     if ((rc = check_tokens(ctx, q->T, q->Hq))) return rc;
-    if ((int64_t)q->max_blocks * c->block > 0x7fffffffLL)
-        return fail(ctx, DRO_ELIMIT, "max_blocks * block = %lld exceeds 2^31 - 1 tokens",
-                    (long long)q->max_blocks * c->block);
     if (!std::isfinite(q->scale) || !std::isfinite(q->softcap) || q->softcap < 0 || q->window < 0 ||
         q->max_new < 0)
         return fail(ctx, DRO_EINVAL, "scale=%g must be finite, softcap=%g, window=%d and max_new=%d "
@@ -263,10 +260,12 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     a.v_scale = c->v_scale;
     a.scale = q->scale;
     a.cap = q->softcap;
-    a.window = q->window;
+    // a window as long as the table hides nothing
+    a.window = q->window < (int64_t)q->max_blocks * c->block ? q->window : 0;
     a.slopes = q->slopes;
     a.prefix = q->prefix;
-    HIPCHK(launch_kv_attention(a, q->dtype, c->dtype, (hipStream_t)stream));
+    if ((rc = ensure_ws(ctx, kv_attention_bytes(a), (hipStream_t)stream))) return rc;
+    HIPCHK(launch_kv_attention(a, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
     return DRO_OK;
 }
 

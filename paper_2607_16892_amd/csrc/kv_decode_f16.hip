@@ -1,0 +1,7 @@
+// Decode attention with f16 queries.
+#include "kv_decode.h"
+
+namespace dro {
+template void launch_kv_decode<f16>(const KvAttnArgs &, const KvCut &, const KvPlan &, int, int, uint32_t,
+                                     uint32_t, bool, float *, float2 *, hipStream_t);
+}  // namespace dro

@@ -1,0 +1,101 @@
+// Register-level pieces of the attention kernels.
+#pragma once
+
+#include "kv.h"
+#include "kv_types.h"
+
+namespace dro {
+
+typedef Vec<float, 4> f32x4;
+typedef Vec<float, 16> f32x16;
+typedef Vec<uint32_t, 4> u32x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// 16 x 16 tile over 32 products.  First operand: lane holds row lane % 16, products
+// (lane / 16) 8 .. + 8; second: column lane % 16, the same products; result: column
+// lane % 16, rows (lane / 16) 4 .. + 4.
+template <class T> __device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c)
+{
+    if constexpr (__is_same(T, bf16))
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Vec<bf16, 8>, x),
+                                                       __builtin_bit_cast(Vec<bf16, 8>, y), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Vec<f16, 8>, x),
+                                                      __builtin_bit_cast(Vec<f16, 8>, y), c, 0, 0, 0);
+}
+
+template <class T> __device__ __forceinline__ uint32_t pack2(float x, float y)
+{
+    return __builtin_bit_cast(uint32_t, Vec<T, 2>{(T)x, (T)y});
+}
+
+// largest over the four groups of 16 lanes, lane by lane
+__device__ __forceinline__ float max_groups(float x)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    x = fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    const uint32_t d = __builtin_bit_cast(uint32_t, x);
+    r = __builtin_amdgcn_permlane16_swap(d, d, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float sum_groups(float x)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    const uint32_t d = __builtin_bit_cast(uint32_t, x);
+    r = __builtin_amdgcn_permlane16_swap(d, d, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// tanh by the exponential: absolute error below 2^-21
+__device__ __forceinline__ float tanh_fast(float x)
+{
+    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.0f * kLog2e)) + 1.0f);
+}
+
+// whether one of the two values of w is infinite or NaN, and w with such values zeroed
+template <class T> __device__ __forceinline__ bool has_nonfinite(uint32_t w)
+{
+    constexpr uint32_t e = __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
+    return (w & e) == e || ((w >> 16) & e) == e;
+}
+template <class T> __device__ __forceinline__ uint32_t zero_nonfinite(uint32_t w)
+{
+    constexpr uint32_t e = __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
+    if ((w & e) == e) w &= 0xffff0000u;
+    if (((w >> 16) & e) == e) w &= 0xffffu;
+    return w;
+}
+
+// N dwords at base + off, aligned to 8 elements of the cache's type: the base is the same
+// for the wave, so an address costs no 64-bit vector arithmetic.
+template <int N> struct Words {
+    uint32_t w[N];
+};
+template <int N> __device__ __forceinline__ Words<N> load_words(const char *base, uint32_t off)
+{
+    Words<N> x;
+    if constexpr (N >= 4) {
+        typedef u32x4 __attribute__((aligned(8))) loose;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const u32x4 y = *(const loose *)(base + 16 * i + off);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.w[4 * i + j] = y[j];
+        }
+    } else if constexpr (N == 2) {
+        typedef Vec<uint32_t, 2> __attribute__((aligned(4))) loose;
+        const Vec<uint32_t, 2> y = *(const loose *)(base + off);
+        x.w[0] = y[0];
+        x.w[1] = y[1];
+    } else {
+        x.w[0] = *(const uint32_t *)(base + off);
+    }
+    return x;
+}
+
+}  // namespace dro
