@@ -43,6 +43,7 @@ hipError_t launch_kv_store(const KvStoreArgs &a, int dtype, int cache_dtype, hip
 struct KvAttnArgs {
     int R, T, Hq, H, G, D;
     int shift, num_blocks, W;
+    int max_new, num_cu;
     const void *q;
     int64_t q_token, q_head;
     void *out;
@@ -60,7 +61,7 @@ struct KvAttnArgs {
 };
 inline size_t kv_rup(size_t v) { return (v + 255) & ~size_t(255); }
 // bytes of scratch that a call needs
-size_t kv_attention_bytes(const KvAttnArgs &a);
+size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype);
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st);
 
 }  // namespace dro

@@ -237,6 +237,8 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     a.shift = block_shift(c->block);
     a.num_blocks = c->num_blocks;
     a.W = q->max_blocks;
+    a.max_new = q->max_new;
+    a.num_cu = ctx->num_cu;
     a.q = q->q;
     a.q_token = q->q_token;
     a.q_head = q->q_head;
@@ -264,7 +266,7 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     a.window = q->window < (int64_t)q->max_blocks * c->block ? q->window : 0;
     a.slopes = q->slopes;
     a.prefix = q->prefix;
-    if ((rc = ensure_ws(ctx, kv_attention_bytes(a), (hipStream_t)stream))) return rc;
+    if ((rc = ensure_ws(ctx, kv_attention_bytes(a, c->dtype), (hipStream_t)stream))) return rc;
     HIPCHK(launch_kv_attention(a, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
     return DRO_OK;
 }

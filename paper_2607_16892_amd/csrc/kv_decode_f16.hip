@@ -1,7 +1,7 @@
-// Decode attention with f16 queries.
+// Attention of few rows a request, f16 queries.
 #include "kv_decode.h"
 
 namespace dro {
-template void launch_kv_decode<f16>(const KvAttnArgs &, const KvCut &, const KvPlan &, int, int, uint32_t,
-                                     uint32_t, bool, float *, float2 *, hipStream_t);
+template void launch_kv_decode<f16>(const KvAttnArgs &, const KvCut &, const uint64_t *, int, int, bool, float *,
+                                   float2 *, KvJoin *, hipStream_t);
 }  // namespace dro

@@ -57,18 +57,16 @@ __device__ __forceinline__ float tanh_fast(float x)
     return 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.0f * kLog2e)) + 1.0f);
 }
 
-// whether one of the two values of w is infinite or NaN, and w with such values zeroed
-template <class T> __device__ __forceinline__ bool has_nonfinite(uint32_t w)
+// the bits of the infinities and NaN among the values of a dword of the cache's type C: an
+// exponent of ones (fp8: NaN alone) carries into the sign's place
+template <class C> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w)
 {
-    constexpr uint32_t e = __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
-    return (w & e) == e || ((w >> 16) & e) == e;
-}
-template <class T> __device__ __forceinline__ uint32_t zero_nonfinite(uint32_t w)
-{
-    constexpr uint32_t e = __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
-    if ((w & e) == e) w &= 0xffff0000u;
-    if (((w >> 16) & e) == e) w &= 0xffffu;
-    return w;
+    if constexpr (sizeof(C) == 1)
+        return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+    else if constexpr (__is_same(C, bf16))
+        return ((((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
+    else
+        return ((((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15) * 0xffffu;
 }
 
 // N dwords at base + off, aligned to 8 elements of the cache's type: the base is the same

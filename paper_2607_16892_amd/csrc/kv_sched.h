@@ -1,12 +1,12 @@
 // How the attention's work is cut into workgroups, found by every workgroup itself.
 //
 // Request r has n new tokens, so n G rows a key head (G query heads each), in tiles of
-// `rows` rows, and spans the keys that its rows can see.  Its tiles' keys are cut into
-// chunks of C keys, where C spreads the keys of all tiles over about 2^target_log2
-// workgroups: one long request beside short ones is split, and many requests of about
-// one length are not.  A request of one chunk writes its rows; the chunks of others
-// leave partial results, fewer than 2^(target_log2 + 1) of them since a request that is
-// cut has more than C keys a tile.
+// `rows` rows; an item is a tile of a key head.
+//
+// Few rows a request: a step is 32 keys of an item, and the steps of all items in order
+// are dealt to `groups` workgroups in equal runs, so requests of any lengths load them
+// alike.  A run that holds a whole item writes its rows; a run that begins or ends within
+// an item leaves a partial result, at most two a workgroup, for the join.
 #pragma once
 
 #include "kv.h"
@@ -23,19 +23,20 @@ struct KvShare {  // of one request
 };
 
 struct KvItem {
-    int r, n, ctx, first_token, tiles, tile, head, chunk, chunks;
-    int C;        // keys a chunk
-    int partial;  // place of the chunk's partial result (chunks > 1)
+    int r, n, ctx, first_token;
+    int tile, head;
+    int step, steps;  // the item's step asked for, and how many it has
 };
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
-    int rows;         // of a tile
-    int align;        // keys a chunk is a multiple of
-    int target_log2;
-    int few;          // tokens
-    bool below;       // the kernel of the requests of up to `few` tokens
+    int rows;      // of a tile
+    int groups;    // workgroups
+    int few;       // tokens
+    bool below;    // the kernel of the requests of up to `few` tokens
 };
+
+constexpr int kStepKeys = 32;
 
 __device__ __forceinline__ KvShare kv_share(const KvAttnArgs &a, const KvCut &c, int r)
 {
@@ -50,31 +51,30 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs &a, const KvCut &c,
     s.span = s.ctx;
     if (a.window && !a.prefix)  // a tile's rows lie within rows / G + 2 tokens
         s.span = (int)min((long long)s.ctx,
-                          (long long)a.window + min(c.rows / a.G + 2, n) + c.align);
+                          (long long)a.window + min(c.rows / a.G + 2, n) + kStepKeys);
     return s;
 }
 
-// Keys a chunk, from the keys of all tiles.
-__device__ __forceinline__ int kv_chunk(const KvCut &c, uint64_t keys)
+__device__ __forceinline__ uint32_t kv_steps(const KvShare &s)
 {
-    const uint64_t x = ((keys >> c.target_log2) + c.align) / c.align * c.align;
-    return (int)min(x, (uint64_t)0x7fffff00);
+    return s.tiles ? (uint32_t)max((s.span + kStepKeys - 1) / kStepKeys, 1) : 0;
+}
+__device__ __forceinline__ uint64_t kv_units(const KvAttnArgs &a, const KvShare &s)
+{
+    return (uint64_t)((uint32_t)s.tiles * (uint32_t)a.H) * kv_steps(s);
 }
 
-__device__ __forceinline__ int kv_chunks(const KvShare &s, int C)
+// steps a workgroup, for `all` steps, the longest of the wave's items having `longest`.  An
+// item of many steps alone would be cut so fine that the join takes longer than the steps.
+__device__ __forceinline__ uint64_t kv_run(const KvCut &c, uint64_t all, uint32_t longest)
 {
-    return s.tiles ? max((s.span + C - 1) / C, 1) : 0;
+    const uint64_t least = __any(longest >= 2048) ? 8 : __any(longest >= 512) ? 4 : __any(longest >= 128) ? 2 : 1;
+    if (all < 0xffff0000u) return max((uint64_t)(((uint32_t)all + (uint32_t)c.groups - 1) / (uint32_t)c.groups), least);
+    return (all + c.groups - 1) / (uint32_t)c.groups;
 }
-
-// The scan's results for R > kInlineRequests, from kv_plan_kernel.
-struct KvPlan {
-    const uint32_t *items;     // [R + 1] exclusive sums of the requests' items
-    const uint32_t *partials;  // [R + 1] and of their partial results
-    const int *C;
-};
 
 // First index of the ascending x[0 .. n] whose next entry exceeds v (x[n] > v): 64 probes a step.
-__device__ __forceinline__ int kv_find(const uint32_t *x, int n, uint32_t v)
+__device__ __forceinline__ int kv_find(const uint64_t *x, int n, uint64_t v)
 {
     int lo = 0, hi = n;  // x[lo] <= v < x[hi]
     const int lane = threadIdx.x & 63;
@@ -88,105 +88,80 @@ __device__ __forceinline__ int kv_find(const uint32_t *x, int n, uint32_t v)
     return lo;
 }
 
-// The work of workgroup b (uniform); false: none.  Workgroups b, b + 8, .. run on one
-// die, which gets consecutive items: the tiles of a request's head share their keys in
-// its L2.
-__device__ __forceinline__ bool kv_item(const KvAttnArgs &a, const KvCut &c, const KvPlan &p, uint32_t b,
-                                        KvItem &w)
-{
-    const int lane = threadIdx.x & 63;
-    uint32_t all, local;
-    KvShare s;
-    auto place = [&](uint32_t &i) {
-        const uint32_t each = (all + 7) / 8;
-        i = (b & 7) * each + (b >> 3);
-        return (b >> 3) < each && i < all;
-    };
-    if (a.R <= kInlineRequests) {
-        s = kv_share(a, c, lane);
-        const uint64_t keys = scan_wave((uint64_t)s.tiles * (uint64_t)s.span * (uint64_t)a.H);
-        w.C = kv_chunk(c, lane_value(keys, 63));
-        const int chunks = kv_chunks(s, w.C);
-        const uint32_t items = (uint32_t)s.tiles * (uint32_t)chunks * (uint32_t)a.H;
-        const uint32_t part = chunks > 1 ? items : 0;
-        const uint32_t upto = scan_wave(items), pupto = scan_wave(part);
-        all = lane_value(upto, 63);
-        uint32_t i;
-        if (!place(i)) return false;
-        w.r = __builtin_ctzll(__ballot(upto > i));
-        local = i - lane_value(upto - items, w.r);
-        w.partial = (int)lane_value(pupto - part, w.r);
-        w.n = (int)lane_value((uint32_t)s.n, w.r);
-        w.ctx = (int)lane_value((uint32_t)s.ctx, w.r);
-        w.tiles = (int)lane_value((uint32_t)s.tiles, w.r);
-        w.chunks = (int)lane_value((uint32_t)chunks, w.r);
-    } else {
-        all = p.items[a.R];
-        uint32_t i;
-        if (!place(i)) return false;
-        w.r = __builtin_amdgcn_readfirstlane(kv_find(p.items, a.R, i));
-        w.C = p.C[0];
-        s = kv_share(a, c, w.r);
-        local = i - p.items[w.r];
-        w.partial = (int)p.partials[w.r];
-        w.n = s.n;
-        w.ctx = s.ctx;
-        w.tiles = s.tiles;
-        w.chunks = kv_chunks(s, w.C);
-    }
-    w.first_token = min(max(a.start[w.r], 0), a.T);
-    w.partial += (int)local;
-    // tiles within chunks within heads
-    const uint32_t per_head = (uint32_t)w.tiles * (uint32_t)w.chunks;
-    w.head = (int)(local / per_head);
-    local -= (uint32_t)w.head * per_head;
-    w.chunk = (int)(local / (uint32_t)w.tiles);
-    w.tile = (int)(local - (uint32_t)w.chunk * (uint32_t)w.tiles);
-    return true;
-}
-
-// The partial results of a row: one of its request's per chunk.
-struct KvParts {
-    int chunks;      // <= 1: none, the row is written already
-    int64_t first;   // of chunk 0, in rows
-    int64_t stride;  // from chunk to chunk, in rows
+// The requests' shares and sums of steps where a workgroup scans them itself.
+struct KvLds {
+    uint64_t upto[kInlineRequests];  // inclusive
+    KvShare share[kInlineRequests];
 };
-__device__ __forceinline__ KvParts kv_row_parts(const KvAttnArgs &a, const KvCut &c, const KvPlan &p, int t,
-                                                int hq)
-{
-    const int lane = threadIdx.x & 63;
-    KvShare s;
-    int r, chunks, part0;
-    if (a.R <= kInlineRequests) {
-        s = kv_share(a, c, lane);
-        const uint64_t keys = scan_wave((uint64_t)s.tiles * (uint64_t)s.span * (uint64_t)a.H);
-        const int C = kv_chunk(c, lane_value(keys, 63));
-        chunks = kv_chunks(s, C);
-        const uint32_t part = chunks > 1 ? (uint32_t)s.tiles * (uint32_t)chunks * (uint32_t)a.H : 0;
-        const uint32_t pupto = scan_wave(part);
-        const uint64_t mine = __ballot(lane < a.R && s.tiles && a.start[min(lane, a.R)] <= t &&
-                                       t < a.start[min(lane, a.R - 1) + 1]);
-        if (!mine) return KvParts{0, 0, 0};
-        r = __builtin_ctzll(mine);
-        part0 = (int)lane_value(pupto - part, r);
-        s.tiles = (int)lane_value((uint32_t)s.tiles, r);
-        chunks = (int)lane_value((uint32_t)chunks, r);
-    } else {
-        if (t < a.start[0] || t >= a.start[a.R]) return KvParts{0, 0, 0};
-        r = __builtin_amdgcn_readfirstlane(kv_find((const uint32_t *)a.start, a.R, (uint32_t)t));
-        s = kv_share(a, c, r);
-        chunks = kv_chunks(s, p.C[0]);
-        part0 = (int)p.partials[r];
+
+// The items by their steps: from the workgroup's own scan in LDS, or, beyond
+// kInlineRequests, from the exclusive sums [R + 1] of kv_plan_kernel.
+struct KvSched {
+    uint64_t all, run;  // all steps, and those of a workgroup
+
+    // (all waves; the results are in LDS after it)
+    __device__ __forceinline__ void init(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, KvLds &lds)
+    {
+        if (a.R <= kInlineRequests) {
+            const int lane = threadIdx.x & 63;
+            const KvShare s = kv_share(a, c, lane);
+            const uint64_t upto = scan_wave(kv_units(a, s));
+            all = lane_value(upto, 63);
+            if (threadIdx.x < 64) {
+                lds.upto[lane] = upto;
+                lds.share[lane] = s;
+            }
+            __syncthreads();
+            run = kv_run(c, all, kv_steps(s));
+        } else {
+            all = sums[a.R];
+            run = kv_run(c, all, 1);
+        }
     }
-    if (chunks <= 1) return KvParts{0, 0, 0};
-    const int h = hq / a.G, row = (t - a.start[r]) * a.G + hq - h * a.G, tile = row / c.rows;
-    if (tile >= s.tiles) return KvParts{0, 0, 0};
-    KvParts x;
-    x.chunks = chunks;
-    x.stride = (int64_t)s.tiles * c.rows;
-    x.first = ((int64_t)part0 + (int64_t)h * chunks * s.tiles + tile) * c.rows + row - tile * c.rows;
-    return x;
-}
+
+    // The item that step u (< all, uniform) belongs to.
+    __device__ __forceinline__ KvItem item(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums,
+                                           const KvLds &lds, uint64_t u) const
+    {
+        KvItem w;
+        KvShare s;
+        uint64_t first;
+        if (a.R <= kInlineRequests) {
+            w.r = __builtin_ctzll(__ballot(lds.upto[threadIdx.x & 63] > u));
+            first = w.r ? lds.upto[w.r - 1] : 0;
+            s = lds.share[w.r];
+        } else {
+            w.r = __builtin_amdgcn_readfirstlane(kv_find(sums, a.R, u));
+            first = sums[w.r];
+            s = kv_share(a, c, w.r);
+        }
+        auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+        w.n = uniform(s.n);
+        w.ctx = uniform(s.ctx);
+        w.steps = uniform((int)kv_steps(s));
+        w.first_token = uniform(min(max(a.start[w.r], 0), a.T));
+        const uint64_t local = u - first;
+        uint32_t item;
+        if (local < 0xffffffffu) item = (uint32_t)local / (uint32_t)w.steps;
+        else item = (uint32_t)(local / (uint32_t)w.steps);
+        item = uniform(item);
+        w.step = uniform((int)(local - (uint64_t)item * (uint32_t)w.steps));
+        const uint32_t tiles = uniform(s.tiles);
+        w.head = uniform(item / tiles);
+        w.tile = uniform(item - (uint32_t)w.head * tiles);
+        return w;
+    }
+};
+
+// An item that begins in a run and ends in another one, for the join.
+struct KvJoin {
+    int parts;        // runs that it reaches over (0: the run leaves no such item)
+    int first_token, row0, rows, head;
+    int pad[3];
+};
+
+// Place of a run's partial result: the run that an item begins in, or a later one.
+__device__ __forceinline__ int64_t kv_part(uint32_t group, bool begins) { return 2 * (int64_t)group + begins; }
 
 // The keys of a tile and of its rows: row `i` (of n G) sees [lo, hi).
 struct KvRange {
@@ -201,10 +176,11 @@ __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, in
     return v;
 }
 
-// Workgroups [first, first + n) of the kernel of few rows a request; `pad`: they zero the
-// rows of no request as well.
+// The kernel of few rows a request; it zeroes the rows of no request as well if `pad`.
 template <class T>
-void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const KvPlan &p, int cache_dtype, int DP,
-                      uint32_t first, uint32_t n, bool pad, float *o, float2 *ml, hipStream_t st);
+void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, int cache_dtype, int DP,
+                      bool pad, float *o, float2 *ml, KvJoin *joins, hipStream_t st);
+// its waves a SIMD
+int kv_decode_waves(int cache_dtype, int DP);
 
 }  // namespace dro

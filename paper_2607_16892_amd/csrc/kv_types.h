@@ -38,4 +38,15 @@ template <class T, bool kHigh> __device__ __forceinline__ uint32_t unpack_fp8(ui
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHigh));
 }
 
+// component d of a value row of the cache
+template <class C> __device__ __forceinline__ float value_at(const char *row, int d)
+{
+    if constexpr (sizeof(C) == 1) {
+        const uint32_t w = ((const uint8_t *)row)[d];
+        return __builtin_bit_cast(float, unpack_fp8<bf16, false>(w) << 16);
+    } else {
+        return to_float(((const C *)row)[d]);
+    }
+}
+
 }  // namespace dro

@@ -88,6 +88,19 @@ def test_long_contexts(ctx, dev, Hq, H, D, dtype, cache, new):
     c.check(c.run(ctx))
 
 
+@pytest.mark.parametrize("R,most,new", [(65, 300, 1), (130, 120, 5), (700, 40, 1), (64, 900, 2), (200, 3000, 1),
+                                        (1500, 9, 2)])
+def test_many_requests(ctx, dev, R, most, new):
+    # more requests than a wave has lanes, some without tokens, one long among short ones
+    r = np.random.default_rng(R)
+    lens = r.integers(0, most + 1, R).tolist()
+    lens[R // 3] = 4 * most
+    news = [int(min(x, n)) for x, n in zip(lens, r.integers(0, new + 1, R))]
+    print(f"[gpu] kv many R={R}", flush=True)
+    c = Case(dev, lens, news, 4, 2, 64, "f16", seed=R)
+    c.check(c.run(ctx))
+
+
 @pytest.mark.parametrize("new", [1, 3, 60])
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f16", 64), ("bf16", 256)])
 def test_hidden_places_may_hold_anything(ctx, dev, new, dtype, D):
