@@ -35,6 +35,8 @@ UNITS = {
     "kv_attention.hip": [],
     "kv_decode_bf16.hip": [],
     "kv_decode_f16.hip": [],
+    "kv_prefill_bf16.hip": [],
+    "kv_prefill_f16.hip": [],
 }
 
 

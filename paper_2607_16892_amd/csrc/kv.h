@@ -59,7 +59,6 @@ struct KvAttnArgs {
     const float *slopes;
     const int32_t *prefix;
 };
-inline size_t kv_rup(size_t v) { return (v + 255) & ~size_t(255); }
 // bytes of scratch that a call needs
 size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype);
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st);

@@ -45,10 +45,55 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs 
     if (threadIdx.x == 0) sums[a.R] = total;
 }
 
+// The tiles of the requests of many rows, in order, and the sums of their steps: first the
+// tiles before each request, then the list, 1024 tiles at a time.
+__global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs a, const KvCut cut, int keys, int most,
+                                                                uint64_t *before, uint64_t *sums, int2 *tiles,
+                                                                int *count)
+{
+    __shared__ uint64_t part[kPlanThreads / 64];
+    const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
+    const int r0 = min((int)threadIdx.x * per, a.R), r1 = min(r0 + per, a.R);
+    uint64_t mine = 0, total;
+    for (int r = r0; r < r1; ++r) mine += kv_share(a, cut, r).tiles;
+    uint64_t at = plan_scan(mine, part, total) - mine;
+    for (int r = r0; r < r1; ++r) {
+        before[r] = at;
+        at += kv_share(a, cut, r).tiles;
+    }
+    __syncthreads();  // (makes `before` visible to the workgroup)
+    const int n = (int)min(total, (uint64_t)most);
+    uint64_t steps_before = 0;
+    for (int e0 = 0; e0 < n; e0 += kPlanThreads) {
+        const int e = e0 + threadIdx.x;
+        uint32_t steps = 0;
+        if (e < n) {
+            int lo = 0, hi = a.R;  // the last request with before[r] <= e: it has tiles
+            while (hi - lo > 1) {
+                const int m = (lo + hi) >> 1;
+                if (before[m] <= (uint64_t)e) lo = m;
+                else hi = m;
+            }
+            const KvShare s = kv_share(a, cut, lo);
+            const int tile = e - (int)before[lo];
+            steps = kv_tile_steps(a, s, lo, tile, cut.rows, keys);
+            tiles[e] = make_int2(lo, tile);
+        }
+        const uint64_t upto = plan_scan(steps, part, total);
+        if (e < n) sums[e] = steps_before + upto - steps;
+        steps_before += total;
+    }
+    if (threadIdx.x == 0) {
+        sums[n] = steps_before;
+        count[0] = n;
+    }
+}
+
 // ---- join -------------------------------------------------------------------------
 //
-// Workgroup (b, y): if an item begins in run b and ends in a later one, rows of it from the
-// partial results of the runs that it reaches over.  The run left what there is to do.  Up
+// Workgroup (b, y): for each run of PER from b PER on that an item begins in and does not
+// end in, rows of the item from the partial results of the runs that it reaches over.  The
+// runs left what there is to do.  Up
 // to kFewParts parts a wave joins a row; more (a long request alone) the waves share, a
 // workgroup to a row.  Bound by latency (the parts come from other dies' caches), so a wave
 // asks for kAhead parts at once.
@@ -56,17 +101,21 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs 
 constexpr int kFewParts = 16;
 constexpr int kAhead = 8;
 
-template <class T, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a, int tile_rows, const float *part_o,
+template <class T, int DP, int WAVES, int PER>
+__global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a, int tile_rows, int runs, const float *part_o,
                                                                   const float2 *part_ml, const KvJoin *joins)
 {
     constexpr int V = DP / 64;
     __shared__ float2 red[WAVES];
     __shared__ float acc[WAVES][DP];
-    const KvJoin it = joins[blockIdx.x];
-    if (it.parts == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float scale = a.v_scale ? a.v_scale[it.head] : 1.0f;
+    int run = blockIdx.x * PER;
+    uint64_t todo = 1;
+    if constexpr (PER > 1) {
+        static_assert(PER <= 64, "a lane per run");
+        todo = __ballot(lane < PER && run + lane < runs && joins[run + lane].parts != 0);
+    }
+    KvJoin it;
     float m, l, o[V];
     auto join = [&](float2 x, const float *z) {
         if (x.y == 0.0f) return;  // no key that the row sees
@@ -90,7 +139,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int n = min(c + i * by, it.parts - 1);
-                const int64_t at = kv_part(blockIdx.x + n, n == 0) * tile_rows + y;
+                const int64_t at = kv_part(run + n, n == 0) * tile_rows + y;
                 x[i] = part_ml[at];
                 z[i] = *(const Vec<float, V> *)(part_o + at * DP + lane * V);
             }
@@ -106,30 +155,35 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
     auto write = [&](int y) {
         const int row = it.row0 + y, token = row / a.G, hq = it.head * a.G + row - token * a.G;
         const int64_t t = it.first_token + token;
-        const float inv = l == 0.0f ? 0.0f : scale / l;
+        const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[it.head] : 1.0f) / l;
         T *out = (T *)a.out + t * a.out_token + hq * a.out_head + lane * V;
         for (int j = 0; j < V; ++j)
             if (lane * V + j < a.D) out[j] = (T)(l == 0.0f ? 0.0f : o[j] * inv);
         if (a.lse && lane == 0)
             a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     };
-    if (it.parts <= kFewParts) {
-        for (int y = blockIdx.y * WAVES + wave; y < it.rows; y += gridDim.y * WAVES) {
-            sum(y, 0, 1);
-            write(y);
+    for (; todo; todo &= todo - 1) {
+        run = blockIdx.x * PER + (PER > 1 ? __builtin_ctzll(todo) : 0);
+        it = joins[run];
+        if (it.parts == 0) continue;
+        if (it.parts <= kFewParts) {
+            for (int y = blockIdx.y * WAVES + wave; y < it.rows; y += gridDim.y * WAVES) {
+                sum(y, 0, 1);
+                write(y);
+            }
+            continue;
         }
-        return;
-    }
-    for (int y = blockIdx.y; y < it.rows; y += gridDim.y) {
-        sum(y, wave, WAVES);
-        if (lane == 0) red[wave] = make_float2(m, l);
-        for (int j = 0; j < V; ++j) acc[wave][lane * V + j] = o[j];
-        __syncthreads();
-        if (wave == 0) {
-            for (int w = 1; w < WAVES; ++w) join(red[w], &acc[w][lane * V]);
-            write(y);
+        for (int y = blockIdx.y; y < it.rows; y += gridDim.y) {
+            sum(y, wave, WAVES);
+            if (lane == 0) red[wave] = make_float2(m, l);
+            for (int j = 0; j < V; ++j) acc[wave][lane * V + j] = o[j];
+            __syncthreads();
+            if (wave == 0) {
+                for (int w = 1; w < WAVES; ++w) join(red[w], &acc[w][lane * V]);
+                write(y);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -137,58 +191,115 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
 
 static int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-static KvCut decode_cut(const KvAttnArgs &a, int cache_dtype)
+// Requests of up to this many rows a key head are the one kernel's, others the other's.
+constexpr int kFewRows = 32;
+
+struct KvPlans {
+    KvCut few, many;       // groups == 0: not launched
+    int most_tiles;        // of the requests of many rows
+};
+
+static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
 {
-    KvCut c;
-    c.rows = 16;
-    c.groups = a.num_cu * 4 * kv_decode_waves(cache_dtype, padded_dim(a.D));
-    c.few = 0x7fffffff;
-    c.below = true;
-    return c;
+    const int DP = padded_dim(a.D), few = std::max(kFewRows / a.G, 1);
+    const bool all_few = a.max_new <= few;
+    KvPlans p{};
+    p.few.rows = 16;
+    p.few.groups = a.num_cu * 4 * kv_decode_waves(cache_dtype, DP);
+    p.few.few = all_few ? 0x7fffffff : few;
+    p.few.below = true;
+    if (!all_few) {
+        p.many.rows = 128;
+        p.many.groups = a.num_cu * kv_prefill_groups(DP) / kDies * kDies;
+        p.many.few = few;
+        p.many.below = false;
+        p.most_tiles = (int)((int64_t)a.T * a.G / p.many.rows + std::min(a.R, a.T / (few + 1) + 1));
+    }
+    return p;
+}
+
+struct KvWork {
+    float *o;
+    float2 *ml;
+    KvJoin *joins;
+    uint64_t *sums;    // few rows: [R + 1]
+    uint64_t *before, *tile_sums;
+    int2 *tiles;
+    int *count;
+    size_t bytes;
+};
+
+static KvWork work_of(const KvAttnArgs &a, const KvPlans &p, void *ws)
+{
+    KvWork w{};
+    char *at = (char *)ws;
+    auto take = [&](size_t bytes) {
+        char *q = at;
+        at += (bytes + 255) & ~size_t(255);
+        return q;
+    };
+    // the kernels run one after the other: their partial results share one place
+    const size_t rows = (size_t)2 * std::max((size_t)p.few.groups * p.few.rows, (size_t)p.many.groups * p.many.rows);
+    w.o = (float *)take(rows * padded_dim(a.D) * 4);
+    w.ml = (float2 *)take(rows * 8);
+    w.joins = (KvJoin *)take(std::max(p.few.groups, p.many.groups) * sizeof(KvJoin));
+    w.sums = (uint64_t *)take(((size_t)a.R + 1) * 8);
+    if (p.many.groups) {
+        w.before = (uint64_t *)take((size_t)a.R * 8);
+        w.tile_sums = (uint64_t *)take(((size_t)p.most_tiles + 1) * 8);
+        w.tiles = (int2 *)take((size_t)p.most_tiles * 8);
+        w.count = (int *)take(4);
+    }
+    w.bytes = at - (char *)ws;
+    return w;
 }
 
 size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype)
 {
-    const KvCut c = decode_cut(a, cache_dtype);
-    const size_t rows = (size_t)2 * c.groups * c.rows;
-    return kv_rup(rows * padded_dim(a.D) * 4) + kv_rup(rows * 8) + kv_rup(((size_t)a.R + 1) * 8) +
-           kv_rup(c.groups * sizeof(KvJoin));
+    return work_of(a, plans(a, cache_dtype), nullptr).bytes;
+}
+
+template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, const KvWork &w, int DP, hipStream_t st)
+{
+    // few items may have many parts and are few among the runs: sixteen waves to a row, 32
+    // runs a workgroup; else a wave to a row, and a run
+    const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
+    const bool few = c.rows == 16 && a.R * (int64_t)a.H <= 64;
+    const dim3 grid(few ? (c.groups + 31) / 32 : c.groups, few ? most : std::min((most + 3) / 4, 16u));
+    auto join = [&](auto kernel) {
+        kernel<<<grid, few ? 1024 : 256, 0, st>>>(a, c.rows, c.groups, w.o, w.ml, w.joins);
+    };
+    auto pick = [&](auto waves, auto per) {
+        constexpr int W = decltype(waves)::value, P = decltype(per)::value;
+        join(DP == 64 ? kv_join_kernel<T, 64, W, P> : DP == 128 ? kv_join_kernel<T, 128, W, P>
+                                                                : kv_join_kernel<T, 256, W, P>);
+    };
+    if (few) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 32>{});
+    else pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+}
+
+template <class T>
+static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w, int cache_dtype, hipStream_t st)
+{
+    const int DP = padded_dim(a.D);
+    if (p.many.groups) {
+        kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles, w.before,
+                                                    w.tile_sums, w.tiles, w.count);
+        const KvTiles t{w.tile_sums, w.tiles, w.count};
+        launch_kv_prefill<T>(a, p.many, t, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
+        launch_join<T>(a, p.many, w, DP, st);
+    }
+    if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);
+    launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, !p.many.groups, w.o, w.ml, w.joins, st);
+    launch_join<T>(a, p.few, w, DP, st);
 }
 
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st)
 {
-    const KvCut c = decode_cut(a, cache_dtype);
-    const int DP = padded_dim(a.D);
-    const size_t rows = (size_t)2 * c.groups * c.rows;
-    char *p = (char *)ws;
-    auto take = [&](size_t bytes) {
-        char *q = p;
-        p += kv_rup(bytes);
-        return q;
-    };
-    float *o = (float *)take(rows * DP * 4);
-    float2 *ml = (float2 *)take(rows * 8);
-    uint64_t *sums = (uint64_t *)take(((size_t)a.R + 1) * 8);
-    KvJoin *joins = (KvJoin *)take(c.groups * sizeof(KvJoin));
-    if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, c, sums);
-    if (dtype == DRO_BF16) launch_kv_decode<bf16>(a, c, sums, cache_dtype, DP, true, o, ml, joins, st);
-    else launch_kv_decode<f16>(a, c, sums, cache_dtype, DP, true, o, ml, joins, st);
-    // few items may have many parts: sixteen waves to a row; else four rows a workgroup
-    const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
-    const bool few = a.R * (int64_t)a.H <= 64;
-    const dim3 grid(c.groups, few ? most : (most + 3) / 4);
-    auto join = [&](auto kernel) { kernel<<<grid, few ? 1024 : 256, 0, st>>>(a, c.rows, o, ml, joins); };
-    auto pick = [&](auto t, auto w) {
-        using T = decltype(t);
-        constexpr int W = decltype(w)::value;
-        join(DP == 64 ? kv_join_kernel<T, 64, W> : DP == 128 ? kv_join_kernel<T, 128, W> : kv_join_kernel<T, 256, W>);
-    };
-    auto waves = [&](auto t) {
-        if (few) pick(t, std::integral_constant<int, 16>{});
-        else pick(t, std::integral_constant<int, 4>{});
-    };
-    if (dtype == DRO_BF16) waves(bf16{});
-    else waves(f16{});
+    const KvPlans p = plans(a, cache_dtype);
+    const KvWork w = work_of(a, p, ws);
+    if (dtype == DRO_BF16) run_attention<bf16>(a, p, w, cache_dtype, st);
+    else run_attention<f16>(a, p, w, cache_dtype, st);
     return hipGetLastError();
 }
 

@@ -20,10 +20,6 @@ namespace dro {
 
 constexpr int kDecodeRows = 16;
 
-// Running maxima are raised only when a step exceeds them by 2^kSlack, so most steps
-// rescale nothing; weights stay below 2^kSlack.
-constexpr float kSlack = 8.0f;
-
 // Waves a SIMD, so registers: the keys of the next step and this one's values (32 x 256
 // bytes each) take 64 of a wave's, beside queries and sums.
 constexpr int decode_waves(int bytes) { return bytes >= 256 ? 2 : bytes >= 128 ? 3 : 4; }
@@ -45,21 +41,7 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
 
     const int lane = threadIdx.x, n16 = lane & 15, grp = lane >> 4;
 
-    if (pad) {  // rows of no request
-        const int t0 = min(max(a.start[0], 0), a.T), t1 = min(max(a.start[a.R], 0), a.T);
-        const int lost = t0 + a.T - t1;
-        for (int x = blockIdx.x; x < lost; x += gridDim.x) {
-            const int t = x < t0 ? x : t1 + x - t0;
-            for (int i = threadIdx.x; i < a.Hq * a.D; i += 64) {
-                const int h = i / a.D;
-                ((T *)a.out)[t * a.out_token + h * a.out_head + (i - h * a.D)] = (T)0.0f;
-            }
-            if (a.lse)
-                for (int h = threadIdx.x; h < a.Hq; h += 64)
-                    a.lse[(int64_t)t * a.Hq + h] = -INFINITY;
-        }
-    }
-
+    if (pad) zero_rows<T>(a);
     KvSched sched;
     sched.init(a, cut, sums, lds);
     if (threadIdx.x == 0) joins[blockIdx.x].parts = 0;

@@ -13,6 +13,10 @@ typedef Vec<uint32_t, 4> u32x4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// Running maxima are raised only when a step exceeds them by 2^kSlack, so most steps
+// rescale nothing; weights stay below 2^kSlack.
+constexpr float kSlack = 8.0f;
+
 // 16 x 16 tile over 32 products.  First operand: lane holds row lane % 16, products
 // (lane / 16) 8 .. + 8; second: column lane % 16, the same products; result: column
 // lane % 16, rows (lane / 16) 4 .. + 4.
@@ -94,6 +98,22 @@ template <int N> __device__ __forceinline__ Words<N> load_words(const char *base
         x.w[0] = *(const uint32_t *)(base + off);
     }
     return x;
+}
+
+// The rows of no request, by all workgroups.
+template <class T> __device__ __forceinline__ void zero_rows(const KvAttnArgs &a)
+{
+    const int t0 = min(max(a.start[0], 0), a.T), t1 = min(max(a.start[a.R], 0), a.T);
+    const int lost = t0 + a.T - t1;
+    for (int x = blockIdx.x; x < lost; x += gridDim.x) {
+        const int t = x < t0 ? x : t1 + x - t0;
+        for (int i = threadIdx.x; i < a.Hq * a.D; i += blockDim.x) {
+            const int h = i / a.D;
+            ((T *)a.out)[t * a.out_token + h * a.out_head + (i - h * a.D)] = (T)0.0f;
+        }
+        if (a.lse)
+            for (int h = threadIdx.x; h < a.Hq; h += blockDim.x) a.lse[(int64_t)t * a.Hq + h] = -INFINITY;
+    }
 }
 
 }  // namespace dro

@@ -28,6 +28,10 @@ struct KvItem {
     int step, steps;  // the item's step asked for, and how many it has
 };
 
+// Many rows a request: the tiles of all requests in order are listed first (their steps
+// differ, as a tile's keys end where its last row's do), and the steps of the list, head by
+// head, are dealt in equal runs in the same way.
+
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
     int rows;      // of a tile
@@ -176,11 +180,46 @@ __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, in
     return v;
 }
 
-// The kernel of few rows a request; it zeroes the rows of no request as well if `pad`.
+// ---- many rows a request ------------------------------------------------------------
+
+constexpr int kDies = 8;  // workgroups go to the dies (an L2 each) in turn
+
+struct KvTiles {
+    const uint64_t *sums;  // [count + 1] exclusive sums of the tiles' steps
+    const int2 *tiles;     // [count] request and tile
+    const int *count;      // [1]
+};
+
+// Steps of `keys` keys of a tile.
+__device__ __forceinline__ uint32_t kv_tile_steps(const KvAttnArgs &a, const KvShare &s, int r, int tile, int rows,
+                                                  int keys)
+{
+    const int prefix = a.prefix ? a.prefix[r] : 0, row0 = tile * rows;
+    const int last = min(s.n - 1, (row0 + rows - 1) / a.G);
+    const int lo = kv_row_range(a, s.ctx, s.n, row0 / a.G, prefix).lo & ~31;
+    const int hi = kv_row_range(a, s.ctx, s.n, last, prefix).hi;
+    return (uint32_t)max((hi - lo + keys - 1) / keys, 1);
+}
+
+// Steps a workgroup: a part of a tile costs about as much as two steps to write and join.
+__device__ __forceinline__ uint64_t kv_tile_run(const KvCut &c, uint64_t all)
+{
+    return max((all + (uint32_t)c.groups - 1) / (uint32_t)c.groups, (uint64_t)4);
+}
+
+// The kernels of few and of many rows a request; they zero the rows of no request as well
+// if `pad`.
 template <class T>
 void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, int cache_dtype, int DP,
                       bool pad, float *o, float2 *ml, KvJoin *joins, hipStream_t st);
 // its waves a SIMD
 int kv_decode_waves(int cache_dtype, int DP);
+
+template <class T>
+void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, int cache_dtype, int DP, bool pad,
+                       float *o, float2 *ml, KvJoin *joins, hipStream_t st);
+// its workgroups a compute unit, and keys a step
+int kv_prefill_groups(int DP);
+int kv_prefill_keys(int DP);
 
 }  // namespace dro
