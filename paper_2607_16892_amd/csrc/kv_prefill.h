@@ -8,8 +8,10 @@
 //   O^T = V^T P^T      components x rows
 // so the softmax of a row is a lane's own work and one exchange with lane + 32, the
 // weights are the second operand as they stand (the order of the keys within a product
-// is theirs; V^T lies in LDS in that order), and rescaling a row is a lane's own product.
-// The next tile is on its way from memory to registers while one is worked on.
+// is theirs), and rescaling a row is a lane's own product.  Rows of both tiles lie in LDS
+// in pieces of 16 bytes whose order is turned from row to row, so that the reads, along
+// the rows and (transposed) across them, meet all banks.  16-bit caches go from memory to
+// LDS directly, the next tile while one is worked on.
 #pragma once
 
 #include "kv_math.h"
@@ -47,7 +49,18 @@ __device__ __forceinline__ float sum_halves(float x)
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
-template <class T, class C, int DP, bool MODS>
+// Where piece c (8 components) of row r lies within the row: a read of one piece of 16
+// rows, and one of 4 pieces of 4 rows, touch 16 different sixteenths of the banks.
+template <int DP> __device__ __forceinline__ int key_turn(int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; }
+template <int DP> __device__ __forceinline__ int value_turn(int r)
+{
+    return DP == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2;
+}
+
+typedef const __attribute__((address_space(1))) void *GlobalPtr;
+typedef __attribute__((address_space(3))) void *LdsPtr;
+
+template <class T, class C, int DP, bool MODS, bool FULL>
 __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     const KvAttnArgs a, const KvCut cut, const KvTiles tiles, bool pad, float *part_o, float2 *part_ml,
     KvJoin *joins)
@@ -58,13 +71,14 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     constexpr int S = DP / 16;           // steps of 16 components of a score
     constexpr int NT = KT / 32;          // score tiles
     constexpr int ND = DP / 32;          // component tiles
-    constexpr int KRow = DP * 2 + 16;    // bytes of a key's row, and of a component's row of
-    constexpr int VRow = KT * 2 + 16;    // values: 16 more, so 16 rows start on all banks
-    constexpr int KG = KT / 8;           // groups of 8 keys
-    constexpr int W = E * 2;             // dwords of 8 components in the cache
-    __shared__ __align__(16) char sk[2][KT * KRow];
-    __shared__ __align__(16) char sv[2][DP * VRow];
-    __shared__ int odd[2][2];  // a tile holds such values, by the wave that staged them
+    constexpr int Row = DP * 2;          // bytes of a row in LDS
+    constexpr int NC = DP / 8;           // pieces of a row
+    constexpr int NG = KT / 16;          // groups of 16 keys (each within one block)
+    constexpr int UP = 2 * NG / 4;       // groups of keys or of values that a wave stages
+    constexpr int IP = DP / 32;          // its loads for one: 64 pieces each
+    constexpr int RP = 64 / NC;          // rows of a load
+    constexpr int Tile = KT * Row;
+    __shared__ __align__(16) char stage[2][2][Tile];  // two tiles of keys and of values
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -74,6 +88,10 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
     if (pad) zero_rows<T>(a);
     if (threadIdx.x == 0) joins[group].parts = 0;
+    if (!FULL) {  // pieces beyond the rows' ends are never written
+        for (int i = threadIdx.x; i < 4 * Tile / 16; i += 256) ((u32x4 *)stage)[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
     const uint64_t all1 = tiles.sums[tiles.count[0]], all = all1 * a.H;
     const uint64_t run = kv_tile_run(cut, all);
     uint64_t unit = group * run;
@@ -115,94 +133,91 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 const int d = s * 16 + half * 8;
-                q[s] = d < a.D ? *(const u32x4 *)(p + 2 * d) : u32x4{0, 0, 0, 0};
+                q[s] = FULL || d < a.D ? *(const u32x4 *)(p + 2 * d) : u32x4{0, 0, 0, 0};
             }
         }
         const float ks = F8 ? a.scale * a.k_scale[h] : a.scale;
-        const float to_exp = MODS ? ks : ks * kLog2e;
         const float slope = MODS && a.slopes ? a.slopes[hq] : 0.0f;
         const float inv_cap = MODS && a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+        float to_exp = ks;
+        if constexpr (!MODS) {  // scale > 0 from here on, so the largest score has the largest weight
+            to_exp = fabsf(ks) * kLog2e;
+            if (ks < 0.0f)
+#pragma unroll
+                for (int s = 0; s < S; ++s) q[s] ^= 0x80008000u;
+        }
 
-        // Staging: waves 0 and 1 take the values (8 keys x 8 components a thread, in the
-        // order of the products), waves 2 and 3 the keys (8 rows x 8 components).  A
-        // thread's keys lie in one group of 16, so in one block.
-        const bool values = wave < 2;
-        const int st = threadIdx.x & 127;
-        const int kg = st % KG, dg = st / KG;              // values
-        const int kc = st % (DP / 8), kr = st / (DP / 8);  // keys
-        const int in_tile = values ? (kg >> 1) * 16 : (kr >> 1) * 16;
-        const int in_group = values ? (kg & 1) * 4 : (kr & 1) * 8;
-        const int sd = (values ? dg : kc) * 8;
-        const char *src = values ? (const char *)a.v + (int64_t)h * a.v_head * E
-                                 : (const char *)a.k + (int64_t)h * a.k_head * E;
-        const int64_t s_block = (values ? a.v_block : a.k_block) * E;
-        const int s_token = (int)(values ? a.v_token : a.k_token) * E;
-        const int s_skip = values ? 8 * s_token : 4 * s_token;  // from row 3 to row 4, less 4 rows
+        // Staging: piece x = lane of load i of group j goes to place 1024 i + 16 lane of the
+        // group's rows, so the lane picks the piece of its row that belongs there.
         const int32_t *table = a.table + (int64_t)r * a.table_stride;
         const int in_block = (1 << a.shift) - 1;
-        int id = 0;
-        auto load_id = [&](int u) { id = table[min(k0 + u * KT + in_tile, k1 - 1) >> a.shift]; };
-        Words<W> reg[8];
-        auto load = [&](int u) {
-            const int at = ((k0 + u * KT + in_tile) & in_block) + in_group;
-            const char *p = src + min(max(id, 0), a.num_blocks - 1) * s_block + (uint32_t)(at * s_token + sd * E);
-            const char *p4 = p + s_skip;
+        int ids[UP];
+        auto load_ids = [&](int u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                Words<W> x{};
-                if (sd < a.D) x = load_words<W>((i < 4 ? p : p4) + (i & 3) * (int64_t)s_token, 0);
-                reg[i] = x;
+            for (int j = 0; j < UP; ++j)
+                ids[j] = table[min(k0 + u * KT + (wave + 4 * j) % NG * 16, k1 - 1) >> a.shift];
+        };
+        Words<2> reg[F8 ? UP * IP : 1];
+        auto load = [&](int u) {
+#pragma unroll
+            for (int j = 0; j < UP; ++j) {
+                const bool vals = (wave + 4 * j) / NG;
+                const int group = (wave + 4 * j) % NG;
+                const int64_t s_token = vals ? a.v_token : a.k_token;
+                const char *base = (vals ? (const char *)a.v + h * a.v_head * E : (const char *)a.k + h * a.k_head * E) +
+                                   ((int64_t)min(max(ids[j], 0), a.num_blocks - 1) * (vals ? a.v_block : a.k_block) +
+                                    ((k0 + u * KT + group * 16) & in_block) * s_token) * E;
+#pragma unroll
+                for (int i = 0; i < IP; ++i) {
+                    const int rr = i * RP + lane / NC;
+                    const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
+                    const uint32_t off = (uint32_t)(lane / NC * (int)s_token + c * 8) * E;
+                    const char *p = base + i * RP * s_token * E;
+                    if (FULL || c * 8 < a.D) {
+                        if constexpr (F8)
+                            reg[j * IP + i] = load_words<2>(p, off);
+                        else
+                            __builtin_amdgcn_global_load_lds((GlobalPtr)(p + off),
+                                                             (LdsPtr)&stage[u & 1][vals][group * 16 * Row + i * 1024],
+                                                             16, 0, 0);
+                    }
+                }
             }
         };
-        auto key_of = [&](int i) { return in_tile + in_group + (values ? (i >> 2) * 8 + (i & 3) : i); };
-        // registers to LDS; values that no row of the tile of rows sees become zero, and in
-        // tiles that hide keys from some rows infinities and NaN do, for `odd`
-        auto store = [&](int u) {
-            const int b = u & 1, key0 = k0 + u * KT;
-            u32x4 x[8];
-            if (values) {
-                const bool edge = key0 < bot.lo || key0 + KT > min(top.hi, k1);
-                if (edge) {
-                    uint32_t bad = 0;
+        auto store = [&](int u) {  // fp8: widened on the way
+            if constexpr (F8) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int key = key0 + key_of(i);
-                        const bool keep = key >= top.lo && key < bot.hi;
+                for (int j = 0; j < UP; ++j) {
+                    const bool vals = (wave + 4 * j) / NG;
+                    const int group = (wave + 4 * j) % NG;
 #pragma unroll
-                        for (int j = 0; j < W; ++j) {
-                            const uint32_t w = keep ? reg[i].w[j] : 0, mask = nonfinite_mask<C>(w);
-                            bad |= mask;
-                            reg[i].w[j] = w & ~mask;
-                        }
+                    for (int i = 0; i < IP; ++i) {
+                        const Words<2> &x = reg[j * IP + i];
+                        const int rr = i * RP + lane / NC;
+                        const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
+                        if (FULL || c * 8 < a.D)
+                            *(u32x4 *)&stage[u & 1][vals][group * 16 * Row + i * 1024 + lane * 16] =
+                                u32x4{unpack_fp8<T, false>(x.w[0]), unpack_fp8<T, true>(x.w[0]),
+                                      unpack_fp8<T, false>(x.w[1]), unpack_fp8<T, true>(x.w[1])};
                     }
-                    bad = __any(bad);
-                    if (lane == 0) odd[b][wave] = bad;
-                } else if (lane == 0) {
-                    odd[b][wave] = 0;
                 }
             }
+        };
+        // 8 weights' worth of component n32 of tile j: keys 16 x + 4 half + {0 .. 3, 8 .. 11}
+        auto value_frag = [&](const char *sv, int x, int j) {
+            u32x4 y;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (F8)
-                    x[i] = u32x4{unpack_fp8<T, false>(reg[i].w[0]), unpack_fp8<T, true>(reg[i].w[0]),
-                                 unpack_fp8<T, false>(reg[i].w[1]), unpack_fp8<T, true>(reg[i].w[1])};
-                else
-                    x[i] = u32x4{reg[i].w[0], reg[i].w[1], reg[i].w[2], reg[i].w[3]};
+            for (int e = 0; e < 2; ++e) {
+                const int i = lane & 15, rr = x * 16 + e * 8 + half * 4 + (i >> 2);
+                const int d = j * 32 + (lane & 16) + (i & 3) * 4;
+                const auto z = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) Vec<short, 4> *)(sv + rr * Row + ((d >> 3) ^ value_turn<DP>(rr)) * 16 +
+                                                                        (d & 4) * 2));
+                const Vec<uint32_t, 2> w = __builtin_bit_cast(Vec<uint32_t, 2>, z);
+                y[2 * e] = w[0];
+                y[2 * e + 1] = w[1];
             }
-            if (values) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {  // component 8 dg + j: keys in order
-                    u32x4 y;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        y[c] = __builtin_amdgcn_perm(x[2 * c + 1][j / 2], x[2 * c][j / 2],
-                                                     j & 1 ? 0x07060302u : 0x05040100u);
-                    *(u32x4 *)&sv[b][(dg * 8 + j) * VRow + kg * 16] = y;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) *(u32x4 *)&sk[b][(kr * 8 + i) * KRow + kc * 16] = x[i];
-            }
+            return y;
         };
 
         float m = -INFINITY, l = 0.0f;
@@ -214,17 +229,19 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
         __syncthreads();  // the last item's tiles are read
         if (steps) {
-            load_id(0);
+            load_ids(0);
             load(0);
-            load_id(1);
+            load_ids(1);
             store(0);
         }
         for (int u = 0; u < steps; ++u) {
             const int b = u & 1, key0 = k0 + u * KT;
-            __syncthreads();  // tile u is in LDS, tile u - 1 is read
+            const char *sk = stage[b][0], *sv = stage[b][1];
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile u has landed
+            __syncthreads();                     // everybody's has, and tile u - 1 is read
             if (u + 1 < steps) {
                 load(u + 1);
-                load_id(u + 2);
+                load_ids(u + 2);
             }
             const bool none = idle || key0 >= wbot.hi || key0 + KT <= wtop.lo;
             if (!none) {
@@ -235,25 +252,31 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
                     for (int x = 0; x < S; ++x)
-                        s[t] = mfma32<T>(*(const u32x4 *)&sk[b][(t * 32 + n32) * KRow + x * 32 + half * 16], q[x], s[t]);
+                        s[t] = mfma32<T>(*(const u32x4 *)&sk[(t * 32 + n32) * Row +
+                                                             ((2 * x + half) ^ key_turn<DP>(n32)) * 16], q[x], s[t]);
                 }
                 const bool edge = key0 < wbot.lo || key0 + KT > min(wtop.hi, k1);
+                const int lane0 = key0 + half * 4, from = see.lo - lane0, dist = lane0 - p_row;
+                const uint32_t seen = (uint32_t)max(see.hi - see.lo, 0);
                 float mt = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int key = key0 + t * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
+                        const int c = t * 32 + (i >> 2) * 8 + (i & 3);  // the key less `lane0`
                         if constexpr (MODS) {
                             float x = s[t][i] * to_exp;
                             if (a.cap > 0.0f) x = a.cap * tanh_fast(x * inv_cap);
-                            s[t][i] = (x + slope * (float)(key - p_row)) * kLog2e;
-                        } else {
-                            s[t][i] *= to_exp;
+                            s[t][i] = (x + slope * (float)(c + dist)) * kLog2e;
                         }
-                        if (edge) s[t][i] = key >= see.lo && key < see.hi ? s[t][i] : -INFINITY;
-                        mt = fmaxf(mt, s[t][i]);
+                        if (edge) s[t][i] = (uint32_t)(c - from) < seen ? s[t][i] : -INFINITY;
                     }
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[t][i]);
+                const float by = MODS ? 1.0f : to_exp;
+                mt *= by;
                 mt = max_halves(mt);
                 if (__any(mt > m + kSlack)) {
                     const float to = fmaxf(m, mt);
@@ -271,18 +294,53 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - mu);
-                        s[t][i + 1] = __builtin_amdgcn_exp2f(s[t][i + 1] - mu);
+                        s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], by, -mu));
+                        s[t][i + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], by, -mu));
                         l += s[t][i] + s[t][i + 1];
                         w[2 * t + (i >> 3)][(i >> 1) & 3] = pack2<T>(s[t][i], s[t][i + 1]);
                     }
-                if (odd[b][0] | odd[b][1]) {  // (rare) infinities and NaN, to the rows that see them
+                if (!edge) {
+#pragma unroll
+                    for (int x = 0; x < NT * 2; ++x)
+#pragma unroll
+                        for (int j = 0; j < ND; ++j) o[j] = mfma32<T>(value_frag(sv, x, j), w[x], o[j]);
+                } else {
+                    // a weight of zero does not silence an infinity or a NaN: values that no row
+                    // of the wave sees become zero, and those that some see are added apart, to
+                    // these rows alone
+                    const int wfrom = wtop.lo - lane0, wupto = min(wbot.hi, k1) - lane0;
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int x = 0; x < NT * 2; ++x) {
+                        u32x4 keep;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int k = x * 16 + (c >> 1) * 8 + (c & 1) * 2;
+                            keep[c] = (k >= wfrom && k < wupto ? 0xffffu : 0u) |
+                                      (k + 1 >= wfrom && k + 1 < wupto ? 0xffff0000u : 0u);
+                        }
+#pragma unroll
+                        for (int j = 0; j < ND; ++j) {
+                            u32x4 y = value_frag(sv, x, j) & keep;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const uint32_t mask = nonfinite_mask<T>(y[c]);
+                                bad |= mask;
+                                y[c] &= ~mask;
+                            }
+                            o[j] = mfma32<T>(y, w[x], o[j]);
+                        }
+                    }
+                    if (__any(bad)) {
                     for (int x = 0; x < NT * 16; ++x) {
                         float mine = 0.0f;
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) mine = x == t * 16 + i ? s[t][i] : mine;
+                            for (int i = 0; i < 16; ++i) {
+                                mine = x == t * 16 + i ? s[t][i] : mine;
+                                __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
+                            }
                         for (int g = 0; g < 2; ++g) {
                             const float wt = __shfl(mine, n32 + 32 * g);
                             const int key = key0 + (x >> 4) * 32 + ((x >> 2) & 3) * 8 + g * 4 + (x & 3);
@@ -298,18 +356,14 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
                                     const int d = j * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-                                    const float y = d < D ? value_at<C>(at, d) : 0.0f;
+                                    const float y = FULL || d < D ? value_at<C>(at, d) : 0.0f;
                                     o[j][i] += seen && !__builtin_isfinite(y) ? wt * y : 0.0f;
                                     __builtin_amdgcn_sched_barrier(0);
                                 }
                         }
                     }
+                    }
                 }
-#pragma unroll
-                for (int x = 0; x < NT * 2; ++x)
-#pragma unroll
-                    for (int j = 0; j < ND; ++j)
-                        o[j] = mfma32<T>(*(const u32x4 *)&sv[b][(j * 32 + n32) * VRow + x * 32 + half * 16], w[x], o[j]);
             }
             if (u + 1 < steps) store(u + 1);
         }
@@ -328,7 +382,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     const int d = j * 32 + (i >> 2) * 8 + half * 4;
                     if (!whole)
                         *(f32x4 *)&part_o[at * DP + d] = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
-                    else if (d < a.D)
+                    else if (FULL || d < a.D)
                         *(uint2 *)(out + d) = l == 0.0f ? make_uint2(0, 0)
                                                         : make_uint2(pack2<T>(o[j][i] * inv, o[j][i + 1] * inv),
                                                                      pack2<T>(o[j][i + 2] * inv, o[j][i + 3] * inv));
@@ -353,8 +407,11 @@ template <class T, class C, int DP>
 void run_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, bool pad, float *o, float2 *ml,
                     KvJoin *joins, hipStream_t st)
 {
-    if (a.cap > 0.0f || a.slopes) kv_prefill_kernel<T, C, DP, true><<<c.groups, 256, 0, st>>>(a, c, t, pad, o, ml, joins);
-    else kv_prefill_kernel<T, C, DP, false><<<c.groups, 256, 0, st>>>(a, c, t, pad, o, ml, joins);
+    auto run = [&](auto kernel) { kernel<<<c.groups, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
+    // (a head dimension between the padded ones takes the kernel of all score changes as well)
+    if (a.D != DP) run(kv_prefill_kernel<T, C, DP, true, false>);
+    else if (a.cap > 0.0f || a.slopes || a.scale == 0.0f) run(kv_prefill_kernel<T, C, DP, true, true>);
+    else run(kv_prefill_kernel<T, C, DP, false, true>);
 }
 
 template <class T>
