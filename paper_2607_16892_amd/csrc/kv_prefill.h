@@ -57,6 +57,9 @@ template <int DP> __device__ __forceinline__ int value_turn(int r)
     return DP == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2;
 }
 
+// (the constant address space: read through the scalar cache, so that a wait for a block's
+// number is no wait for the tile that is on its way)
+typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
 typedef const __attribute__((address_space(1))) void *GlobalPtr;
 typedef __attribute__((address_space(3))) void *LdsPtr;
 
@@ -79,6 +82,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     constexpr int RP = 64 / NC;          // rows of a load
     constexpr int Tile = KT * Row;
     __shared__ __align__(16) char stage[2][2][Tile];  // two tiles of keys and of values
+    __shared__ int odd[4];                            // a wave found infinities or NaN
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -149,7 +153,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
         // Staging: piece x = lane of load i of group j goes to place 1024 i + 16 lane of the
         // group's rows, so the lane picks the piece of its row that belongs there.
-        const int32_t *table = a.table + (int64_t)r * a.table_stride;
+        const ScalarInts table = (ScalarInts)(a.table + (int64_t)r * a.table_stride);
         const int in_block = (1 << a.shift) - 1;
         int ids[UP];
         auto load_ids = [&](int u) {
@@ -236,12 +240,32 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         }
         for (int u = 0; u < steps; ++u) {
             const int b = u & 1, key0 = k0 + u * KT;
-            const char *sk = stage[b][0], *sv = stage[b][1];
+            char *sk = stage[b][0], *sv = stage[b][1];
             __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile u has landed
             __syncthreads();                     // everybody's has, and tile u - 1 is read
             if (u + 1 < steps) {
                 load(u + 1);
                 load_ids(u + 2);
+            }
+            // A weight of zero does not silence an infinity or a NaN.  Where some row of the
+            // workgroup does not see some key of the tile, such values become zero in LDS and are
+            // added apart, to the rows that see them.
+            const bool mixed = key0 < bot.lo || key0 + KT > top.hi;
+            if (mixed) {
+                uint32_t bad = 0;
+                for (int i = threadIdx.x; i < Tile / 16; i += 256) {
+                    u32x4 &y = ((u32x4 *)sv)[i];
+                    u32x4 mask;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        mask[c] = nonfinite_mask<T>(y[c]);
+                        bad |= mask[c];
+                    }
+                    if (mask[0] | mask[1] | mask[2] | mask[3]) y &= ~mask;
+                }
+                bad = __any(bad);
+                if (lane == 0) odd[wave] = bad;
+                __syncthreads();
             }
             const bool none = idle || key0 >= wbot.hi || key0 + KT <= wtop.lo;
             if (!none) {
@@ -299,39 +323,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                         l += s[t][i] + s[t][i + 1];
                         w[2 * t + (i >> 3)][(i >> 1) & 3] = pack2<T>(s[t][i], s[t][i + 1]);
                     }
-                if (!edge) {
-#pragma unroll
-                    for (int x = 0; x < NT * 2; ++x)
-#pragma unroll
-                        for (int j = 0; j < ND; ++j) o[j] = mfma32<T>(value_frag(sv, x, j), w[x], o[j]);
-                } else {
-                    // a weight of zero does not silence an infinity or a NaN: values that no row
-                    // of the wave sees become zero, and those that some see are added apart, to
-                    // these rows alone
-                    const int wfrom = wtop.lo - lane0, wupto = min(wbot.hi, k1) - lane0;
-                    uint32_t bad = 0;
-#pragma unroll
-                    for (int x = 0; x < NT * 2; ++x) {
-                        u32x4 keep;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int k = x * 16 + (c >> 1) * 8 + (c & 1) * 2;
-                            keep[c] = (k >= wfrom && k < wupto ? 0xffffu : 0u) |
-                                      (k + 1 >= wfrom && k + 1 < wupto ? 0xffff0000u : 0u);
-                        }
-#pragma unroll
-                        for (int j = 0; j < ND; ++j) {
-                            u32x4 y = value_frag(sv, x, j) & keep;
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const uint32_t mask = nonfinite_mask<T>(y[c]);
-                                bad |= mask;
-                                y[c] &= ~mask;
-                            }
-                            o[j] = mfma32<T>(y, w[x], o[j]);
-                        }
-                    }
-                    if (__any(bad)) {
+                if (mixed && (odd[0] | odd[1] | odd[2] | odd[3])) {
                     for (int x = 0; x < NT * 16; ++x) {
                         float mine = 0.0f;
 #pragma unroll
@@ -362,8 +354,11 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                                 }
                         }
                     }
-                    }
                 }
+#pragma unroll
+                for (int x = 0; x < NT * 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < ND; ++j) o[j] = mfma32<T>(value_frag(sv, x, j), w[x], o[j]);
             }
             if (u + 1 < steps) store(u + 1);
         }
