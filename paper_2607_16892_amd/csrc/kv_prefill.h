@@ -14,6 +14,8 @@
 // LDS directly, the next tile while one is worked on.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_math.h"
 #include "kv_sched.h"
 
@@ -42,6 +44,17 @@ __device__ __forceinline__ float max_halves(float x)
     auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
     return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
+// The larger, a NaN aside.  (fmaxf first quiets operands that a matrix product made, an
+// operation each; the median with infinity does not.)
+__device__ __forceinline__ float max_raw(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
+__device__ __forceinline__ float max_of(const f32x16 &x)
+{
+    float m[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int i = 4; i < 16; ++i) m[i & 3] = max_raw(m[i & 3], x[i]);
+    return max_raw(max_raw(m[0], m[1]), max_raw(m[2], m[3]));
+}
+
 __device__ __forceinline__ float sum_halves(float x)
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
@@ -81,8 +94,10 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     constexpr int IP = DP / 32;          // its loads for one: 64 pieces each
     constexpr int RP = 64 / NC;          // rows of a load
     constexpr int Tile = KT * Row;
-    __shared__ __align__(16) char stage[2][2][Tile];  // two tiles of keys and of values
-    __shared__ int odd[4];                            // a wave found infinities or NaN
+    // two tiles of keys and of values, by name: the compiler then knows that reading one waits
+    // for no load into another
+    __shared__ __align__(16) char k_even[Tile], k_odd[Tile], v_even[Tile], v_odd[Tile];
+    __shared__ int found[4];                            // a wave found infinities or NaN
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -93,7 +108,13 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     if (pad) zero_rows<T>(a);
     if (threadIdx.x == 0) joins[group].parts = 0;
     if (!FULL) {  // pieces beyond the rows' ends are never written
-        for (int i = threadIdx.x; i < 4 * Tile / 16; i += 256) ((u32x4 *)stage)[i] = u32x4{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < Tile / 16; i += 256) {
+            const u32x4 zero = {0, 0, 0, 0};
+            ((u32x4 *)k_even)[i] = zero;
+            ((u32x4 *)k_odd)[i] = zero;
+            ((u32x4 *)v_even)[i] = zero;
+            ((u32x4 *)v_odd)[i] = zero;
+        }
         __syncthreads();
     }
     const uint64_t all1 = tiles.sums[tiles.count[0]], all = all1 * a.H;
@@ -162,7 +183,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 ids[j] = table[min(k0 + u * KT + (wave + 4 * j) % NG * 16, k1 - 1) >> a.shift];
         };
         Words<2> reg[F8 ? UP * IP : 1];
-        auto load = [&](int u) {
+        auto load = [&](auto odd_tile, int u) {
 #pragma unroll
             for (int j = 0; j < UP; ++j) {
                 const bool vals = (wave + 4 * j) / NG;
@@ -180,15 +201,19 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     if (FULL || c * 8 < a.D) {
                         if constexpr (F8)
                             reg[j * IP + i] = load_words<2>(p, off);
+                        else if (vals)
+                            __builtin_amdgcn_global_load_lds(
+                                (GlobalPtr)(p + off),
+                                (LdsPtr)((decltype(odd_tile)::value ? v_odd : v_even) + group * 16 * Row + i * 1024), 16, 0, 0);
                         else
-                            __builtin_amdgcn_global_load_lds((GlobalPtr)(p + off),
-                                                             (LdsPtr)&stage[u & 1][vals][group * 16 * Row + i * 1024],
-                                                             16, 0, 0);
+                            __builtin_amdgcn_global_load_lds(
+                                (GlobalPtr)(p + off),
+                                (LdsPtr)((decltype(odd_tile)::value ? k_odd : k_even) + group * 16 * Row + i * 1024), 16, 0, 0);
                     }
                 }
             }
         };
-        auto store = [&](int u) {  // fp8: widened on the way
+        auto store = [&](auto odd_tile) {  // fp8: widened on the way
             if constexpr (F8) {
 #pragma unroll
                 for (int j = 0; j < UP; ++j) {
@@ -200,7 +225,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                         const int rr = i * RP + lane / NC;
                         const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
                         if (FULL || c * 8 < a.D)
-                            *(u32x4 *)&stage[u & 1][vals][group * 16 * Row + i * 1024 + lane * 16] =
+                            *(u32x4 *)((vals ? (decltype(odd_tile)::value ? v_odd : v_even)
+                                              : (decltype(odd_tile)::value ? k_odd : k_even)) +
+                                        group * 16 * Row + i * 1024 + lane * 16) =
                                 u32x4{unpack_fp8<T, false>(x.w[0]), unpack_fp8<T, true>(x.w[0]),
                                       unpack_fp8<T, false>(x.w[1]), unpack_fp8<T, true>(x.w[1])};
                     }
@@ -231,20 +258,23 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
 
+        constexpr std::integral_constant<bool, false> even{};
+        constexpr std::integral_constant<bool, true> odd{};
         __syncthreads();  // the last item's tiles are read
         if (steps) {
             load_ids(0);
-            load(0);
+            load(even, 0);
             load_ids(1);
-            store(0);
+            store(even);
         }
-        for (int u = 0; u < steps; ++u) {
-            const int b = u & 1, key0 = k0 + u * KT;
-            char *sk = stage[b][0], *sv = stage[b][1];
+        auto step = [&](auto odd_tile, int u) {
+            constexpr std::integral_constant<bool, !decltype(odd_tile)::value> next{};
+            const int key0 = k0 + u * KT;
+            char *sk = decltype(odd_tile)::value ? k_odd : k_even, *sv = decltype(odd_tile)::value ? v_odd : v_even;
             __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile u has landed
             __syncthreads();                     // everybody's has, and tile u - 1 is read
             if (u + 1 < steps) {
-                load(u + 1);
+                load(next, u + 1);
                 load_ids(u + 2);
             }
             // A weight of zero does not silence an infinity or a NaN.  Where some row of the
@@ -264,7 +294,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     if (mask[0] | mask[1] | mask[2] | mask[3]) y &= ~mask;
                 }
                 bad = __any(bad);
-                if (lane == 0) odd[wave] = bad;
+                if (lane == 0) found[wave] = bad;
                 __syncthreads();
             }
             const bool none = idle || key0 >= wbot.hi || key0 + KT <= wtop.lo;
@@ -282,23 +312,31 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const bool edge = key0 < wbot.lo || key0 + KT > min(wtop.hi, k1);
                 const int lane0 = key0 + half * 4, from = see.lo - lane0, dist = lane0 - p_row;
                 const uint32_t seen = (uint32_t)max(see.hi - see.lo, 0);
-                float mt = -INFINITY;
+                if constexpr (MODS) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int c = t * 32 + (i >> 2) * 8 + (i & 3);  // the key less `lane0`
-                        if constexpr (MODS) {
+                        for (int i = 0; i < 16; ++i) {
+                            const int c = t * 32 + (i >> 2) * 8 + (i & 3);  // the key less `lane0`
                             float x = s[t][i] * to_exp;
                             if (a.cap > 0.0f) x = a.cap * tanh_fast(x * inv_cap);
                             s[t][i] = (x + slope * (float)(c + dist)) * kLog2e;
                         }
-                        if (edge) s[t][i] = (uint32_t)(c - from) < seen ? s[t][i] : -INFINITY;
-                    }
+                }
+                if (edge) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[t][i]);
+                        for (int i = 0; i < 16; ++i) {
+                            const int c = t * 32 + (i >> 2) * 8 + (i & 3);
+                            float x = (uint32_t)(c - from) < seen ? s[t][i] : -INFINITY;
+                            asm volatile("" : "+v"(x));  // keeps the branch: most tiles have no edge
+                            s[t][i] = x;
+                        }
+                }
+                float mt = max_of(s[0]);
+#pragma unroll
+                for (int t = 1; t < NT; ++t) mt = max_raw(mt, max_of(s[t]));
                 const float by = MODS ? 1.0f : to_exp;
                 mt *= by;
                 mt = max_halves(mt);
@@ -323,7 +361,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                         l += s[t][i] + s[t][i + 1];
                         w[2 * t + (i >> 3)][(i >> 1) & 3] = pack2<T>(s[t][i], s[t][i + 1]);
                     }
-                if (mixed && (odd[0] | odd[1] | odd[2] | odd[3])) {
+                if (mixed && (found[0] | found[1] | found[2] | found[3])) {
                     for (int x = 0; x < NT * 16; ++x) {
                         float mine = 0.0f;
 #pragma unroll
@@ -360,7 +398,11 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
                     for (int j = 0; j < ND; ++j) o[j] = mfma32<T>(value_frag(sv, x, j), w[x], o[j]);
             }
-            if (u + 1 < steps) store(u + 1);
+            if (u + 1 < steps) store(next);
+        };
+        for (int u = 0; u < steps; u += 2) {
+            step(even, u);
+            if (u + 1 < steps) step(odd, u + 1);
         }
 
         l = sum_halves(l);
