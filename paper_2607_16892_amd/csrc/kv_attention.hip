@@ -45,11 +45,11 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs 
     if (threadIdx.x == 0) sums[a.R] = total;
 }
 
-// The tiles of the requests of many rows, in order, and the sums of their steps: first the
+// The tiles of the requests of many rows and the sums of their steps or chunks: first the
 // tiles before each request, then the list, 1024 tiles at a time.
 __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs a, const KvCut cut, int keys, int most,
-                                                                uint64_t *before, uint64_t *sums, int2 *tiles,
-                                                                int *count)
+                                                                bool chunked, uint64_t *before, uint64_t *sums,
+                                                                KvTile *tiles, int *count)
 {
     __shared__ uint64_t part[kPlanThreads / 64];
     const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
@@ -75,25 +75,42 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
                 else hi = m;
             }
             const KvShare s = kv_share(a, cut, lo);
-            const int tile = e - (int)before[lo];
+            const int tile = max(s.tiles - 1 - (e - (int)before[lo]), 0);
             steps = kv_tile_steps(a, s, lo, tile, cut.rows, keys);
-            tiles[e] = make_int2(lo, tile);
+            tiles[e] = KvTile{lo, tile, (int)steps, 0};
         }
         const uint64_t upto = plan_scan(steps, part, total);
-        if (e < n) sums[e] = steps_before + upto - steps;
+        if (!chunked && e < n) sums[e] = steps_before + upto - steps;
         steps_before += total;
     }
+    uint64_t all = steps_before, parts = 0;
+    if (chunked) {
+        const uint64_t most_steps = kv_tile_run(cut, steps_before * a.H);
+        all = 0;
+        for (int e0 = 0; e0 < n; e0 += kPlanThreads) {
+            const int e = e0 + threadIdx.x;
+            const uint64_t chunks = e < n ? (tiles[e].steps + most_steps - 1) / most_steps : 0;  // (this thread's entry)
+            const uint64_t own = chunks > 1 ? chunks | chunks << 32 : chunks;
+            const uint64_t upto = plan_scan(own, part, total) - own;
+            if (e < n) {
+                sums[e] = all + (uint32_t)upto;
+                tiles[e].part = (int)(parts + (upto >> 32));
+            }
+            all += (uint32_t)total;
+            parts += total >> 32;
+        }
+    }
     if (threadIdx.x == 0) {
-        sums[n] = steps_before;
+        sums[n] = all;
         count[0] = n;
+        count[1] = (int)parts;
     }
 }
 
 // ---- join -------------------------------------------------------------------------
 //
-// Workgroup (b, y): for each run of PER from b PER on that an item begins in and does not
-// end in, rows of the item from the partial results of the runs that it reaches over.  The
-// runs left what there is to do.  Up
+// Workgroup (b, y): for each of the PER entries from b PER on that has parts, rows of the item
+// from its partial results.  The kernel before left the entries.  Up
 // to kFewParts parts a wave joins a row; more (a long request alone) the waves share, a
 // workgroup to a row.  Bound by latency (the parts come from other dies' caches), so a wave
 // asks for kAhead parts at once.
@@ -139,7 +156,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int n = min(c + i * by, it.parts - 1);
-                const int64_t at = kv_part(run + n, n == 0) * tile_rows + y;
+                const int64_t at = (int64_t)(n == 0 ? it.first : it.next + (n - 1) * it.stride) * tile_rows + y;
                 x[i] = part_ml[at];
                 z[i] = *(const Vec<float, V> *)(part_o + at * DP + lane * V);
             }
@@ -197,6 +214,8 @@ constexpr int kFewRows = 32;
 struct KvPlans {
     KvCut few, many;       // groups == 0: not launched
     int most_tiles;        // of the requests of many rows
+    bool chunked;          // a workgroup to a tile
+    unsigned grid;
 };
 
 static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
@@ -214,6 +233,11 @@ static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
         p.many.few = few;
         p.many.below = false;
         p.most_tiles = (int)((int64_t)a.T * a.G / p.many.rows + std::min(a.R, a.T / (few + 1) + 1));
+        const int64_t items = (int64_t)p.most_tiles * a.H;
+        // four tiles a workgroup of one round level the differences; more launches than 2^23
+        // workgroups are not needed either way
+        p.chunked = items >= 4 * p.many.groups && items < (1 << 23);
+        p.grid = (unsigned)(p.chunked ? items + p.many.groups + kDies : p.many.groups);
     }
     return p;
 }
@@ -224,7 +248,7 @@ struct KvWork {
     KvJoin *joins;
     uint64_t *sums;    // few rows: [R + 1]
     uint64_t *before, *tile_sums;
-    int2 *tiles;
+    KvTile *tiles;
     int *count;
     size_t bytes;
 };
@@ -242,13 +266,13 @@ static KvWork work_of(const KvAttnArgs &a, const KvPlans &p, void *ws)
     const size_t rows = (size_t)2 * std::max((size_t)p.few.groups * p.few.rows, (size_t)p.many.groups * p.many.rows);
     w.o = (float *)take(rows * padded_dim(a.D) * 4);
     w.ml = (float2 *)take(rows * 8);
-    w.joins = (KvJoin *)take(std::max(p.few.groups, p.many.groups) * sizeof(KvJoin));
+    w.joins = (KvJoin *)take(std::max(p.few.groups, 2 * p.many.groups) * sizeof(KvJoin));
     w.sums = (uint64_t *)take(((size_t)a.R + 1) * 8);
     if (p.many.groups) {
         w.before = (uint64_t *)take((size_t)a.R * 8);
         w.tile_sums = (uint64_t *)take(((size_t)p.most_tiles + 1) * 8);
-        w.tiles = (int2 *)take((size_t)p.most_tiles * 8);
-        w.count = (int *)take(4);
+        w.tiles = (KvTile *)take((size_t)p.most_tiles * sizeof(KvTile));
+        w.count = (int *)take(8);
     }
     w.bytes = at - (char *)ws;
     return w;
@@ -259,15 +283,16 @@ size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype)
     return work_of(a, plans(a, cache_dtype), nullptr).bytes;
 }
 
-template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, const KvWork &w, int DP, hipStream_t st)
+template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, int entries, const KvWork &w, int DP,
+                        hipStream_t st)
 {
     // few items may have many parts and are few among the runs: sixteen waves to a row, 32
     // runs a workgroup; else a wave to a row, and a run
     const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
     const bool few = c.rows == 16 && a.R * (int64_t)a.H <= 64;
-    const dim3 grid(few ? (c.groups + 31) / 32 : c.groups, few ? most : std::min((most + 3) / 4, 16u));
+    const dim3 grid(few ? (entries + 31) / 32 : entries, few ? most : std::min((most + 3) / 4, 16u));
     auto join = [&](auto kernel) {
-        kernel<<<grid, few ? 1024 : 256, 0, st>>>(a, c.rows, c.groups, w.o, w.ml, w.joins);
+        kernel<<<grid, few ? 1024 : 256, 0, st>>>(a, c.rows, entries, w.o, w.ml, w.joins);
     };
     auto pick = [&](auto waves, auto per) {
         constexpr int W = decltype(waves)::value, P = decltype(per)::value;
@@ -283,15 +308,15 @@ static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w
 {
     const int DP = padded_dim(a.D);
     if (p.many.groups) {
-        kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles, w.before,
-                                                    w.tile_sums, w.tiles, w.count);
-        const KvTiles t{w.tile_sums, w.tiles, w.count};
-        launch_kv_prefill<T>(a, p.many, t, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
-        launch_join<T>(a, p.many, w, DP, st);
+        kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles, p.chunked,
+                                                    w.before, w.tile_sums, w.tiles, w.count);
+        const KvTiles t{w.tile_sums, w.tiles, w.count, p.chunked};
+        launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
+        launch_join<T>(a, p.many, p.chunked ? 2 * p.many.groups : p.many.groups, w, DP, st);
     }
     if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);
     launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, !p.many.groups, w.o, w.ml, w.joins, st);
-    launch_join<T>(a, p.few, w, DP, st);
+    launch_join<T>(a, p.few, p.few.groups, w, DP, st);
 }
 
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st)

@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
         const bool whole = go >= it.steps;
         if (n16 < rows) {
             const int64_t t = it.first_token + token;
-            const int64_t at = kv_part(blockIdx.x, it.step == 0) * kDecodeRows + n16;
+            const int64_t at = (int64_t)kv_part(blockIdx.x, it.step == 0) * kDecodeRows + n16;
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
 #pragma unroll
@@ -339,6 +339,9 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
             j.row0 = row0;
             j.rows = rows;
             j.head = h;
+            j.first = kv_part(blockIdx.x, true);
+            j.next = kv_part(blockIdx.x + 1, false);
+            j.stride = 2;
         }
     }
 }

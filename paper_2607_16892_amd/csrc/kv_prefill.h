@@ -23,6 +23,9 @@ namespace dro {
 
 constexpr int kPrefillRows = 128;
 
+// masks of the scheduler's groups
+constexpr int kMfma = 0x8, kDsRead = 0x100;
+
 constexpr int prefill_keys(int DP) { return 8192 / DP; }  // 16 KB of keys, as much of values
 constexpr int prefill_groups(int DP) { return DP == 256 ? 1 : 2; }  // workgroups a compute unit
 
@@ -101,12 +104,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
-    // runs next to one another on one die: the tiles of a head share its keys in the L2
-    const uint32_t per_die = gridDim.x / kDies;
-    const uint32_t group = (blockIdx.x % kDies) * per_die + blockIdx.x / kDies;
-
     if (pad) zero_rows<T>(a);
-    if (threadIdx.x == 0) joins[group].parts = 0;
     if (!FULL) {  // pieces beyond the rows' ends are never written
         for (int i = threadIdx.x; i < Tile / 16; i += 256) {
             const u32x4 zero = {0, 0, 0, 0};
@@ -117,21 +115,58 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         }
         __syncthreads();
     }
-    const uint64_t all1 = tiles.sums[tiles.count[0]], all = all1 * a.H;
-    const uint64_t run = kv_tile_run(cut, all);
-    uint64_t unit = group * run;
-    const uint64_t end = min(unit + run, all);
+    // Workgroups b, b + 8, .. run on one die: it gets consecutive runs or tiles, since the
+    // tiles of a head share its keys in the L2.
+    const uint64_t all1 = tiles.sums[tiles.count[0]], all = all1 * a.H;  // of a head, and in all
+    const uint32_t die = blockIdx.x % kDies, nth = blockIdx.x / kDies;
+    uint32_t group = 0;
+    uint64_t run = 1, unit, end;
+    if (tiles.chunked) {
+        const uint64_t each = (all + kDies - 1) / kDies;
+        unit = die * each + nth;
+        end = nth < each && unit < all ? unit + 1 : unit;
+        if (blockIdx.x == 0)  // places of no tile
+            for (int i = tiles.count[1] * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
+    } else {
+        run = kv_tile_run(cut, all);
+        group = die * (gridDim.x / kDies) + nth;
+        unit = group * run;
+        end = min(unit + run, all);
+        if (threadIdx.x == 0) joins[group].parts = 0;
+    }
     while (unit < end) {
         const int h = (int)(unit / all1);
         const uint64_t u1 = unit - h * all1;
         const int entry = __builtin_amdgcn_readfirstlane(kv_find(tiles.sums, tiles.count[0], u1));
-        const int2 rt = tiles.tiles[entry];
-        const int r = rt.x, tile = rt.y;
+        const KvTile rt = tiles.tiles[entry];
+        const int r = rt.r, tile = rt.tile;
         const KvShare sh = kv_share(a, cut, r);
-        const int item_steps = (int)(tiles.sums[entry + 1] - tiles.sums[entry]);
-        const int step0 = (int)(u1 - tiles.sums[entry]);
-        const int go = (int)min(end - unit, (uint64_t)(item_steps - step0));
-        unit += go;
+        const int item_steps = rt.steps;
+        int step0 = (int)(u1 - tiles.sums[entry]), go, place;
+        if (tiles.chunked) {
+            const int chunks = (int)(tiles.sums[entry + 1] - tiles.sums[entry]);
+            const int each = (item_steps + chunks - 1) / chunks;
+            place = rt.part + tiles.count[1] * h + step0;
+            step0 *= each;
+            go = chunks == 1 ? item_steps : min(each, max(item_steps - step0, 0));
+            unit += 1;
+            if (chunks > 1 && threadIdx.x == 0) {
+                joins[place].parts = step0 == 0 ? chunks : 0;
+                joins[place].first = place;
+                joins[place].next = place + 1;
+                joins[place].stride = 1;
+            }
+        } else {
+            go = (int)min(end - unit, (uint64_t)(item_steps - step0));
+            unit += go;
+            place = kv_part(group, step0 == 0);
+            if (step0 == 0 && go < item_steps && threadIdx.x == 0) {
+                joins[group].parts = 1 + (int)((item_steps - go + run - 1) / run);
+                joins[group].first = place;
+                joins[group].next = kv_part(group + 1, false);
+                joins[group].stride = 2;
+            }
+        }
         const int first_token = min(max(a.start[r], 0), a.T);
         const int row0 = tile * kPrefillRows;
         const int rows = min(sh.n * a.G - row0, kPrefillRows);
@@ -299,16 +334,41 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
             const bool none = idle || key0 >= wbot.hi || key0 + KT <= wtop.lo;
             if (!none) {
+                // pieces of the keys are read a score tile ahead of their use, those of the
+                // values four products ahead (the first ones before the softmax)
+                auto key_frag = [&](int t, int x) {
+                    return *(const u32x4 *)&sk[(t * 32 + n32) * Row + ((2 * x + half) ^ key_turn<DP>(n32)) * 16];
+                };
+                __builtin_amdgcn_s_setprio(1);
                 f32x16 s[NT];
+                u32x4 kf[S];
+#pragma unroll
+                for (int x = 0; x < S; ++x) kf[x] = key_frag(0, x);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
-                    for (int x = 0; x < S; ++x)
-                        s[t] = mfma32<T>(*(const u32x4 *)&sk[(t * 32 + n32) * Row +
-                                                             ((2 * x + half) ^ key_turn<DP>(n32)) * 16], q[x], s[t]);
+                    for (int x = 0; x < S; ++x) {
+                        s[t] = mfma32<T>(kf[x], q[x], s[t]);
+                        if (t + 1 < NT) kf[x] = key_frag(t + 1, x);
+                    }
                 }
+                u32x4 vf[ND];
+#pragma unroll
+                for (int j = 0; j < ND; ++j) vf[j] = value_frag(sv, 0, j);
+                __builtin_amdgcn_sched_group_barrier(kDsRead, S, 0);
+#pragma unroll
+                for (int x = 0; x < S * (NT - 1); ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+                }
+#pragma unroll
+                for (int x = 0; x < S; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kDsRead, (2 * ND + S - 1) / S, 0);
+                }
+                __builtin_amdgcn_s_setprio(0);
                 const bool edge = key0 < wbot.lo || key0 + KT > min(wtop.hi, k1);
                 const int lane0 = key0 + half * 4, from = see.lo - lane0, dist = lane0 - p_row;
                 const uint32_t seen = (uint32_t)max(see.hi - see.lo, 0);
@@ -393,10 +453,21 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                         }
                     }
                 }
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int x = 0; x < NT * 2; ++x)
 #pragma unroll
-                    for (int j = 0; j < ND; ++j) o[j] = mfma32<T>(value_frag(sv, x, j), w[x], o[j]);
+                    for (int j = 0; j < ND; ++j) {
+                        o[j] = mfma32<T>(vf[j], w[x], o[j]);
+                        if (x + 1 < NT * 2) vf[j] = value_frag(sv, x + 1, j);
+                    }
+#pragma unroll
+                for (int x = 0; x < (NT * 2 - 1) * ND; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(kMfma, ND, 0);
+                __builtin_amdgcn_s_setprio(0);
             }
             if (u + 1 < steps) store(next);
         };
@@ -409,7 +480,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         const bool whole = go >= item_steps;
         if (wave * 32 + n32 < rows) {
             const int64_t t = first_token + token;
-            const int64_t at = kv_part(group, step0 == 0) * kPrefillRows + wave * 32 + n32;
+            const int64_t at = (int64_t)place * kPrefillRows + wave * 32 + n32;
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
 #pragma unroll
@@ -430,8 +501,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         }
         if (!whole && step0 == 0 && threadIdx.x == 0) {
-            KvJoin &j = joins[group];
-            j.parts = 1 + (int)((item_steps - go + run - 1) / run);
+            KvJoin &j = joins[tiles.chunked ? place : group];
             j.first_token = first_token;
             j.row0 = row0;
             j.rows = rows;
@@ -441,10 +511,10 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 }
 
 template <class T, class C, int DP>
-void run_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, bool pad, float *o, float2 *ml,
+void run_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, bool pad, float *o, float2 *ml,
                     KvJoin *joins, hipStream_t st)
 {
-    auto run = [&](auto kernel) { kernel<<<c.groups, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
+    auto run = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
     // (a head dimension between the padded ones takes the kernel of all score changes as well)
     if (a.D != DP) run(kv_prefill_kernel<T, C, DP, true, false>);
     else if (a.cap > 0.0f || a.slopes || a.scale == 0.0f) run(kv_prefill_kernel<T, C, DP, true, true>);
@@ -452,13 +522,13 @@ void run_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, bool 
 }
 
 template <class T>
-void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, int cache_dtype, int DP, bool pad,
+void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
                        float *o, float2 *ml, KvJoin *joins, hipStream_t st)
 {
     const bool f8 = cache_dtype == DRO_FP8_E4M3;
-    if (DP == 64) (f8 ? run_kv_prefill<T, fp8, 64> : run_kv_prefill<T, T, 64>)(a, c, t, pad, o, ml, joins, st);
-    else if (DP == 128) (f8 ? run_kv_prefill<T, fp8, 128> : run_kv_prefill<T, T, 128>)(a, c, t, pad, o, ml, joins, st);
-    else (f8 ? run_kv_prefill<T, fp8, 256> : run_kv_prefill<T, T, 256>)(a, c, t, pad, o, ml, joins, st);
+    if (DP == 64) (f8 ? run_kv_prefill<T, fp8, 64> : run_kv_prefill<T, T, 64>)(a, c, t, grid, pad, o, ml, joins, st);
+    else if (DP == 128) (f8 ? run_kv_prefill<T, fp8, 128> : run_kv_prefill<T, T, 128>)(a, c, t, grid, pad, o, ml, joins, st);
+    else (f8 ? run_kv_prefill<T, fp8, 256> : run_kv_prefill<T, T, 256>)(a, c, t, grid, pad, o, ml, joins, st);
 }
 
 }  // namespace dro

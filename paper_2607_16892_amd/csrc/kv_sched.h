@@ -28,9 +28,13 @@ struct KvItem {
     int step, steps;  // the item's step asked for, and how many it has
 };
 
-// Many rows a request: the tiles of all requests in order are listed first (their steps
-// differ, as a tile's keys end where its last row's do), and the steps of the list, head by
-// head, are dealt in equal runs in the same way.
+// Many rows a request: the tiles of all requests are listed first (their steps differ, as a
+// tile's keys end where its last row's do), a request's last tile, the longest, first.  With
+// few tiles the steps of the list, head by head, are dealt in equal runs in the same way;
+// with many, a workgroup takes a tile and the hardware deals them, longest first, since
+// beginning a tile takes as long as several steps and workgroups do not run at one speed
+// (a prompt of 8192 tokens, 64 heads on 8: equal runs of eight tiles ended after 1143 to
+// 1694 us).  There a tile of more than an equal share of the steps is cut into chunks.
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
@@ -157,15 +161,15 @@ struct KvSched {
     }
 };
 
-// An item that begins in a run and ends in another one, for the join.
+// An item in parts, for the join.
 struct KvJoin {
-    int parts;        // runs that it reaches over (0: the run leaves no such item)
+    int parts;  // 0: nothing to join here
     int first_token, row0, rows, head;
-    int pad[3];
+    int first, next, stride;  // places of part 0, of part 1, and from there on
 };
 
 // Place of a run's partial result: the run that an item begins in, or a later one.
-__device__ __forceinline__ int64_t kv_part(uint32_t group, bool begins) { return 2 * (int64_t)group + begins; }
+__device__ __forceinline__ int kv_part(uint32_t group, bool begins) { return 2 * (int)group + begins; }
 
 // The keys of a tile and of its rows: row `i` (of n G) sees [lo, hi).
 struct KvRange {
@@ -184,10 +188,16 @@ __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, in
 
 constexpr int kDies = 8;  // workgroups go to the dies (an L2 each) in turn
 
+struct KvTile {
+    int r, tile;
+    int steps;
+    int part;  // chunked: place of its first partial result, of head 0
+};
 struct KvTiles {
-    const uint64_t *sums;  // [count + 1] exclusive sums of the tiles' steps
-    const int2 *tiles;     // [count] request and tile
-    const int *count;      // [1]
+    const uint64_t *sums;  // [count + 1] exclusive sums of the tiles' steps, or chunks
+    const KvTile *tiles;   // [count]
+    const int *count;      // [2] tiles, and partial results of a head
+    bool chunked;
 };
 
 // Steps of `keys` keys of a tile.
@@ -216,7 +226,7 @@ void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums,
 int kv_decode_waves(int cache_dtype, int DP);
 
 template <class T>
-void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, int cache_dtype, int DP, bool pad,
+void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
                        float *o, float2 *ml, KvJoin *joins, hipStream_t st);
 // its workgroups a compute unit, and keys a step
 int kv_prefill_groups(int DP);
