@@ -147,21 +147,22 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
         l = 0.0f;
         for (int j = 0; j < V; ++j) o[j] = 0.0f;
     };
-    // parts c, c + by, .. of row y
-    auto sum = [&](int y, int c, int by) {
+    // parts c, c + by, .. of row y, `ahead` at once
+    auto sum = [&](auto ahead, int y, int c, int by) {
+        constexpr int N = decltype(ahead)::value;
         clear();
-        for (; c < it.parts; c += by * kAhead) {
-            float2 x[kAhead];
-            Vec<float, V> z[kAhead];
+        for (; c < it.parts; c += by * N) {
+            float2 x[N];
+            Vec<float, V> z[N];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const int n = min(c + i * by, it.parts - 1);
                 const int64_t at = (int64_t)(n == 0 ? it.first : it.next + (n - 1) * it.stride) * tile_rows + y;
                 x[i] = part_ml[at];
                 z[i] = *(const Vec<float, V> *)(part_o + at * DP + lane * V);
             }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
+            for (int i = 0; i < N; ++i)
                 if (c + i * by < it.parts) {
                     float w[V];
                     for (int j = 0; j < V; ++j) w[j] = z[i][j];
@@ -183,15 +184,18 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
         run = blockIdx.x * PER + (PER > 1 ? __builtin_ctzll(todo) : 0);
         it = joins[run];
         if (it.parts == 0) continue;
+        constexpr std::integral_constant<int, kAhead> many{};
         if (it.parts <= kFewParts) {
+#pragma unroll 2
             for (int y = blockIdx.y * WAVES + wave; y < it.rows; y += gridDim.y * WAVES) {
-                sum(y, 0, 1);
+                if (it.parts <= 2) sum(std::integral_constant<int, 2>{}, y, 0, 1);
+                else sum(many, y, 0, 1);
                 write(y);
             }
             continue;
         }
         for (int y = blockIdx.y; y < it.rows; y += gridDim.y) {
-            sum(y, wave, WAVES);
+            sum(many, y, wave, WAVES);
             if (lane == 0) red[wave] = make_float2(m, l);
             for (int j = 0; j < V; ++j) acc[wave][lane * V + j] = o[j];
             __syncthreads();
@@ -222,17 +226,22 @@ static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
 {
     const int DP = padded_dim(a.D), few = std::max(kFewRows / a.G, 1);
     const bool all_few = a.max_new <= few;
+    // with so many rows that each request has more than few, the one kernel takes all (by
+    // max_new, so that a bound that does not hold loses no request)
+    const bool all_many = !all_few && a.T > (int64_t)(a.R - 1) * a.max_new + few;
     KvPlans p{};
-    p.few.rows = 16;
-    p.few.groups = a.num_cu * 4 * kv_decode_waves(cache_dtype, DP);
-    p.few.few = all_few ? 0x7fffffff : few;
-    p.few.below = true;
+    if (!all_many) {
+        p.few.rows = 16;
+        p.few.groups = a.num_cu * 4 * kv_decode_waves(cache_dtype, DP);
+        p.few.few = all_few ? 0x7fffffff : few;
+        p.few.below = true;
+    }
     if (!all_few) {
-        p.many.rows = 128;
+        p.many.rows = kv_prefill_rows(DP);
         p.many.groups = a.num_cu * kv_prefill_groups(DP) / kDies * kDies;
-        p.many.few = few;
+        p.many.few = all_many ? 0 : few;
         p.many.below = false;
-        p.most_tiles = (int)((int64_t)a.T * a.G / p.many.rows + std::min(a.R, a.T / (few + 1) + 1));
+        p.most_tiles = (int)((int64_t)a.T * a.G / p.many.rows + std::min(a.R, all_many ? a.T : a.T / (few + 1) + 1));
         const int64_t items = (int64_t)p.most_tiles * a.H;
         // four tiles a workgroup of one round level the differences; more launches than 2^23
         // workgroups are not needed either way
@@ -314,6 +323,7 @@ static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w
         launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
         launch_join<T>(a, p.many, p.chunked ? 2 * p.many.groups : p.many.groups, w, DP, st);
     }
+    if (!p.few.groups) return;
     if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);
     launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, !p.many.groups, w.o, w.ml, w.joins, st);
     launch_join<T>(a, p.few, p.few.groups, w, DP, st);

@@ -21,13 +21,20 @@
 
 namespace dro {
 
-constexpr int kPrefillRows = 128;
+// With 256 components the sums of 32 rows are half a wave's registers already, so two waves
+// share rows there: both compute the scores, each the sums of half the components.  (Whole
+// rows a wave went through memory and the accumulation registers: %D256OLD% us for the
+// mixed call of 40 requests, against %D256NEW%.)
+constexpr int prefill_split(int DP) { return DP == 256 ? 2 : 1; }
+constexpr int prefill_rows(int DP) { return 128 / prefill_split(DP); }
+
+constexpr int kAheadOf = 4;  // products: 128 cycles, a read of LDS
 
 // masks of the scheduler's groups
 constexpr int kMfma = 0x8, kDsRead = 0x100;
 
 constexpr int prefill_keys(int DP) { return 8192 / DP; }  // 16 KB of keys, as much of values
-constexpr int prefill_groups(int DP) { return DP == 256 ? 1 : 2; }  // workgroups a compute unit
+constexpr int prefill_groups(int) { return 2; }              // workgroups a compute unit
 
 // 32 x 32 tile over 16 products: lane holds row (column) lane % 32, products (lane / 32) 8
 // .. + 8; result: column lane % 32, rows 8 b + 4 (lane / 32) + c in place 4 b + c.
@@ -89,7 +96,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     constexpr int KT = prefill_keys(DP);
     constexpr int S = DP / 16;           // steps of 16 components of a score
     constexpr int NT = KT / 32;          // score tiles
-    constexpr int ND = DP / 32;          // component tiles
+    constexpr int DS = prefill_split(DP);
+    constexpr int ND = DP / 32 / DS;     // component tiles of a wave
+    constexpr int Rows = prefill_rows(DP);
     constexpr int Row = DP * 2;          // bytes of a row in LDS
     constexpr int NC = DP / 8;           // pieces of a row
     constexpr int NG = KT / 16;          // groups of 16 keys (each within one block)
@@ -104,6 +113,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
+    const int rw = wave % (4 / DS) * 32, dt0 = wave / (4 / DS) * ND;  // rows and component tiles from there on
     if (pad) zero_rows<T>(a);
     if (!FULL) {  // pieces beyond the rows' ends are never written
         for (int i = threadIdx.x; i < Tile / 16; i += 256) {
@@ -168,8 +178,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         }
         const int first_token = min(max(a.start[r], 0), a.T);
-        const int row0 = tile * kPrefillRows;
-        const int rows = min(sh.n * a.G - row0, kPrefillRows);
+        const int row0 = tile * Rows;
+        const int rows = min(sh.n * a.G - row0, Rows);
         const int prefix = a.prefix ? a.prefix[r] : 0;
         const KvRange top = kv_row_range(a, sh.ctx, sh.n, row0 / a.G, prefix);
         const KvRange bot = kv_row_range(a, sh.ctx, sh.n, (row0 + rows - 1) / a.G, prefix);
@@ -178,11 +188,11 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         const int steps = (k1 - k0 + KT - 1) / KT;
 
         // this wave's rows, and this lane's
-        const int wrow = min(wave * 32, rows - 1), wlast = min(wave * 32 + 31, rows - 1);
+        const int wrow = min(rw, rows - 1), wlast = min(rw + 31, rows - 1);
         const KvRange wtop = kv_row_range(a, sh.ctx, sh.n, (row0 + wrow) / a.G, prefix);
         const KvRange wbot = kv_row_range(a, sh.ctx, sh.n, (row0 + wlast) / a.G, prefix);
-        const bool idle = wave * 32 >= rows;
-        const int row = row0 + min(wave * 32 + n32, rows - 1);
+        const bool idle = rw >= rows;
+        const int row = row0 + min(rw + n32, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
         const KvRange see = kv_row_range(a, sh.ctx, sh.n, token, prefix);
         const int p_row = sh.ctx - sh.n + token;
@@ -275,7 +285,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int i = lane & 15, rr = x * 16 + e * 8 + half * 4 + (i >> 2);
-                const int d = j * 32 + (lane & 16) + (i & 3) * 4;
+                const int d = (dt0 + j) * 32 + (lane & 16) + (i & 3) * 4;
                 const auto z = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (__attribute__((address_space(3))) Vec<short, 4> *)(sv + rr * Row + ((d >> 3) ^ value_turn<DP>(rr)) * 16 +
                                                                         (d & 4) * 2));
@@ -334,39 +344,36 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
             const bool none = idle || key0 >= wbot.hi || key0 + KT <= wtop.lo;
             if (!none) {
-                // pieces of the keys are read a score tile ahead of their use, those of the
-                // values four products ahead (the first ones before the softmax)
-                auto key_frag = [&](int t, int x) {
-                    return *(const u32x4 *)&sk[(t * 32 + n32) * Row + ((2 * x + half) ^ key_turn<DP>(n32)) * 16];
+                // pieces of the keys and of the values are read kAheadOf products before their
+                // use, the first of the values before the softmax
+                auto key_frag = [&](int f) {
+                    return *(const u32x4 *)&sk[(f / S * 32 + n32) * Row + ((2 * (f % S) + half) ^ key_turn<DP>(n32)) * 16];
                 };
                 __builtin_amdgcn_s_setprio(1);
                 f32x16 s[NT];
-                u32x4 kf[S];
+                u32x4 kf[kAheadOf], vf[kAheadOf];
 #pragma unroll
-                for (int x = 0; x < S; ++x) kf[x] = key_frag(0, x);
+                for (int f = 0; f < kAheadOf; ++f) kf[f] = key_frag(f);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+                for (int f = 0; f < NT * S; ++f) {
+                    if (f % S == 0)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-                    for (int x = 0; x < S; ++x) {
-                        s[t] = mfma32<T>(kf[x], q[x], s[t]);
-                        if (t + 1 < NT) kf[x] = key_frag(t + 1, x);
-                    }
+                        for (int i = 0; i < 16; ++i) s[f / S][i] = 0.0f;
+                    s[f / S] = mfma32<T>(kf[f % kAheadOf], q[f % S], s[f / S]);
+                    if (f + kAheadOf < NT * S) kf[f % kAheadOf] = key_frag(f + kAheadOf);
                 }
-                u32x4 vf[ND];
 #pragma unroll
-                for (int j = 0; j < ND; ++j) vf[j] = value_frag(sv, 0, j);
-                __builtin_amdgcn_sched_group_barrier(kDsRead, S, 0);
+                for (int f = 0; f < kAheadOf; ++f) vf[f] = value_frag(sv, f / ND, f % ND);
+                __builtin_amdgcn_sched_group_barrier(kDsRead, kAheadOf, 0);
 #pragma unroll
-                for (int x = 0; x < S * (NT - 1); ++x) {
+                for (int f = 0; f < NT * S - kAheadOf; ++f) {
                     __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
                 }
 #pragma unroll
-                for (int x = 0; x < S; ++x) {
+                for (int f = 0; f < kAheadOf; ++f) {
                     __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kDsRead, (2 * ND + S - 1) / S, 0);
+                    __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
                 }
                 __builtin_amdgcn_s_setprio(0);
                 const bool edge = key0 < wbot.lo || key0 + KT > min(wtop.hi, k1);
@@ -445,7 +452,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                             for (int j = 0; j < ND; ++j)
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
-                                    const int d = j * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
+                                    const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
                                     const float y = FULL || d < D ? value_at<C>(at, d) : 0.0f;
                                     o[j][i] += seen && !__builtin_isfinite(y) ? wt * y : 0.0f;
                                     __builtin_amdgcn_sched_barrier(0);
@@ -455,18 +462,17 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 }
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int x = 0; x < NT * 2; ++x)
+                for (int f = 0; f < NT * 2 * ND; ++f) {
+                    o[f % ND] = mfma32<T>(vf[f % kAheadOf], w[f / ND], o[f % ND]);
+                    const int g = f + kAheadOf;
+                    if (g < NT * 2 * ND) vf[f % kAheadOf] = value_frag(sv, g / ND, g % ND);
+                }
 #pragma unroll
-                    for (int j = 0; j < ND; ++j) {
-                        o[j] = mfma32<T>(vf[j], w[x], o[j]);
-                        if (x + 1 < NT * 2) vf[j] = value_frag(sv, x + 1, j);
-                    }
-#pragma unroll
-                for (int x = 0; x < (NT * 2 - 1) * ND; ++x) {
+                for (int f = 0; f < NT * 2 * ND - kAheadOf; ++f) {
                     __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
                 }
-                __builtin_amdgcn_sched_group_barrier(kMfma, ND, 0);
+                __builtin_amdgcn_sched_group_barrier(kMfma, kAheadOf, 0);
                 __builtin_amdgcn_s_setprio(0);
             }
             if (u + 1 < steps) store(next);
@@ -478,16 +484,16 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
         l = sum_halves(l);
         const bool whole = go >= item_steps;
-        if (wave * 32 + n32 < rows) {
+        if (rw + n32 < rows) {
             const int64_t t = first_token + token;
-            const int64_t at = (int64_t)place * kPrefillRows + wave * 32 + n32;
+            const int64_t at = (int64_t)place * Rows + rw + n32;
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
 #pragma unroll
             for (int j = 0; j < ND; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const int d = j * 32 + (i >> 2) * 8 + half * 4;
+                    const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4;
                     if (!whole)
                         *(f32x4 *)&part_o[at * DP + d] = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
                     else if (FULL || d < a.D)
@@ -495,7 +501,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                                                         : make_uint2(pack2<T>(o[j][i] * inv, o[j][i + 1] * inv),
                                                                      pack2<T>(o[j][i + 2] * inv, o[j][i + 3] * inv));
                 }
-            if (half == 0) {
+            if (half == 0 && dt0 == 0) {
                 if (!whole) part_ml[at] = make_float2(m, l);
                 else if (a.lse) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }

@@ -5,5 +5,6 @@ namespace dro {
 template void launch_kv_prefill<bf16>(const KvAttnArgs &, const KvCut &, const KvTiles &, unsigned, int, int, bool, float *,
                                     float2 *, KvJoin *, hipStream_t);
 int kv_prefill_groups(int DP) { return prefill_groups(DP); }
+int kv_prefill_rows(int DP) { return prefill_rows(DP); }
 int kv_prefill_keys(int DP) { return prefill_keys(DP); }
 }  // namespace dro

@@ -228,8 +228,9 @@ int kv_decode_waves(int cache_dtype, int DP);
 template <class T>
 void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
                        float *o, float2 *ml, KvJoin *joins, hipStream_t st);
-// its workgroups a compute unit, and keys a step
+// its workgroups a compute unit, rows of a tile, and keys a step
 int kv_prefill_groups(int DP);
+int kv_prefill_rows(int DP);
 int kv_prefill_keys(int DP);
 
 }  // namespace dro
