@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs 
 // tiles before each request, then the list, 1024 tiles at a time.
 __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs a, const KvCut cut, int keys, int most,
                                                                 bool chunked, uint64_t *before, uint64_t *sums,
-                                                                KvTile *tiles, int *count)
+                                                                KvTile *tiles, KvTileList *list)
 {
     __shared__ uint64_t part[kPlanThreads / 64];
     const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
@@ -77,10 +77,10 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
             const KvShare s = kv_share(a, cut, lo);
             const int tile = max(s.tiles - 1 - (e - (int)before[lo]), 0);
             steps = kv_tile_steps(a, s, lo, tile, cut.rows, keys);
-            tiles[e] = KvTile{lo, tile, (int)steps, 0};
+            tiles[e] = KvTile{lo, tile, s.n, s.ctx, min(max(a.start[lo], 0), a.T), (int)steps, 0, 1, 0};
         }
         const uint64_t upto = plan_scan(steps, part, total);
-        if (!chunked && e < n) sums[e] = steps_before + upto - steps;
+        if (!chunked && e < n) sums[e] = tiles[e].before = steps_before + upto - steps;
         steps_before += total;
     }
     uint64_t all = steps_before, parts = 0;
@@ -93,8 +93,9 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
             const uint64_t own = chunks > 1 ? chunks | chunks << 32 : chunks;
             const uint64_t upto = plan_scan(own, part, total) - own;
             if (e < n) {
-                sums[e] = all + (uint32_t)upto;
+                sums[e] = tiles[e].before = all + (uint32_t)upto;
                 tiles[e].part = (int)(parts + (upto >> 32));
+                tiles[e].chunks = (int)chunks;
             }
             all += (uint32_t)total;
             parts += total >> 32;
@@ -102,8 +103,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
     }
     if (threadIdx.x == 0) {
         sums[n] = all;
-        count[0] = n;
-        count[1] = (int)parts;
+        *list = KvTileList{n, (int)parts, all};
     }
 }
 
@@ -258,7 +258,7 @@ struct KvWork {
     uint64_t *sums;    // few rows: [R + 1]
     uint64_t *before, *tile_sums;
     KvTile *tiles;
-    int *count;
+    KvTileList *list;
     size_t bytes;
 };
 
@@ -281,7 +281,7 @@ static KvWork work_of(const KvAttnArgs &a, const KvPlans &p, void *ws)
         w.before = (uint64_t *)take((size_t)a.R * 8);
         w.tile_sums = (uint64_t *)take(((size_t)p.most_tiles + 1) * 8);
         w.tiles = (KvTile *)take((size_t)p.most_tiles * sizeof(KvTile));
-        w.count = (int *)take(8);
+        w.list = (KvTileList *)take(sizeof(KvTileList));
     }
     w.bytes = at - (char *)ws;
     return w;
@@ -318,8 +318,8 @@ static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w
     const int DP = padded_dim(a.D);
     if (p.many.groups) {
         kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles, p.chunked,
-                                                    w.before, w.tile_sums, w.tiles, w.count);
-        const KvTiles t{w.tile_sums, w.tiles, w.count, p.chunked};
+                                                    w.before, w.tile_sums, w.tiles, w.list);
+        const KvTiles t{w.tile_sums, w.tiles, w.list, p.chunked};
         launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
         launch_join<T>(a, p.many, p.chunked ? 2 * p.many.groups : p.many.groups, w, DP, st);
     }

@@ -79,10 +79,10 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
             }
         }
         const float ks = F8 ? a.scale * a.k_scale[h] : a.scale;
-        const float slope = a.slopes ? a.slopes[hq] : 0.0f;
-        const bool mods = a.cap > 0.0f || a.slopes;
-        const float to_exp = mods ? ks : ks * kLog2e;
-        const float inv_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+        // scores to exponents of two: times to_exp, plus slope a key's distance; with a cap
+        // to_exp leads to the exponent of its tanh
+        const float slope = a.slopes ? a.slopes[hq] * kLog2e : 0.0f;
+        const float cap = a.cap * kLog2e, to_exp = a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
         const int p_row = it.ctx - it.n + token;
 
         const char *kp = (const char *)a.k + (int64_t)h * a.k_head * E;
@@ -197,12 +197,12 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
             float e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) e[i] = s[i >> 2][i & 3] * to_exp;
-            if (mods) {
+            if (a.cap > 0.0f || a.slopes) {
+                const float b0 = slope * (float)(key0 + grp * 4 - p_row);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int key = key0 + (i >> 2) * 16 + grp * 4 + (i & 3);
-                    if (a.cap > 0.0f) e[i] = a.cap * tanh_fast(e[i] * inv_cap);
-                    e[i] = (e[i] + slope * (float)(key - p_row)) * kLog2e;
+                    const float add = __builtin_fmaf((float)((i >> 2) * 16 + (i & 3)), slope, b0);
+                    e[i] = a.cap > 0.0f ? tanh_scaled(e[i], cap, add) : e[i] + add;
                 }
             }
             if (edge) {

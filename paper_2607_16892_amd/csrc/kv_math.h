@@ -55,10 +55,10 @@ __device__ __forceinline__ float sum_groups(float x)
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
-// tanh by the exponential: absolute error below 2^-21
-__device__ __forceinline__ float tanh_fast(float x)
+// cap tanh(y) + add for x = 2 y log2 e, by tanh y = 1 - 2 / (2^x + 1): to 2^-21 of the cap
+__device__ __forceinline__ float tanh_scaled(float x, float cap, float add)
 {
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.0f * kLog2e)) + 1.0f);
+    return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x) + 1.0f), cap + add);
 }
 
 // the bits of the infinities and NaN among the values of a dword of the cache's type C: an

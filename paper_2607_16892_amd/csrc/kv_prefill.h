@@ -127,7 +127,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     }
     // Workgroups b, b + 8, .. run on one die: it gets consecutive runs or tiles, since the
     // tiles of a head share its keys in the L2.
-    const uint64_t all1 = tiles.sums[tiles.count[0]], all = all1 * a.H;  // of a head, and in all
+    const KvTileList list = *tiles.list;
+    const uint64_t all1 = list.all, all = all1 * a.H;  // of a head, and in all
     const uint32_t die = blockIdx.x % kDies, nth = blockIdx.x / kDies;
     uint32_t group = 0;
     uint64_t run = 1, unit, end;
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         unit = die * each + nth;
         end = nth < each && unit < all ? unit + 1 : unit;
         if (blockIdx.x == 0)  // places of no tile
-            for (int i = tiles.count[1] * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
+            for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
     } else {
         run = kv_tile_run(cut, all);
         group = die * (gridDim.x / kDies) + nth;
@@ -144,19 +145,20 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         end = min(unit + run, all);
         if (threadIdx.x == 0) joins[group].parts = 0;
     }
+    int entry = -1;
     while (unit < end) {
         const int h = (int)(unit / all1);
         const uint64_t u1 = unit - h * all1;
-        const int entry = __builtin_amdgcn_readfirstlane(kv_find(tiles.sums, tiles.count[0], u1));
+        // (a run goes on with the next tile, or the first one of the next head)
+        entry = entry < 0 ? __builtin_amdgcn_readfirstlane(kv_find(tiles.sums, list.count, u1)) : u1 ? entry + 1 : 0;
         const KvTile rt = tiles.tiles[entry];
         const int r = rt.r, tile = rt.tile;
-        const KvShare sh = kv_share(a, cut, r);
         const int item_steps = rt.steps;
-        int step0 = (int)(u1 - tiles.sums[entry]), go, place;
+        int step0 = (int)(u1 - rt.before), go, place;
         if (tiles.chunked) {
-            const int chunks = (int)(tiles.sums[entry + 1] - tiles.sums[entry]);
+            const int chunks = rt.chunks;
             const int each = (item_steps + chunks - 1) / chunks;
-            place = rt.part + tiles.count[1] * h + step0;
+            place = rt.part + list.parts * h + step0;
             step0 *= each;
             go = chunks == 1 ? item_steps : min(each, max(item_steps - step0, 0));
             unit += 1;
@@ -177,25 +179,25 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 joins[group].stride = 2;
             }
         }
-        const int first_token = min(max(a.start[r], 0), a.T);
+        const int first_token = rt.first_token;
         const int row0 = tile * Rows;
-        const int rows = min(sh.n * a.G - row0, Rows);
+        const int rows = min(rt.n * a.G - row0, Rows);
         const int prefix = a.prefix ? a.prefix[r] : 0;
-        const KvRange top = kv_row_range(a, sh.ctx, sh.n, row0 / a.G, prefix);
-        const KvRange bot = kv_row_range(a, sh.ctx, sh.n, (row0 + rows - 1) / a.G, prefix);
+        const KvRange top = kv_row_range(a, rt.ctx, rt.n, row0 / a.G, prefix);
+        const KvRange bot = kv_row_range(a, rt.ctx, rt.n, (row0 + rows - 1) / a.G, prefix);
         const int base = top.lo & ~31;
         const int k0 = min(base + step0 * KT, bot.hi), k1 = min(base + (step0 + go) * KT, bot.hi);
         const int steps = (k1 - k0 + KT - 1) / KT;
 
         // this wave's rows, and this lane's
         const int wrow = min(rw, rows - 1), wlast = min(rw + 31, rows - 1);
-        const KvRange wtop = kv_row_range(a, sh.ctx, sh.n, (row0 + wrow) / a.G, prefix);
-        const KvRange wbot = kv_row_range(a, sh.ctx, sh.n, (row0 + wlast) / a.G, prefix);
+        const KvRange wtop = kv_row_range(a, rt.ctx, rt.n, (row0 + wrow) / a.G, prefix);
+        const KvRange wbot = kv_row_range(a, rt.ctx, rt.n, (row0 + wlast) / a.G, prefix);
         const bool idle = rw >= rows;
         const int row = row0 + min(rw + n32, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
-        const KvRange see = kv_row_range(a, sh.ctx, sh.n, token, prefix);
-        const int p_row = sh.ctx - sh.n + token;
+        const KvRange see = kv_row_range(a, rt.ctx, rt.n, token, prefix);
+        const int p_row = rt.ctx - rt.n + token;
 
         u32x4 q[S];
         {
@@ -207,9 +209,11 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         }
         const float ks = F8 ? a.scale * a.k_scale[h] : a.scale;
-        const float slope = MODS && a.slopes ? a.slopes[hq] : 0.0f;
-        const float inv_cap = MODS && a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
-        float to_exp = ks;
+        // scores to exponents of two: times to_exp, plus slope a key's distance; with a cap
+        // to_exp leads to the exponent of its tanh
+        const float slope = MODS && a.slopes ? a.slopes[hq] * kLog2e : 0.0f;
+        const float cap = a.cap * kLog2e;
+        float to_exp = MODS && a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
         if constexpr (!MODS) {  // scale > 0 from here on, so the largest score has the largest weight
             to_exp = fabsf(ks) * kLog2e;
             if (ks < 0.0f)
@@ -380,15 +384,24 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const int lane0 = key0 + half * 4, from = see.lo - lane0, dist = lane0 - p_row;
                 const uint32_t seen = (uint32_t)max(see.hi - see.lo, 0);
                 if constexpr (MODS) {
+                    const float b0 = slope * (float)dist;
+                    if (a.cap > 0.0f) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                        for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int c = t * 32 + (i >> 2) * 8 + (i & 3);  // the key less `lane0`
-                            float x = s[t][i] * to_exp;
-                            if (a.cap > 0.0f) x = a.cap * tanh_fast(x * inv_cap);
-                            s[t][i] = (x + slope * (float)(c + dist)) * kLog2e;
-                        }
+                            for (int i = 0; i < 16; ++i) {
+                                const float c = (float)(t * 32 + (i >> 2) * 8 + (i & 3));  // the key less `lane0`
+                                s[t][i] = tanh_scaled(s[t][i] * to_exp, cap, __builtin_fmaf(c, slope, b0));
+                            }
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float c = (float)(t * 32 + (i >> 2) * 8 + (i & 3));
+                                s[t][i] = __builtin_fmaf(s[t][i], to_exp, __builtin_fmaf(c, slope, b0));
+                            }
+                    }
                 }
                 if (edge) {
 #pragma unroll

@@ -190,13 +190,21 @@ constexpr int kDies = 8;  // workgroups go to the dies (an L2 each) in turn
 
 struct KvTile {
     int r, tile;
+    int n, ctx, first_token;  // of the request
     int steps;
-    int part;  // chunked: place of its first partial result, of head 0
+    int part;    // chunked: place of its first partial result, of head 0
+    int chunks;  // 1 if not chunked
+    uint64_t before;  // steps, or chunks, of the tiles before it
+};
+struct KvTileList {  // (one load)
+    int count;  // tiles
+    int parts;  // partial results of a head
+    uint64_t all;  // steps, or chunks, of a head
 };
 struct KvTiles {
     const uint64_t *sums;  // [count + 1] exclusive sums of the tiles' steps, or chunks
     const KvTile *tiles;   // [count]
-    const int *count;      // [2] tiles, and partial results of a head
+    const KvTileList *list;
     bool chunked;
 };
 
