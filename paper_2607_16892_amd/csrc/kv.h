@@ -21,6 +21,7 @@ struct KvTablesArgs {
     int32_t *pos;
     uint8_t *granted;
     int4 *rows;     // scratch [R]: what each request takes and gives (see kv_cache.hip)
+    uint32_t *backs;  // scratch [R]: blocks given back before each request
     int32_t *tops;  // scratch [2]: blocks free before and after the ended requests' ones
 };
 hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st);

@@ -139,7 +139,7 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *p, const int32_t *len, cons
         return fail(ctx, DRO_EINVAL, "a required output is NULL");
     ENTER_DEVICE(ctx);
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = ensure_ws(ctx, rup((size_t)p->R * sizeof(int4)) + rup(8), st))) return rc;
+    if ((rc = ensure_ws(ctx, rup((size_t)p->R * sizeof(int4)) + rup((size_t)p->R * 4) + rup(8), st))) return rc;
     Arena ar{(char *)ctx->ws, 0};
     KvTablesArgs a{};
     a.R = p->R;
@@ -163,6 +163,7 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *p, const int32_t *len, cons
     a.pos = pos;
     a.granted = granted;
     a.rows = ar.take<int4>(p->R);
+    a.backs = ar.take<uint32_t>(p->R);
     a.tops = ar.take<int32_t>(2);
     HIPCHK(launch_kv_tables(a, st));
     return DRO_OK;

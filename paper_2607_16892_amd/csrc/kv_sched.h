@@ -81,8 +81,9 @@ __device__ __forceinline__ uint64_t kv_run(const KvCut &c, uint64_t all, uint32_
     return (all + c.groups - 1) / (uint32_t)c.groups;
 }
 
-// First index of the ascending x[0 .. n] whose next entry exceeds v (x[n] > v): 64 probes a step.
-__device__ __forceinline__ int kv_find(const uint64_t *x, int n, uint64_t v)
+// First index of the ascending x[0 .. n) whose next entry exceeds v (the n-th counts as
+// larger): 64 probes a step, by the whole wave.
+template <class U> __device__ __forceinline__ int kv_find(const U *x, int n, U v)
 {
     int lo = 0, hi = n;  // x[lo] <= v < x[hi]
     const int lane = threadIdx.x & 63;

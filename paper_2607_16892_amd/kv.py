@@ -185,16 +185,21 @@ def kv_block_tables(ctx: Context, pool: BlockPool, length: torch.Tensor, add: to
     i32 = torch.int32
     len_p, add_p = _need(length, i32, "length", dev, R), _need(add, i32, "add", dev, R)
     res_p = None if reserve is None else _need(reserve, i32, "reserve", dev, R)
-    out = out or {}
     with nullcontext() if stream is None else torch.cuda.stream(stream):
-        o = {}
-        for name, n, dtype in (("held", R, i32), ("free", 1, i32), ("context", R, i32),
-                               ("start", R + 1, i32), ("slot", T, torch.int64), ("pos", T, i32),
-                               ("granted", R, torch.uint8)):
-            t = out.get(name)
-            o[name] = torch.empty(n, dtype=dtype, device=dev) if t is None else _out(t, (n,), dtype, dev, name)
+        if out:
+            o = {name: _out(out.get(name), (n,), dtype, dev, name)
+                 for name, n, dtype in (("held", R, i32), ("free", 1, i32), ("context", R, i32),
+                                        ("start", R + 1, i32), ("pos", T, i32),
+                                        ("slot", T, torch.int64), ("granted", R, torch.uint8))}
+        else:  # one buffer for the 32-bit ones
+            parts = torch.empty(3 * R + 2 + T, dtype=i32, device=dev).split((R, 1, R, R + 1, T))
+            o = dict(zip(("held", "free", "context", "start", "pos"), parts))
+            o["slot"] = torch.empty(T, dtype=torch.int64, device=dev)
+            o["granted"] = torch.empty(R, dtype=torch.uint8, device=dev)
     rc = ctx._lib.kv_block_tables(ctx.handle, ct.byref(ps), len_p, add_p, res_p, T,
-                                  *[t.data_ptr() for t in o.values()], _queue(stream, dev))
+                                  o["held"].data_ptr(), o["free"].data_ptr(), o["context"].data_ptr(),
+                                  o["start"].data_ptr(), o["slot"].data_ptr(), o["pos"].data_ptr(),
+                                  o["granted"].data_ptr(), _queue(stream, dev))
     if rc:
         ctx.check(rc, "kv_block_tables")
     if stream is not None:
