@@ -110,98 +110,117 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
 // ---- join -------------------------------------------------------------------------
 //
 // Workgroup (b, y): for each of the PER entries from b PER on that has parts, rows of the item
-// from its partial results.  The kernel before left the entries.  Up
-// to kFewParts parts a wave joins a row; more (a long request alone) the waves share, a
-// workgroup to a row.  Bound by latency (the parts come from other dies' caches), so a wave
-// asks for kAhead parts at once.
+// from its partial results.  The kernel before left the entries.  Up to kFewParts parts a
+// wave joins as many rows as its lanes reach with 16 bytes each; more (a long request alone)
+// the waves share, a workgroup to a row.  Bound by latency (the parts come from other dies'
+// caches), so a wave asks for several parts at once.
 
 constexpr int kFewParts = 16;
-constexpr int kAhead = 8;
 
-template <class T, int DP, int WAVES, int PER>
-__global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a, int tile_rows, int runs, const float *part_o,
-                                                                  const float2 *part_ml, const KvJoin *joins)
-{
-    constexpr int V = DP / 64;
-    __shared__ float2 red[WAVES];
-    __shared__ float acc[WAVES][DP];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int run = blockIdx.x * PER;
-    uint64_t todo = 1;
-    if constexpr (PER > 1) {
-        static_assert(PER <= 64, "a lane per run");
-        todo = __ballot(lane < PER && run + lane < runs && joins[run + lane].parts != 0);
-    }
-    KvJoin it;
+// The running join of a row's parts, V components a lane.
+template <int V> struct RowSum {
     float m, l, o[V];
-    auto join = [&](float2 x, const float *z) {
+    __device__ __forceinline__ void clear()
+    {
+        m = -INFINITY;
+        l = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = 0.0f;
+    }
+    __device__ __forceinline__ void add(float2 x, const float *z)
+    {
         if (x.y == 0.0f) return;  // no key that the row sees
         const float to = fmaxf(m, x.x), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
         const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - to);
         m = to;
         l = l * by + f * x.y;
-        for (int j = 0; j < V; ++j) o[j] = o[j] * by + f * z[j];
-    };
-    auto clear = [&]() {
-        m = -INFINITY;
-        l = 0.0f;
-        for (int j = 0; j < V; ++j) o[j] = 0.0f;
-    };
-    // parts c, c + by, .. of row y, `ahead` at once
-    auto sum = [&](auto ahead, int y, int c, int by) {
-        constexpr int N = decltype(ahead)::value;
-        clear();
-        for (; c < it.parts; c += by * N) {
-            float2 x[N];
-            Vec<float, V> z[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
+        for (int j = 0; j < V; ++j) o[j] = o[j] * by + f * z[j];
+    }
+    // parts c, c + by, .. of row y, AHEAD at once, components from d on
+    template <int DP, int AHEAD>
+    __device__ __forceinline__ void sum(const KvJoin &it, int tile_rows, const float *part_o, const float2 *part_ml,
+                                        int y, int d, int c, int by)
+    {
+        for (; c < it.parts; c += by * AHEAD) {
+            float2 x[AHEAD];
+            Vec<float, V> z[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
                 const int n = min(c + i * by, it.parts - 1);
                 const int64_t at = (int64_t)(n == 0 ? it.first : it.next + (n - 1) * it.stride) * tile_rows + y;
                 x[i] = part_ml[at];
-                z[i] = *(const Vec<float, V> *)(part_o + at * DP + lane * V);
+                z[i] = *(const Vec<float, V> *)(part_o + at * DP + d);
             }
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+            for (int i = 0; i < AHEAD; ++i)
                 if (c + i * by < it.parts) {
                     float w[V];
+#pragma unroll
                     for (int j = 0; j < V; ++j) w[j] = z[i][j];
-                    join(x[i], w);
+                    add(x[i], w);
                 }
         }
-    };
-    auto write = [&](int y) {
+    }
+    template <class T>
+    __device__ __forceinline__ void write(const KvAttnArgs &a, const KvJoin &it, int y, int d) const
+    {
         const int row = it.row0 + y, token = row / a.G, hq = it.head * a.G + row - token * a.G;
         const int64_t t = it.first_token + token;
         const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[it.head] : 1.0f) / l;
-        T *out = (T *)a.out + t * a.out_token + hq * a.out_head + lane * V;
-        for (int j = 0; j < V; ++j)
-            if (lane * V + j < a.D) out[j] = (T)(l == 0.0f ? 0.0f : o[j] * inv);
-        if (a.lse && lane == 0)
-            a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-    };
+        T *out = (T *)a.out + t * a.out_token + hq * a.out_head + d;
+        if constexpr (V == 4) {  // (the dimension is a multiple of 8)
+            if (d < a.D)
+                *(uint2 *)out = l == 0.0f ? make_uint2(0, 0) : make_uint2(pack2<T>(o[0] * inv, o[1] * inv),
+                                                                          pack2<T>(o[2] * inv, o[3] * inv));
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (d + j < a.D) out[j] = (T)(l == 0.0f ? 0.0f : o[j] * inv);
+        }
+        if (a.lse && d == 0) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+};
+
+template <class T, int DP, int WAVES, int PER>
+__global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a, int tile_rows, int entries,
+                                                             const float *part_o, const float2 *part_ml,
+                                                             const KvJoin *joins)
+{
+    constexpr int V = DP / 64, Lanes = DP / 4, Rows = 64 / Lanes;
+    __shared__ float2 red[WAVES];
+    __shared__ float acc[WAVES][DP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t todo = 1;
+    if constexpr (PER > 1) {
+        static_assert(PER <= 64, "a lane per entry");
+        const int e = blockIdx.x * PER + lane;
+        todo = __ballot(lane < PER && e < entries && joins[e].parts != 0);
+    }
     for (; todo; todo &= todo - 1) {
-        run = blockIdx.x * PER + (PER > 1 ? __builtin_ctzll(todo) : 0);
-        it = joins[run];
+        const KvJoin it = joins[blockIdx.x * PER + (PER > 1 ? __builtin_ctzll(todo) : 0)];
         if (it.parts == 0) continue;
-        constexpr std::integral_constant<int, kAhead> many{};
         if (it.parts <= kFewParts) {
-#pragma unroll 2
-            for (int y = blockIdx.y * WAVES + wave; y < it.rows; y += gridDim.y * WAVES) {
-                if (it.parts <= 2) sum(std::integral_constant<int, 2>{}, y, 0, 1);
-                else sum(many, y, 0, 1);
-                write(y);
+            const int d = lane % Lanes * 4;
+            for (int y = (blockIdx.y * WAVES + wave) * Rows + lane / Lanes; y < it.rows; y += gridDim.y * WAVES * Rows) {
+                RowSum<4> s;
+                s.clear();
+                if (it.parts <= 2) s.sum<DP, 2>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
+                else s.sum<DP, 8>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
+                s.write<T>(a, it, y, d);
             }
             continue;
         }
         for (int y = blockIdx.y; y < it.rows; y += gridDim.y) {
-            sum(many, y, wave, WAVES);
-            if (lane == 0) red[wave] = make_float2(m, l);
-            for (int j = 0; j < V; ++j) acc[wave][lane * V + j] = o[j];
+            RowSum<V> s;
+            s.clear();
+            s.template sum<DP, 8>(it, tile_rows, part_o, part_ml, y, lane * V, wave, WAVES);
+            if (lane == 0) red[wave] = make_float2(s.m, s.l);
+            for (int j = 0; j < V; ++j) acc[wave][lane * V + j] = s.o[j];
             __syncthreads();
             if (wave == 0) {
-                for (int w = 1; w < WAVES; ++w) join(red[w], &acc[w][lane * V]);
-                write(y);
+                for (int w = 1; w < WAVES; ++w) s.add(red[w], &acc[w][lane * V]);
+                s.template write<T>(a, it, y, lane * V);
             }
             __syncthreads();
         }
@@ -296,10 +315,11 @@ template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, 
                         hipStream_t st)
 {
     // few items may have many parts and are few among the runs: sixteen waves to a row, 32
-    // runs a workgroup; else a wave to a row, and a run
+    // runs a workgroup; else a workgroup to a run and as many rows as it joins at once
     const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
     const bool few = c.rows == 16 && a.R * (int64_t)a.H <= 64;
-    const dim3 grid(few ? (entries + 31) / 32 : entries, few ? most : std::min((most + 3) / 4, 16u));
+    const unsigned at_once = 4 * (256 / DP);  // rows of a workgroup
+    const dim3 grid(few ? (entries + 31) / 32 : entries, few ? most : (most + at_once - 1) / at_once);
     auto join = [&](auto kernel) {
         kernel<<<grid, few ? 1024 : 256, 0, st>>>(a, c.rows, entries, w.o, w.ml, w.joins);
     };
