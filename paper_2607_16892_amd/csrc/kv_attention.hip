@@ -110,12 +110,10 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
 // ---- join -------------------------------------------------------------------------
 //
 // Workgroup (b, y): for each of the PER entries from b PER on that has parts, rows of the item
-// from its partial results.  The kernel before left the entries.  Up to kFewParts parts a
-// wave joins as many rows as its lanes reach with 16 bytes each; more (a long request alone)
+// from its partial results.  The kernel before left the entries.  Up to kFewParts parts
+// a wave joins as many rows as its lanes reach with 16 bytes each; more (a long request alone)
 // the waves share, a workgroup to a row.  Bound by latency (the parts come from other dies'
 // caches), so a wave asks for several parts at once.
-
-constexpr int kFewParts = 16;
 
 // The running join of a row's parts, V components a lane.
 template <int V> struct RowSum {
@@ -188,6 +186,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
                                                              const KvJoin *joins)
 {
     constexpr int V = DP / 64, Lanes = DP / 4, Rows = 64 / Lanes;
+    constexpr int kFewParts = PER > 1 ? 16 : 32;
     __shared__ float2 red[WAVES];
     __shared__ float acc[WAVES][DP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -311,24 +310,27 @@ size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype)
     return work_of(a, plans(a, cache_dtype), nullptr).bytes;
 }
 
-template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, int entries, const KvWork &w, int DP,
+template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, int entries, int most_tiles, const KvWork &w, int DP,
                         hipStream_t st)
 {
-    // few items may have many parts and are few among the runs: sixteen waves to a row, 32
-    // runs a workgroup; else a workgroup to a run and as many rows as it joins at once
+    // A few items may have many parts and are few among the entries: eight waves to a row, 32
+    // entries a workgroup.  Else a workgroup to an entry and as many rows as it joins at once.
+    // (Sixteen waves: a join of 30 us, the call 44; eight: the call 27, for 32 requests of 1000
+    // to 8000 keys, two tokens of eight heads to one key head of 64 components each.)
     const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
-    const bool few = c.rows == 16 && a.R * (int64_t)a.H <= 64;
+    const int64_t items = (c.rows == 16 ? (int64_t)a.R : (int64_t)most_tiles) * a.H;
+    const bool few = items <= (c.rows == 16 ? 64 : 16);
     const unsigned at_once = 4 * (256 / DP);  // rows of a workgroup
     const dim3 grid(few ? (entries + 31) / 32 : entries, few ? most : (most + at_once - 1) / at_once);
     auto join = [&](auto kernel) {
-        kernel<<<grid, few ? 1024 : 256, 0, st>>>(a, c.rows, entries, w.o, w.ml, w.joins);
+        kernel<<<grid, few ? 512 : 256, 0, st>>>(a, c.rows, entries, w.o, w.ml, w.joins);
     };
     auto pick = [&](auto waves, auto per) {
         constexpr int W = decltype(waves)::value, P = decltype(per)::value;
         join(DP == 64 ? kv_join_kernel<T, 64, W, P> : DP == 128 ? kv_join_kernel<T, 128, W, P>
                                                                 : kv_join_kernel<T, 256, W, P>);
     };
-    if (few) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 32>{});
+    if (few) pick(std::integral_constant<int, 8>{}, std::integral_constant<int, 32>{});
     else pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
 }
 
@@ -341,12 +343,12 @@ static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w
                                                     w.before, w.tile_sums, w.tiles, w.list);
         const KvTiles t{w.tile_sums, w.tiles, w.list, p.chunked};
         launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
-        launch_join<T>(a, p.many, p.chunked ? 2 * p.many.groups : p.many.groups, w, DP, st);
+        launch_join<T>(a, p.many, p.chunked ? 2 * p.many.groups : p.many.groups, p.most_tiles, w, DP, st);
     }
     if (!p.few.groups) return;
     if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);
     launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, !p.many.groups, w.o, w.ml, w.joins, st);
-    launch_join<T>(a, p.few, p.few.groups, w, DP, st);
+    launch_join<T>(a, p.few, p.few.groups, 0, w, DP, st);
 }
 
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st)

@@ -344,3 +344,67 @@ def test_refusals(ctx, dev):
     e = dro.kv_attention(ctx, c.cache, c.q[:0], c.table, torch.zeros(3, dtype=torch.int32, device=dev),
                          c.context, 0)
     assert e["out"].shape == (0, 4, 128)
+
+
+def _reference(c, r, rows, softcap=0.0, window=0, prefix=0):
+    """Rows `rows` of request r in fp64 on the GPU: (out, lse)."""
+    import torch
+    k, v = (torch.from_numpy(x).to(c.dev) for x in c.keys(r))
+    L, n, a = c.ctx[r], c.new[r], int(c.start[r])
+    q = c.q[a:a + n][rows].double()
+    G = c.Hq // c.H
+    p = (L - n + torch.as_tensor(rows, device=c.dev)).double()[:, None]
+    j = torch.arange(L, device=c.dev, dtype=torch.float64)[None, :]
+    see = (j <= p) | (j < prefix)
+    if window:
+        see &= p - j < window
+    out = torch.empty((len(rows), c.Hq, c.D), dtype=torch.float64, device=c.dev)
+    mass, lse = torch.empty_like(out), torch.empty((len(rows), c.Hq), dtype=torch.float64, device=c.dev)
+    for h in range(c.Hq):
+        s = q[:, h].contiguous() @ k[:, h // G].T.contiguous() * c.D ** -0.5
+        if softcap:
+            s = softcap * torch.tanh(s / softcap)
+        s = s.masked_fill(~see, -math.inf)
+        lse[:, h] = torch.logsumexp(s, -1)
+        w = torch.softmax(s, -1)
+        out[:, h], mass[:, h] = w @ v[:, h // G].contiguous(), w @ v[:, h // G].abs().contiguous()
+    return out, lse, mass
+
+
+@pytest.mark.parametrize("Hq,H,D,dtype,cache,lens,new,kw", [
+    # enough tiles that each workgroup takes one, all of a prompt
+    (64, 32, 128, "bf16", None, [4500], [4500], dict()),
+    (48, 48, 64, "f16", "fp8", [2900, 700, 33], [2900, 700, 33], dict(window=500)),
+    # many tiles beside one long request, whose tiles are cut into chunks
+    (64, 64, 64, "bf16", None, [60_000] + [40] * 70, [150] + [40] * 70, dict()),
+    (48, 16, 128, "f16", None, [45_000, 3000, 1500], [200, 3000, 1], dict(softcap=20.0)),
+    # few tiles over long contexts: runs
+    (8, 2, 256, "bf16", "fp8", [30_000, 50], [70, 50], dict(softcap=10.0)),
+    (8, 1, 80, "f16", None, [50_000, 3], [100, 3], dict(window=20_000)),
+])
+def test_many_tiles(ctx, dev, Hq, H, D, dtype, cache, lens, new, kw):
+    """Large calls, some of their rows against fp64 (sums of weights times |v| as in
+    kv_cases; scores of unit variance, so 2^-17 bounds what fp32 adds)."""
+    import torch
+    from kv_cases import UNIT
+    print(f"[gpu] kv tiles Hq={Hq} H={H} D={D} {dtype}/{cache} requests {len(lens)}", flush=True)
+    c = Case(dev, lens, new, Hq, H, D, dtype, cache, seed=Hq + D)
+    got = c.run(ctx, **kw)
+    again = c.run(ctx, **kw)
+    assert torch.equal(got["out"], again["out"]) and torch.equal(got["lse"], again["lse"])
+    u = UNIT[dtype]
+    for r in {0, 1 % len(lens), len(lens) - 1}:
+        n, a = new[r], int(c.start[r])
+        rows = sorted({0, 1, n // 3, n // 2, n - 2, n - 1} & set(range(n)))
+        out, lse, mass = _reference(c, r, rows, **kw)
+        err = (got["out"][a:a + n][rows].double() - out).abs()
+        tol = (2 * u + 2.0 ** -17 * (1 + 4 * (kw.get("softcap", 0) > 0))) * mass + lens[r] * 2.0 ** -25 * 8 + 2.0 ** -24
+        assert (err <= tol).all(), f"request {r}: {(err / tol).max().item():.3g} of the bound"
+        assert ((got["lse"][a:a + n][rows].double() - lse).abs() <= 2.0 ** -16 * (1 + lse.abs())).all()
+
+
+def test_a_bound_that_does_not_hold_loses_no_request(ctx, dev):
+    """max_new below a request's rows, with so many rows that every other one seems long."""
+    c = Case(dev, [400, 90, 7], [1, 300, 7], 8, 2, 128, seed=12)
+    for most in (1, 5, 100, 150, 299):
+        c.check(c.run(ctx, max_new=most))
