@@ -80,10 +80,12 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
             tiles[e] = KvTile{lo, tile, s.n, s.ctx, min(max(a.start[lo], 0), a.T), (int)steps, 0, 1, 0};
         }
         const uint64_t upto = plan_scan(steps, part, total);
-        if (!chunked && e < n) sums[e] = tiles[e].before = steps_before + upto - steps;
+        if (e < n) sums[e] = tiles[e].before = steps_before + upto - steps;
         steps_before += total;
     }
     uint64_t all = steps_before, parts = 0;
+    // a few steps a workgroup: beginning a tile takes longer, so none takes two
+    chunked = chunked || steps_before * a.H < (uint64_t)kFewSteps * cut.groups;
     if (chunked) {
         const uint64_t most_steps = kv_tile_run(cut, steps_before * a.H);
         all = 0;
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
     }
     if (threadIdx.x == 0) {
         sums[n] = all;
-        *list = KvTileList{n, (int)parts, all};
+        *list = KvTileList{n, (int)parts, all, chunked};
     }
 }
 
@@ -186,30 +188,34 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
                                                              const KvJoin *joins)
 {
     constexpr int V = DP / 64, Lanes = DP / 4, Rows = 64 / Lanes;
-    constexpr int kFewParts = PER > 1 ? 16 : 32;
+    constexpr int kFewParts = PER > 4 ? 16 : 32;
     __shared__ float2 red[WAVES];
     __shared__ float acc[WAVES][DP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint64_t todo = 1;
-    if constexpr (PER > 1) {
-        static_assert(PER <= 64, "a lane per entry");
+    uint64_t one = 0, many = 0;  // entries whose rows a wave joins, and the others
+    {
         const int e = blockIdx.x * PER + lane;
-        todo = __ballot(lane < PER && e < entries && joins[e].parts != 0);
+        static_assert(PER <= 64, "a lane per entry");
+        const int parts = lane < PER && e < entries ? joins[e].parts : 0;
+        one = __ballot(parts > 0 && parts <= kFewParts);
+        many = __ballot(parts > kFewParts);
     }
-    for (; todo; todo &= todo - 1) {
-        const KvJoin it = joins[blockIdx.x * PER + (PER > 1 ? __builtin_ctzll(todo) : 0)];
-        if (it.parts == 0) continue;
-        if (it.parts <= kFewParts) {
-            const int d = lane % Lanes * 4;
-            for (int y = (blockIdx.y * WAVES + wave) * Rows + lane / Lanes; y < it.rows; y += gridDim.y * WAVES * Rows) {
-                RowSum<4> s;
-                s.clear();
-                if (it.parts <= 2) s.sum<DP, 2>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
-                else s.sum<DP, 8>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
-                s.write<T>(a, it, y, d);
-            }
-            continue;
+    // with several entries the waves take them in turn, with one its rows
+    const int d = lane % Lanes * 4, mine = PER > 1 ? wave : 0, y_waves = PER > 1 ? 1 : WAVES;
+    const int y0 = (blockIdx.y * y_waves + (PER > 1 ? 0 : wave)) * Rows + lane / Lanes;
+    for (int nth = 0; one; one &= one - 1, ++nth) {
+        if (PER > 1 && nth % WAVES != mine) continue;
+        const KvJoin it = joins[blockIdx.x * PER + __builtin_ctzll(one)];
+        for (int y = y0; y < it.rows; y += gridDim.y * y_waves * Rows) {
+            RowSum<4> s;
+            s.clear();
+            if (it.parts <= 2) s.sum<DP, 2>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
+            else s.sum<DP, 8>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
+            s.write<T>(a, it, y, d);
         }
+    }
+    for (; many; many &= many - 1) {
+        const KvJoin it = joins[blockIdx.x * PER + __builtin_ctzll(many)];
         for (int y = blockIdx.y; y < it.rows; y += gridDim.y) {
             RowSum<V> s;
             s.clear();
@@ -236,7 +242,7 @@ constexpr int kFewRows = 32;
 struct KvPlans {
     KvCut few, many;       // groups == 0: not launched
     int most_tiles;        // of the requests of many rows
-    bool chunked;          // a workgroup to a tile
+    bool chunked;          // a workgroup to a tile (the device may find that so besides)
     unsigned grid;
 };
 
@@ -264,7 +270,7 @@ static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
         // four tiles a workgroup of one round level the differences; more launches than 2^23
         // workgroups are not needed either way
         p.chunked = items >= 4 * p.many.groups && items < (1 << 23);
-        p.grid = (unsigned)(p.chunked ? items + p.many.groups + kDies : p.many.groups);
+        p.grid = (unsigned)(std::min<int64_t>(items, 1 << 23) + p.many.groups + kDies);
     }
     return p;
 }
@@ -319,19 +325,18 @@ template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, 
     // to 8000 keys, two tokens of eight heads to one key head of 64 components each.)
     const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
     const int64_t items = (c.rows == 16 ? (int64_t)a.R : (int64_t)most_tiles) * a.H;
-    const bool few = items <= (c.rows == 16 ? 64 : 16);
-    const unsigned at_once = 4 * (256 / DP);  // rows of a workgroup
-    const dim3 grid(few ? (entries + 31) / 32 : entries, few ? most : (most + at_once - 1) / at_once);
-    auto join = [&](auto kernel) {
-        kernel<<<grid, few ? 512 : 256, 0, st>>>(a, c.rows, entries, w.o, w.ml, w.joins);
-    };
-    auto pick = [&](auto waves, auto per) {
+    const bool few = items <= 64;
+    const unsigned at_once = 4 * (256 / DP);  // rows of four waves
+    const unsigned rows = (most + at_once - 1) / at_once;
+    auto pick = [&](auto waves, auto per, unsigned y) {
         constexpr int W = decltype(waves)::value, P = decltype(per)::value;
-        join(DP == 64 ? kv_join_kernel<T, 64, W, P> : DP == 128 ? kv_join_kernel<T, 128, W, P>
-                                                                : kv_join_kernel<T, 256, W, P>);
+        auto kernel = DP == 64 ? kv_join_kernel<T, 64, W, P> : DP == 128 ? kv_join_kernel<T, 128, W, P>
+                                                                         : kv_join_kernel<T, 256, W, P>;
+        kernel<<<dim3((entries + P - 1) / P, y), W * 64, 0, st>>>(a, c.rows, entries, w.o, w.ml, w.joins);
     };
-    if (few) pick(std::integral_constant<int, 8>{}, std::integral_constant<int, 32>{});
-    else pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+    if (few) pick(std::integral_constant<int, 8>{}, std::integral_constant<int, 32>{}, most);
+    else if (c.rows == 16) pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{}, rows);
+    else pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{}, 2 * rows);
 }
 
 template <class T>
@@ -341,9 +346,9 @@ static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w
     if (p.many.groups) {
         kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles, p.chunked,
                                                     w.before, w.tile_sums, w.tiles, w.list);
-        const KvTiles t{w.tile_sums, w.tiles, w.list, p.chunked};
+        const KvTiles t{w.tile_sums, w.tiles, w.list};
         launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
-        launch_join<T>(a, p.many, p.chunked ? 2 * p.many.groups : p.many.groups, p.most_tiles, w, DP, st);
+        launch_join<T>(a, p.many, 2 * p.many.groups, p.most_tiles, w, DP, st);
     }
     if (!p.few.groups) return;
     if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);

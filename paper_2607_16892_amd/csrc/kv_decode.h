@@ -261,13 +261,13 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
                         const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
                         const char *at = vp + (id * a.v_block + (int64_t)(key & in_block) * a.v_token) * E;
                         int D = a.D;
-                        asm volatile("" : "+s"(D));  // compared with anew: 32 masks would not fit
+                        asm volatile("" : "+s"(D));  // compared with anew: 32 addresses would not fit
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
 #pragma unroll
                             for (int j = 0; j < VW; ++j) {
                                 const int d = VW * (grp * 4 + c) + j;
-                                const float y = FULL || d < D ? value_at<C>(at, d) : 0.0f;
+                                const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
                                 o[j][c] += seen && !__builtin_isfinite(y) ? wt * y : 0.0f;
                                 __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
                             }

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     const uint32_t die = blockIdx.x % kDies, nth = blockIdx.x / kDies;
     uint32_t group = 0;
     uint64_t run = 1, unit, end;
-    if (tiles.chunked) {
+    if (list.chunked) {
         const uint64_t each = (all + kDies - 1) / kDies;
         unit = die * each + nth;
         end = nth < each && unit < all ? unit + 1 : unit;
@@ -140,10 +140,11 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
     } else {
         run = kv_tile_run(cut, all);
-        group = die * (gridDim.x / kDies) + nth;
+        if ((int)blockIdx.x >= cut.groups) return;
+        group = die * (cut.groups / kDies) + nth;
         unit = group * run;
         end = min(unit + run, all);
-        if (threadIdx.x == 0) joins[group].parts = 0;
+        if (threadIdx.x == 0) joins[group].parts = joins[cut.groups + group].parts = 0;
     }
     int entry = -1;
     while (unit < end) {
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         const int r = rt.r, tile = rt.tile;
         const int item_steps = rt.steps;
         int step0 = (int)(u1 - rt.before), go, place;
-        if (tiles.chunked) {
+        if (list.chunked) {
             const int chunks = rt.chunks;
             const int each = (item_steps + chunks - 1) / chunks;
             place = rt.part + list.parts * h + step0;
@@ -460,13 +461,13 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                             const char *at = (const char *)a.v + (id * a.v_block + (int64_t)(kk & in_block) * a.v_token +
                                                                   (int64_t)h * a.v_head) * E;
                             int D = a.D;
-                            asm volatile("" : "+s"(D));  // compared with anew: the masks would not fit
+                            asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
 #pragma unroll
                             for (int j = 0; j < ND; ++j)
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
                                     const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-                                    const float y = FULL || d < D ? value_at<C>(at, d) : 0.0f;
+                                    const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
                                     o[j][i] += seen && !__builtin_isfinite(y) ? wt * y : 0.0f;
                                     __builtin_amdgcn_sched_barrier(0);
                                 }
@@ -520,7 +521,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         }
         if (!whole && step0 == 0 && threadIdx.x == 0) {
-            KvJoin &j = joins[tiles.chunked ? place : group];
+            KvJoin &j = joins[list.chunked ? place : group];
             j.first_token = first_token;
             j.row0 = row0;
             j.rows = rows;

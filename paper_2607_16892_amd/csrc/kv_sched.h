@@ -34,7 +34,8 @@ struct KvItem {
 // with many, a workgroup takes a tile and the hardware deals them, longest first, since
 // beginning a tile takes as long as several steps and workgroups do not run at one speed
 // (a prompt of 8192 tokens, 64 heads on 8: equal runs of eight tiles ended after 1143 to
-// 1694 us).  There a tile of more than an equal share of the steps is cut into chunks.
+// 1694 us).  There a tile of more than an equal share of the steps is cut into chunks.  So it
+// is where there are few steps: a workgroup then begins one tile and not several.
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
@@ -187,6 +188,8 @@ __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, in
 
 // ---- many rows a request ------------------------------------------------------------
 
+constexpr int kFewSteps = 8;  // of a workgroup
+
 constexpr int kDies = 8;  // workgroups go to the dies (an L2 each) in turn
 
 struct KvTile {
@@ -201,12 +204,12 @@ struct KvTileList {  // (one load)
     int count;  // tiles
     int parts;  // partial results of a head
     uint64_t all;  // steps, or chunks, of a head
+    int chunked;
 };
 struct KvTiles {
     const uint64_t *sums;  // [count + 1] exclusive sums of the tiles' steps, or chunks
     const KvTile *tiles;   // [count]
     const KvTileList *list;
-    bool chunked;
 };
 
 // Steps of `keys` keys of a tile.
