@@ -18,8 +18,9 @@
  * Block 1 of Alg. 1 under the memory-capacity constraint (Sec. 3.4).
  * Further entry points: the same table exactly from value counts, the
  * dual over continuous gamma, per-class moments and the cost of given
- * reservations (the policy comparison of Sec. 5), and the rest of Alg. 1
- * (routing LP, prefix caching, configuration search; last section).
+ * reservations (the policy comparison of Sec. 5), the rest of Alg. 1
+ * (routing LP, prefix caching, configuration search), and the paged cache that
+ * the reservations are for (block tables, store, attention; last section).
  *
  * Conventions, binding on every entry point:
  *  - Array arguments are DEVICE memory owned by the caller unless the field
@@ -46,6 +47,9 @@
  *    correctly.  A replay uses the ctx's workspace and staged offsets as they
  *    are then: after any call on that ctx with another problem or on another
  *    stream, capture again.  (dro_cost_eval_noalloc has no such bond to its ctx.)
+ *    kv_block_tables, kv_store and kv_attention enqueue kernels only as well, once
+ *    the workspace is as large as they need: a replay stays right until a call on
+ *    that ctx needs a larger one.
  *  - Exactness limits (DRO_ELIMIT when exceeded): 0 <= x, eta <= L <= 2^15,
  *    N_c <= 2^26 samples per class, every lam, c_p, c_w in [2^-10, 2^7];
  *    K <= 2^15 + 1 grid points, M <= 65536 multipliers, K * M < 2^31 pairs,
@@ -421,7 +425,8 @@ int dro_bcd_solve(dro_ctx *ctx, const dro_problem *p, const float *eps, const dr
  * 1024 tokens, a power of two; head dimension a multiple of 8 up to 256; R up
  * to 2^20 requests, T up to 2^24 tokens a call, T * heads up to 2^30,
  * max_blocks * block up to 2^30 tokens a request, R * max_blocks and
- * num_blocks * block up to 2^31 - 1 (byte offsets into the cache are 64-bit), a head's tokens within a block closer than 2^31 bytes.
+ * num_blocks * block up to 2^31 - 1 (byte offsets into the cache are 64-bit),
+ * the tokens of a block within 2^31 bytes.
  * Device data steers no read or write outside the arrays given: a block
  * outside the pool is read as the nearest one of the pool, a slot outside it
  * is not written, lengths and offsets are cut to the table and to T.
@@ -447,9 +452,10 @@ enum { DRO_BF16 = 0, DRO_F16 = 1, DRO_FP8_E4M3 = 2 };
  *   granted [R] = 1 or 0, start [R+1] = the exclusive sums of n, and for token
  *   t = start[r] + i < T of a granted request pos[t] = len[r] + i and its slot
  *   slot[t]; -1 in both for tokens that were not granted and for t >= start[R].
- * held_out and free_out may be held and free_count themselves (in place); as
- * they may be others, a step can be tried: called again with the same inputs
- * it gives the same outputs.  Negative lengths count as 0, held as cut to
+ * held_out and free_out may be held and free_count themselves (in place); no
+ * other output may overlap an input.  With others the step leaves its inputs as
+ * they are but for entries that are free or unnamed before it, so it can be tried:
+ * called again with the same inputs it gives the same outputs.  Negative lengths count as 0, held as cut to
  * [0, max_blocks], free_count to [0, num_blocks]. */
 typedef struct {
     int32_t R;             /* requests                                                */
@@ -471,9 +477,10 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *pool, const int32_t *len, c
 /* One layer's cache: element (block b, token i, head h, component d) of the keys
  * is k[b k_block + i k_token + h k_head + d], so blocks may hold their tokens
  * or their heads together.  Components are contiguous; every stride is a multiple
- * of 8 elements, and k and v are aligned to 8 elements.  dtype DRO_FP8_E4M3 holds key / k_scale[h] and value /
- * v_scale[h], rounded to nearest even and saturated at +-448 (NaN stays NaN);
- * the scales ([heads], > 0) are NULL for the other types. */
+ * of 8 elements, and k and v are aligned to 8 elements.  dtype DRO_FP8_E4M3 holds
+ * key / k_scale[h] and value / v_scale[h], rounded to nearest even and saturated
+ * at +-448 (NaN stays NaN); the scales ([heads], > 0) are NULL for the other
+ * types. */
 typedef struct {
     int32_t dtype;
     int32_t heads, dim, block, num_blocks;
@@ -504,8 +511,9 @@ int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, 
  * A row that sees no key (or whose s are all -infinity) has out = 0 and lse =
  * -infinity; keys and values that a row does not see do not enter it, whatever
  * they hold.  Rows of no request (t outside [start[0], start[R])) are zero with
- * lse -infinity.  Products, sums and the softmax are kept in fp32; the weights
- * are rounded to q's type for the product with the values.
+ * lse -infinity.  Products, sums and the softmax are kept in fp32 (the cap's tanh
+ * to 2^-21 of the cap); the weights are rounded to q's type for the product with
+ * the values.  Two calls with the same arguments give the same bits.
  * max_new bounds the rows of one request and picks the kernels (a larger request
  * is computed all the same). */
 typedef struct {

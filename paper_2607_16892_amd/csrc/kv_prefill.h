@@ -95,7 +95,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     constexpr bool F8 = E == 1;
     constexpr int KT = prefill_keys(DP);
     constexpr int S = DP / 16;           // steps of 16 components of a score
-    constexpr int NT = KT / 32;          // score tiles
+    // keys whose scores are in registers at once: 128 beside the changes of the scores spill
+    constexpr int SK = MODS && KT > 64 ? 64 : KT;
+    constexpr int NT = SK / 32;          // their tiles
     constexpr int DS = prefill_split(DP);
     constexpr int ND = DP / 32 / DS;     // component tiles of a wave
     constexpr int Rows = prefill_rows(DP);
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     // two tiles of keys and of values, by name: the compiler then knows that reading one waits
     // for no load into another
     __shared__ __align__(16) char k_even[Tile], k_odd[Tile], v_even[Tile], v_odd[Tile];
-    __shared__ int found[4];                            // a wave found infinities or NaN
+    __shared__ int found;  // infinities or NaN among values that only some rows see
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         const float cap = a.cap * kLog2e;
         float to_exp = MODS && a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
         if constexpr (!MODS) {  // scale > 0 from here on, so the largest score has the largest weight
-            to_exp = fabsf(ks) * kLog2e;
+            to_exp = fmaxf(fabsf(ks) * kLog2e, 0x1p-126f);  // (a hidden key's -infinity times zero would be NaN)
             if (ks < 0.0f)
 #pragma unroll
                 for (int s = 0; s < S; ++s) q[s] ^= 0x80008000u;
@@ -234,6 +236,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         };
         Words<2> reg[F8 ? UP * IP : 1];
         auto load = [&](auto odd_tile, int u) {
+            int lane = threadIdx.x & 63;
+            asm volatile("" : "+v"(lane));  // (see `fresh`)
 #pragma unroll
             for (int j = 0; j < UP; ++j) {
                 const bool vals = (wave + 4 * j) / NG;
@@ -284,16 +288,23 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 }
             }
         };
+        // Where a lane reads, for piece 0 of the keys and of the values; the others follow by an
+        // exclusive or and an offset.  Each step computes them anew: kept over the steps they take
+        // the registers of the queries, which then come back from memory behind the tile on its way.
+        auto key_place = [&](int lane) {
+            return (uint32_t)((lane & 31) * Row + ((lane >> 5) ^ key_turn<DP>(lane & 31)) * 16);
+        };
+        auto value_place = [&](int lane) {
+            const int i = lane & 15, rr = (lane >> 5) * 4 + (i >> 2), d = dt0 * 32 + (lane & 16) + (i & 3) * 4;
+            return (uint32_t)(rr * Row + ((d >> 3) ^ value_turn<DP>(rr)) * 16 + (d & 4) * 2);
+        };
         // 8 weights' worth of component n32 of tile j: keys 16 x + 4 half + {0 .. 3, 8 .. 11}
-        auto value_frag = [&](const char *sv, int x, int j) {
+        auto value_frag = [&](const char *sv, uint32_t at, int x, int j) {
             u32x4 y;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int i = lane & 15, rr = x * 16 + e * 8 + half * 4 + (i >> 2);
-                const int d = (dt0 + j) * 32 + (lane & 16) + (i & 3) * 4;
                 const auto z = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) Vec<short, 4> *)(sv + rr * Row + ((d >> 3) ^ value_turn<DP>(rr)) * 16 +
-                                                                        (d & 4) * 2));
+                    (__attribute__((address_space(3))) Vec<short, 4> *)(sv + (at ^ (j * 64)) + (x * 16 + e * 8) * Row));
                 const Vec<uint32_t, 2> w = __builtin_bit_cast(Vec<uint32_t, 2>, z);
                 y[2 * e] = w[0];
                 y[2 * e + 1] = w[1];
@@ -311,6 +322,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         constexpr std::integral_constant<bool, false> even{};
         constexpr std::integral_constant<bool, true> odd{};
         __syncthreads();  // the last item's tiles are read
+        if (threadIdx.x == 0) found = 0;
         if (steps) {
             load_ids(0);
             load(even, 0);
@@ -319,7 +331,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         }
         auto step = [&](auto odd_tile, int u) {
             constexpr std::integral_constant<bool, !decltype(odd_tile)::value> next{};
-            const int key0 = k0 + u * KT;
+            const int tile0 = k0 + u * KT;
             char *sk = decltype(odd_tile)::value ? k_odd : k_even, *sv = decltype(odd_tile)::value ? v_odd : v_even;
             __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile u has landed
             __syncthreads();                     // everybody's has, and tile u - 1 is read
@@ -329,8 +341,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
             // A weight of zero does not silence an infinity or a NaN.  Where some row of the
             // workgroup does not see some key of the tile, such values become zero in LDS and are
-            // added apart, to the rows that see them.
-            const bool mixed = key0 < bot.lo || key0 + KT > top.hi;
+            // added after the last step, to the rows that see them.
+            const bool mixed = tile0 < bot.lo || tile0 + KT > top.hi;
             if (mixed) {
                 uint32_t bad = 0;
                 for (int i = threadIdx.x; i < Tile / 16; i += 256) {
@@ -343,16 +355,21 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     }
                     if (mask[0] | mask[1] | mask[2] | mask[3]) y &= ~mask;
                 }
-                bad = __any(bad);
-                if (lane == 0) found[wave] = bad;
+                if (bad) found = 1;
                 __syncthreads();
             }
-            const bool none = idle || key0 >= wbot.hi || key0 + KT <= wtop.lo;
-            if (!none) {
+#pragma unroll
+            for (int sub = 0; sub < KT; sub += SK) {
+                const int key0 = tile0 + sub;
+                const bool none = idle || key0 >= wbot.hi || key0 + SK <= wtop.lo;
+                if (none) continue;
                 // pieces of the keys and of the values are read kAheadOf products before their
                 // use, the first of the values before the softmax
+                int fresh = lane;
+                asm volatile("" : "+v"(fresh));
+                const uint32_t k_at = key_place(fresh), v_at = value_place(fresh);
                 auto key_frag = [&](int f) {
-                    return *(const u32x4 *)&sk[(f / S * 32 + n32) * Row + ((2 * (f % S) + half) ^ key_turn<DP>(n32)) * 16];
+                    return *(const u32x4 *)&sk[(k_at ^ (f % S * 32)) + (sub + f / S * 32) * Row];
                 };
                 __builtin_amdgcn_s_setprio(1);
                 f32x16 s[NT];
@@ -368,7 +385,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     if (f + kAheadOf < NT * S) kf[f % kAheadOf] = key_frag(f + kAheadOf);
                 }
 #pragma unroll
-                for (int f = 0; f < kAheadOf; ++f) vf[f] = value_frag(sv, f / ND, f % ND);
+                for (int f = 0; f < kAheadOf; ++f) vf[f] = value_frag(sv + sub * Row, v_at, f / ND, f % ND);
                 __builtin_amdgcn_sched_group_barrier(kDsRead, kAheadOf, 0);
 #pragma unroll
                 for (int f = 0; f < NT * S - kAheadOf; ++f) {
@@ -381,26 +398,31 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
                 }
                 __builtin_amdgcn_s_setprio(0);
-                const bool edge = key0 < wbot.lo || key0 + KT > min(wtop.hi, k1);
+                const bool edge = key0 < wbot.lo || key0 + SK > min(wtop.hi, k1);
                 const int lane0 = key0 + half * 4, from = see.lo - lane0, dist = lane0 - p_row;
                 const uint32_t seen = (uint32_t)max(see.hi - see.lo, 0);
                 if constexpr (MODS) {
-                    const float b0 = slope * (float)dist;
+                    // (groups of four keys, so that few constants take registers)
+                    const float b0 = slope * (float)dist, by4[4] = {0.0f, slope, 2.0f * slope, 3.0f * slope};
+                    auto add = [&](int t, int i) {
+                        const float b = __builtin_fmaf((float)(t * 4 + (i >> 2)), 8.0f * slope, b0);
+                        return i & 3 ? b + by4[i & 3] : b;
+                    };
                     if (a.cap > 0.0f) {
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                const float c = (float)(t * 32 + (i >> 2) * 8 + (i & 3));  // the key less `lane0`
-                                s[t][i] = tanh_scaled(s[t][i] * to_exp, cap, __builtin_fmaf(c, slope, b0));
+                                s[t][i] = tanh_scaled(s[t][i] * to_exp, cap, add(t, i));
+                                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                             }
                     } else {
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                const float c = (float)(t * 32 + (i >> 2) * 8 + (i & 3));
-                                s[t][i] = __builtin_fmaf(s[t][i], to_exp, __builtin_fmaf(c, slope, b0));
+                                s[t][i] = __builtin_fmaf(s[t][i], to_exp, add(t, i));
+                                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                             }
                     }
                 }
@@ -442,44 +464,12 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                         l += s[t][i] + s[t][i + 1];
                         w[2 * t + (i >> 3)][(i >> 1) & 3] = pack2<T>(s[t][i], s[t][i + 1]);
                     }
-                if (mixed && (found[0] | found[1] | found[2] | found[3])) {
-                    for (int x = 0; x < NT * 16; ++x) {
-                        float mine = 0.0f;
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                mine = x == t * 16 + i ? s[t][i] : mine;
-                                __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
-                            }
-                        for (int g = 0; g < 2; ++g) {
-                            const float wt = __shfl(mine, n32 + 32 * g);
-                            const int key = key0 + (x >> 4) * 32 + ((x >> 2) & 3) * 8 + g * 4 + (x & 3);
-                            const bool seen = key >= see.lo && key < see.hi;
-                            const int kk = min(key, k1 - 1);
-                            const int id = min(max(table[kk >> a.shift], 0), a.num_blocks - 1);
-                            const char *at = (const char *)a.v + (id * a.v_block + (int64_t)(kk & in_block) * a.v_token +
-                                                                  (int64_t)h * a.v_head) * E;
-                            int D = a.D;
-                            asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
-#pragma unroll
-                            for (int j = 0; j < ND; ++j)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-                                    const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
-                                    o[j][i] += seen && !__builtin_isfinite(y) ? wt * y : 0.0f;
-                                    __builtin_amdgcn_sched_barrier(0);
-                                }
-                        }
-                    }
-                }
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int f = 0; f < NT * 2 * ND; ++f) {
                     o[f % ND] = mfma32<T>(vf[f % kAheadOf], w[f / ND], o[f % ND]);
                     const int g = f + kAheadOf;
-                    if (g < NT * 2 * ND) vf[f % kAheadOf] = value_frag(sv, g / ND, g % ND);
+                    if (g < NT * 2 * ND) vf[f % kAheadOf] = value_frag(sv + sub * Row, v_at, g / ND, g % ND);
                 }
 #pragma unroll
                 for (int f = 0; f < NT * 2 * ND - kAheadOf; ++f) {
@@ -496,6 +486,28 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             if (u + 1 < steps) step(odd, u + 1);
         }
 
+        if (steps && found && !idle) {  // (the steps' barriers order `found`)
+            // whatever its weight, an infinity stays one, and a NaN
+            for (int key = k0; key < k1; ++key) {
+                const int at_step = (key - k0) & ~(KT - 1);
+                if (k0 + at_step >= bot.lo && k0 + at_step + KT <= top.hi) continue;  // not zeroed
+                const bool seen = key >= see.lo && key < see.hi;
+                const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
+                const char *at = (const char *)a.v +
+                                 (id * a.v_block + (int64_t)(key & in_block) * a.v_token + (int64_t)h * a.v_head) * E;
+                int D = a.D;
+                asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
+#pragma unroll
+                for (int j = 0; j < ND; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
+                        const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
+                        if (seen && !__builtin_isfinite(y)) o[j][i] += y;
+                        __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
+                    }
+            }
+        }
         l = sum_halves(l);
         const bool whole = go >= item_steps;
         if (rw + n32 < rows) {

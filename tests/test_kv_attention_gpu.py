@@ -247,6 +247,19 @@ def test_large_scores_and_flat_weights(ctx, dev):
     c.check(c.run(ctx))
 
 
+@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("scale", [1e-30, -1e-30])
+def test_scores_that_vanish(ctx, dev, new, scale):
+    """A scale and a key scale whose product is below the smallest float: every key seen weighs
+    the same, and hidden ones nothing."""
+    import torch
+    import paper_2607_16892_amd as dro
+    c = Case(dev, [new + 70, new], [new, new], 4, 2, 128, "bf16", "fp8", seed=11)
+    c.ks = torch.full((2,), 1e-20)
+    c.cache = dro.KvCache(c.k, c.v, c.ks.to(dev), c.vs.to(dev))
+    c.check(c.run(ctx, scale=scale), scale=scale)
+
+
 def test_side_stream_and_graph(dev):
     """On a stream of its own, and captured: replays follow new inputs in place."""
     import torch
