@@ -45,11 +45,11 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs 
     if (threadIdx.x == 0) sums[a.R] = total;
 }
 
-// The tiles of the requests of many rows and the sums of their steps or chunks: first the
-// tiles before each request, then the list, 1024 tiles at a time.
+// The tiles of the requests of many rows and the sums of their chunks: first the tiles before
+// each request, then the list and its steps, then the chunks, 1024 tiles at a time.
 __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs a, const KvCut cut, int keys, int most,
-                                                                bool chunked, uint64_t *before, uint64_t *sums,
-                                                                KvTile *tiles, KvTileList *list)
+                                                                uint64_t *before, uint32_t *sums, KvTile *tiles,
+                                                                KvTileList *list)
 {
     __shared__ uint64_t part[kPlanThreads / 64];
     const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
     }
     __syncthreads();  // (makes `before` visible to the workgroup)
     const int n = (int)min(total, (uint64_t)most);
-    uint64_t steps_before = 0;
+    uint64_t steps_all = 0;
     for (int e0 = 0; e0 < n; e0 += kPlanThreads) {
         const int e = e0 + threadIdx.x;
         uint32_t steps = 0;
@@ -79,33 +79,29 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
             steps = kv_tile_steps(a, s, lo, tile, cut.rows, keys);
             tiles[e] = KvTile{lo, tile, s.n, s.ctx, min(max(a.start[lo], 0), a.T), (int)steps, 0, 1, 0};
         }
-        const uint64_t upto = plan_scan(steps, part, total);
-        if (e < n) sums[e] = tiles[e].before = steps_before + upto - steps;
-        steps_before += total;
+        plan_scan(steps, part, total);
+        steps_all += total;
     }
-    uint64_t all = steps_before, parts = 0;
-    // a few steps a workgroup: beginning a tile takes longer, so none takes two
-    chunked = chunked || steps_before * a.H < (uint64_t)kFewSteps * cut.groups;
-    if (chunked) {
-        const uint64_t most_steps = kv_tile_run(cut, steps_before * a.H);
-        all = 0;
-        for (int e0 = 0; e0 < n; e0 += kPlanThreads) {
-            const int e = e0 + threadIdx.x;
-            const uint64_t chunks = e < n ? (tiles[e].steps + most_steps - 1) / most_steps : 0;  // (this thread's entry)
-            const uint64_t own = chunks > 1 ? chunks | chunks << 32 : chunks;
-            const uint64_t upto = plan_scan(own, part, total) - own;
-            if (e < n) {
-                sums[e] = tiles[e].before = all + (uint32_t)upto;
-                tiles[e].part = (int)(parts + (upto >> 32));
-                tiles[e].chunks = (int)chunks;
-            }
-            all += (uint32_t)total;
-            parts += total >> 32;
+    // Chunks: of the tiles that are cut, with 1.5 shares or more, a tile has at most 4/3 as many
+    // as shares, so there are fewer than 2 `groups` of them over all heads.
+    const uint64_t share = kv_tile_share(cut, steps_all * a.H);
+    uint32_t all = 0, parts = 0;
+    for (int e0 = 0; e0 < n; e0 += kPlanThreads) {
+        const int e = e0 + threadIdx.x;
+        const uint64_t chunks = e < n ? max((tiles[e].steps + share / 2) / share, (uint64_t)1) : 0;  // (this thread's entry)
+        const uint64_t own = chunks > 1 ? chunks | chunks << 32 : chunks;
+        const uint64_t upto = plan_scan(own, part, total) - own;
+        if (e < n) {
+            sums[e] = tiles[e].before = all + (uint32_t)upto;
+            tiles[e].part = (int)(parts + (uint32_t)(upto >> 32));
+            tiles[e].chunks = (int)chunks;
         }
+        all += (uint32_t)total;
+        parts += (uint32_t)(total >> 32);
     }
     if (threadIdx.x == 0) {
         sums[n] = all;
-        *list = KvTileList{n, (int)parts, all, chunked};
+        *list = KvTileList{n, (int)parts, all};
     }
 }
 
@@ -188,7 +184,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
                                                              const KvJoin *joins)
 {
     constexpr int V = DP / 64, Lanes = DP / 4, Rows = 64 / Lanes;
-    constexpr int kFewParts = PER > 4 ? 16 : 32;
+    constexpr int kFewParts = 64;
     __shared__ float2 red[WAVES];
     __shared__ float acc[WAVES][DP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -236,19 +232,21 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
 
 static int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-// Requests of up to this many rows a key head are the one kernel's, others the other's.
-constexpr int kFewRows = 32;
+// Requests of up to this many rows a key head are the kernel's for few rows, others the other's:
+// one of its tiles.  Where the calls are small, two, as they have no list of tiles to wait for.
+// (32 requests of 1000 to 8000 keys, 8 heads to each of 4, 16 rows a key head: %FEWA%; 32
+// rows %FEWB%.  One request of 1000 keys, 32 rows: %FEWC%.)
+static int few_rows(const KvAttnArgs &a) { return (int64_t)a.R * a.H < 16 ? 32 : 16; }
 
 struct KvPlans {
     KvCut few, many;       // groups == 0: not launched
     int most_tiles;        // of the requests of many rows
-    bool chunked;          // a workgroup to a tile (the device may find that so besides)
     unsigned grid;
 };
 
 static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
 {
-    const int DP = padded_dim(a.D), few = std::max(kFewRows / a.G, 1);
+    const int DP = padded_dim(a.D), few = std::max(few_rows(a) / a.G, 1);
     const bool all_few = a.max_new <= few;
     // with so many rows that each request has more than few, the one kernel takes all (by
     // max_new, so that a bound that does not hold loses no request)
@@ -267,10 +265,8 @@ static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
         p.many.below = false;
         p.most_tiles = (int)((int64_t)a.T * a.G / p.many.rows + std::min(a.R, all_many ? a.T : a.T / (few + 1) + 1));
         const int64_t items = (int64_t)p.most_tiles * a.H;
-        // four tiles a workgroup of one round level the differences; more launches than 2^23
-        // workgroups are not needed either way
-        p.chunked = items >= 4 * p.many.groups && items < (1 << 23);
-        p.grid = (unsigned)(std::min<int64_t>(items, 1 << 23) + p.many.groups + kDies);
+        // a workgroup to a chunk (2^23 of 256 threads are a grid's limit at half)
+        p.grid = (unsigned)std::min<int64_t>((items + 2 * p.many.groups + kDies) / kDies * kDies, 1 << 23);
     }
     return p;
 }
@@ -280,7 +276,8 @@ struct KvWork {
     float2 *ml;
     KvJoin *joins;
     uint64_t *sums;    // few rows: [R + 1]
-    uint64_t *before, *tile_sums;
+    uint64_t *before;
+    uint32_t *tile_sums;
     KvTile *tiles;
     KvTileList *list;
     size_t bytes;
@@ -303,7 +300,7 @@ static KvWork work_of(const KvAttnArgs &a, const KvPlans &p, void *ws)
     w.sums = (uint64_t *)take(((size_t)a.R + 1) * 8);
     if (p.many.groups) {
         w.before = (uint64_t *)take((size_t)a.R * 8);
-        w.tile_sums = (uint64_t *)take(((size_t)p.most_tiles + 1) * 8);
+        w.tile_sums = (uint32_t *)take(((size_t)p.most_tiles + 1) * 4);
         w.tiles = (KvTile *)take((size_t)p.most_tiles * sizeof(KvTile));
         w.list = (KvTileList *)take(sizeof(KvTileList));
     }
@@ -344,7 +341,7 @@ static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w
 {
     const int DP = padded_dim(a.D);
     if (p.many.groups) {
-        kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles, p.chunked,
+        kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles,
                                                     w.before, w.tile_sums, w.tiles, w.list);
         const KvTiles t{w.tile_sums, w.tiles, w.list};
         launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);

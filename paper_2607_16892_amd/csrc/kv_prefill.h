@@ -23,8 +23,8 @@ namespace dro {
 
 // With 256 components the sums of 32 rows are half a wave's registers already, so two waves
 // share rows there: both compute the scores, each the sums of half the components.  (Whole
-// rows a wave went through memory and the accumulation registers: %D256OLD% us for the
-// mixed call of 40 requests, against %D256NEW%.)
+// rows a wave went through scratch memory: 284 us for a mixed call of 40 requests, 8 heads on
+// 4, against 141.)
 constexpr int prefill_split(int DP) { return DP == 256 ? 2 : 1; }
 constexpr int prefill_rows(int DP) { return 128 / prefill_split(DP); }
 
@@ -127,61 +127,24 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         }
         __syncthreads();
     }
-    // Workgroups b, b + 8, .. run on one die: it gets consecutive runs or tiles, since the
-    // tiles of a head share its keys in the L2.
+    // Workgroups b, b + 8, .. run on one die: it gets consecutive tiles, since the tiles of a
+    // head share its keys in the L2.
     const KvTileList list = *tiles.list;
-    const uint64_t all1 = list.all, all = all1 * a.H;  // of a head, and in all
-    const uint32_t die = blockIdx.x % kDies, nth = blockIdx.x / kDies;
-    uint32_t group = 0;
-    uint64_t run = 1, unit, end;
-    if (list.chunked) {
-        const uint64_t each = (all + kDies - 1) / kDies;
-        unit = die * each + nth;
-        end = nth < each && unit < all ? unit + 1 : unit;
-        if (blockIdx.x == 0)  // places of no tile
-            for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
-    } else {
-        run = kv_tile_run(cut, all);
-        if ((int)blockIdx.x >= cut.groups) return;
-        group = die * (cut.groups / kDies) + nth;
-        unit = group * run;
-        end = min(unit + run, all);
-        if (threadIdx.x == 0) joins[group].parts = joins[cut.groups + group].parts = 0;
-    }
-    int entry = -1;
-    while (unit < end) {
+    const uint32_t all1 = list.all, all = all1 * a.H;  // chunks of a head, and in all
+    const uint32_t each = (all + kDies - 1) / kDies, first = blockIdx.x % kDies * each;
+    if (blockIdx.x == 0)  // places of no tile
+        for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
+    for (uint32_t nth = blockIdx.x / kDies; nth < each && first + nth < all; nth += gridDim.x / kDies) {
+        const uint32_t unit = first + nth;
         const int h = (int)(unit / all1);
-        const uint64_t u1 = unit - h * all1;
-        // (a run goes on with the next tile, or the first one of the next head)
-        entry = entry < 0 ? __builtin_amdgcn_readfirstlane(kv_find(tiles.sums, list.count, u1)) : u1 ? entry + 1 : 0;
-        const KvTile rt = tiles.tiles[entry];
+        const uint32_t u1 = unit - h * all1;
+        const KvTile rt = tiles.tiles[__builtin_amdgcn_readfirstlane(kv_find(tiles.sums, list.count, u1))];
         const int r = rt.r, tile = rt.tile;
-        const int item_steps = rt.steps;
-        int step0 = (int)(u1 - rt.before), go, place;
-        if (list.chunked) {
-            const int chunks = rt.chunks;
-            const int each = (item_steps + chunks - 1) / chunks;
-            place = rt.part + list.parts * h + step0;
-            step0 *= each;
-            go = chunks == 1 ? item_steps : min(each, max(item_steps - step0, 0));
-            unit += 1;
-            if (chunks > 1 && threadIdx.x == 0) {
-                joins[place].parts = step0 == 0 ? chunks : 0;
-                joins[place].first = place;
-                joins[place].next = place + 1;
-                joins[place].stride = 1;
-            }
-        } else {
-            go = (int)min(end - unit, (uint64_t)(item_steps - step0));
-            unit += go;
-            place = kv_part(group, step0 == 0);
-            if (step0 == 0 && go < item_steps && threadIdx.x == 0) {
-                joins[group].parts = 1 + (int)((item_steps - go + run - 1) / run);
-                joins[group].first = place;
-                joins[group].next = kv_part(group + 1, false);
-                joins[group].stride = 2;
-            }
-        }
+        // steps of its own
+        const int chunk = (int)(u1 - rt.before), each_steps = (rt.steps + rt.chunks - 1) / rt.chunks;
+        const int step0 = chunk * each_steps, go = min(each_steps, max(rt.steps - step0, 0));
+        const int place = rt.part + list.parts * h + chunk;
+        const bool whole = rt.chunks == 1;
         const int first_token = rt.first_token;
         const int row0 = tile * Rows;
         const int rows = min(rt.n * a.G - row0, Rows);
@@ -509,7 +472,6 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         }
         l = sum_halves(l);
-        const bool whole = go >= item_steps;
         if (rw + n32 < rows) {
             const int64_t t = first_token + token;
             const int64_t at = (int64_t)place * Rows + rw + n32;
@@ -532,12 +494,16 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 else if (a.lse) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }
         }
-        if (!whole && step0 == 0 && threadIdx.x == 0) {
-            KvJoin &j = joins[list.chunked ? place : group];
+        if (!whole && threadIdx.x == 0) {
+            KvJoin &j = joins[place];
+            j.parts = chunk ? 0 : rt.chunks;
             j.first_token = first_token;
             j.row0 = row0;
             j.rows = rows;
             j.head = h;
+            j.first = place;
+            j.next = place + 1;
+            j.stride = 1;
         }
     }
 }

@@ -29,13 +29,14 @@ struct KvItem {
 };
 
 // Many rows a request: the tiles of all requests are listed first (their steps differ, as a
-// tile's keys end where its last row's do), a request's last tile, the longest, first.  With
-// few tiles the steps of the list, head by head, are dealt in equal runs in the same way;
-// with many, a workgroup takes a tile and the hardware deals them, longest first, since
-// beginning a tile takes as long as several steps and workgroups do not run at one speed
-// (a prompt of 8192 tokens, 64 heads on 8: equal runs of eight tiles ended after 1143 to
-// 1694 us).  There a tile of more than an equal share of the steps is cut into chunks.  So it
-// is where there are few steps: a workgroup then begins one tile and not several.
+// tile's keys end where its last row's do), a request's last tile, the longest, first.  A
+// workgroup takes a tile and the hardware deals them, longest first, since beginning a tile
+// takes as long as several steps and workgroups do not run at one speed.  A tile is cut into
+// as many chunks as it has equal shares of all steps, to the nearest: so one of up to 1.5
+// shares stays whole and no part of it is written or joined.  (Equal runs of steps, as above,
+// against this: a prompt of 8192 tokens, 64 heads on 8, 1546 against 1160 us; four prompts of
+// 2000 tokens, 32 heads on 8, 256 against %P4%; chunks of 512 tokens over 4000 to 8192, 281
+// against %CHUNK%.  Cut at one share, upwards, the last 320 us.)
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
@@ -188,26 +189,23 @@ __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, in
 
 // ---- many rows a request ------------------------------------------------------------
 
-constexpr int kFewSteps = 8;  // of a workgroup
-
 constexpr int kDies = 8;  // workgroups go to the dies (an L2 each) in turn
 
 struct KvTile {
     int r, tile;
     int n, ctx, first_token;  // of the request
     int steps;
-    int part;    // chunked: place of its first partial result, of head 0
-    int chunks;  // 1 if not chunked
-    uint64_t before;  // steps, or chunks, of the tiles before it
+    int part;    // place of its first partial result, of head 0
+    int chunks;  // 1: whole
+    uint32_t before;  // chunks of the tiles before it
 };
 struct KvTileList {  // (one load)
     int count;  // tiles
     int parts;  // partial results of a head
-    uint64_t all;  // steps, or chunks, of a head
-    int chunked;
+    uint32_t all;  // chunks of a head (fewer than 2^26 over all heads)
 };
 struct KvTiles {
-    const uint64_t *sums;  // [count + 1] exclusive sums of the tiles' steps, or chunks
+    const uint32_t *sums;  // [count + 1] exclusive sums of the tiles' chunks
     const KvTile *tiles;   // [count]
     const KvTileList *list;
 };
@@ -223,8 +221,10 @@ __device__ __forceinline__ uint32_t kv_tile_steps(const KvAttnArgs &a, const KvS
     return (uint32_t)max((hi - lo + keys - 1) / keys, 1);
 }
 
-// Steps a workgroup: a part of a tile costs about as much as two steps to write and join.
-__device__ __forceinline__ uint64_t kv_tile_run(const KvCut &c, uint64_t all)
+// An equal share of `all` steps, not below four: a part of a tile costs about as much as two
+// steps to write and join (64 tokens of 8 heads over 8000 keys: 49 us, and 65 with shares down
+// to one step).
+__device__ __forceinline__ uint64_t kv_tile_share(const KvCut &c, uint64_t all)
 {
     return max((all + (uint32_t)c.groups - 1) / (uint32_t)c.groups, (uint64_t)4);
 }
