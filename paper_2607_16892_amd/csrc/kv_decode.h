@@ -36,7 +36,6 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
     constexpr int KWords = F8 ? S * 2 : S * 4;   // dwords a lane reads of a key row
     constexpr int VWords = F8 ? VW / 4 : VW / 2; // and of a value row
     constexpr bool AHEAD = DP * E <= 256;  // keys of the next step fit beside this one's values
-    __shared__ float weights[kStepKeys * kDecodeRows];
     __shared__ KvLds lds;
 
     const int lane = threadIdx.x, n16 = lane & 15, grp = lane >> 4;
@@ -100,6 +99,7 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
         // Steps: keys k0 + 32 u.  A lane holds the block of one group of 16 keys, 32 steps ahead.
         const int steps = (k1 - k0 + kStepKeys - 1) / kStepKeys;
         int ids = 0;
+        bool found = false;  // infinities or NaN among values that only some rows see
         auto fetch_ids = [&](int u) {
             const int key = k0 + (u + (lane >> 1)) * kStepKeys + (lane & 1) * 16;
             ids = min(max(table[min(key, k1 - 1) >> a.shift], 0), a.num_blocks - 1);
@@ -232,8 +232,8 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
 
             if (edge) {
                 // a weight of zero does not silence an infinity or a NaN: values that no row of
-                // the tile sees become zero, and those that some see are added apart, to these
-                // rows alone
+                // the tile sees become zero, and those that some see are added after the last
+                // step, to these rows alone
                 uint32_t odd = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -246,33 +246,11 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
                     }
                 }
                 if (__any(odd)) {
+                    found = true;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int x = (i >> 2) * 16 + grp * 4 + (i & 3);
-                        const bool seen = key0 + x >= see.lo && key0 + x < see.hi;
-                        weights[x * 16 + n16] = seen ? e[i] : -1.0f;
+                    for (int i = 0; i < 8; ++i)
 #pragma unroll
                         for (int j = 0; j < VWords; ++j) v[i].w[j] &= ~nonfinite_mask<C>(v[i].w[j]);
-                    }
-                    for (int x = 0; x < kStepKeys; ++x) {
-                        const float wt = weights[x * 16 + n16];
-                        const bool seen = !(wt < 0.0f);  // by this lane's row (NaN: seen)
-                        const int key = min(key0 + x, k1 - 1);
-                        const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
-                        const char *at = vp + (id * a.v_block + (int64_t)(key & in_block) * a.v_token) * E;
-                        int D = a.D;
-                        asm volatile("" : "+s"(D));  // compared with anew: 32 addresses would not fit
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-#pragma unroll
-                            for (int j = 0; j < VW; ++j) {
-                                const int d = VW * (grp * 4 + c) + j;
-                                const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
-                                o[j][c] += seen && !__builtin_isfinite(y) ? wt * y : 0.0f;
-                                __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
-                            }
-                        }
-                    }
                 }
             }
             // V^T: dword y of column j holds rows 2y and 2y + 1
@@ -306,6 +284,27 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
             }
         }
 
+        if (found) {
+            // whatever its weight, an infinity stays one, and a NaN
+            for (int key = k0; key < k1; ++key) {
+                const int step = k0 + ((key - k0) & ~(kStepKeys - 1));
+                if (step >= all_lo && step + kStepKeys <= min(all_hi, k1)) continue;  // not zeroed
+                const bool seen = key >= see.lo && key < see.hi;
+                const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
+                const char *at = vp + (id * a.v_block + (int64_t)(key & in_block) * a.v_token) * E;
+                int D = a.D;
+                asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < VW; ++j) {
+                        const int d = VW * (grp * 4 + c) + j;
+                        const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
+                        if (seen && !__builtin_isfinite(y)) o[j][c] += y;
+                        __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
+                    }
+            }
+        }
         l = sum_groups(l);
         const bool whole = go >= it.steps;
         if (n16 < rows) {

@@ -32,7 +32,7 @@ struct KvItem {
 // tile's keys end where its last row's do), a request's last tile, the longest, first.  A
 // workgroup takes a tile and the hardware deals them, longest first, since beginning a tile
 // takes as long as several steps and workgroups do not run at one speed.  A tile is cut into
-// as many chunks as it has equal shares of all steps, to the nearest: so one of up to 1.5
+// as many chunks as it has equal shares of all steps, a quarter aside: so one of less than 1.75
 // shares stays whole and no part of it is written or joined.  (Equal runs of steps, as above,
 // against this: a prompt of 8192 tokens, 64 heads on 8, 1546 against 1160 us; four prompts of
 // 2000 tokens, 32 heads on 8, 256 against %P4%; chunks of 512 tokens over 4000 to 8192, 281
