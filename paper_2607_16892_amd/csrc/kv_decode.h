@@ -10,7 +10,7 @@
 // transpose of 8 rows x 16 bytes inside each lane.  A workgroup is one wave with its own
 // run of steps: while one begins or ends an item, the other seven of the compute unit
 // read on.  (Four waves that shared a run and met in LDS after each item: 124 us for 64
-// requests of 50 to 8192 keys on 8 heads, 464 MB, against %RAGGED% now.)
+// requests of 50 to 8192 keys on 8 heads, 464 MB, against 103 now.)
 #pragma once
 
 #include "kv_math.h"

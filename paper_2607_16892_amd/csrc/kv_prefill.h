@@ -127,17 +127,19 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         }
         __syncthreads();
     }
-    // Workgroups b, b + 8, .. run on one die: it gets consecutive tiles, since the tiles of a
-    // head share its keys in the L2.
+    // Workgroups b, b + 8, .. run on one die.  It gets whole heads where their number allows, one
+    // after the other, since the tiles of a head share its keys in the L2; else the heads take
+    // turns, which with 1, 2 or 4 gives a die one head as well.
     const KvTileList list = *tiles.list;
     const uint32_t all1 = list.all, all = all1 * a.H;  // chunks of a head, and in all
-    const uint32_t each = (all + kDies - 1) / kDies, first = blockIdx.x % kDies * each;
+    const bool by_head = a.H % kDies == 0;
     if (blockIdx.x == 0)  // places of no tile
         for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
-    for (uint32_t nth = blockIdx.x / kDies; nth < each && first + nth < all; nth += gridDim.x / kDies) {
-        const uint32_t unit = first + nth;
-        const int h = (int)(unit / all1);
-        const uint32_t u1 = unit - h * all1;
+    for (uint32_t unit = blockIdx.x; unit < all; unit += gridDim.x) {
+        const uint32_t nth = unit / kDies, per = by_head ? all1 : (uint32_t)a.H, quot = (by_head ? nth : unit) / per,
+                       rest = (by_head ? nth : unit) - quot * per;
+        const int h = by_head ? unit % kDies * (a.H / kDies) + quot : rest;
+        const uint32_t u1 = by_head ? rest : quot;
         const KvTile rt = tiles.tiles[__builtin_amdgcn_readfirstlane(kv_find(tiles.sums, list.count, u1))];
         const int r = rt.r, tile = rt.tile;
         // steps of its own

@@ -35,8 +35,8 @@ struct KvItem {
 // as many chunks as it has equal shares of all steps, a quarter aside: so one of less than 1.75
 // shares stays whole and no part of it is written or joined.  (Equal runs of steps, as above,
 // against this: a prompt of 8192 tokens, 64 heads on 8, 1546 against 1160 us; four prompts of
-// 2000 tokens, 32 heads on 8, 256 against %P4%; chunks of 512 tokens over 4000 to 8192, 281
-// against %CHUNK%.  Cut at one share, upwards, the last 320 us.)
+// 2000 tokens, 32 heads on 8, 256 against 168; four chunks of 512 tokens over 4000 to 8192, 281
+// against 244, and 320 with every tile of more than one share cut.)
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {

@@ -421,3 +421,50 @@ def test_a_bound_that_does_not_hold_loses_no_request(ctx, dev):
     c = Case(dev, [400, 90, 7], [1, 300, 7], 8, 2, 128, seed=12)
     for most in (1, 5, 100, 150, 299):
         c.check(c.run(ctx, max_new=most))
+
+
+@pytest.mark.parametrize("Hq,H,D,lens,new", [
+    (8, 1, 64, [300 + i % 7 for i in range(61)], [300] * 61),             # more tiles than a pass lists
+    (24, 12, 64, [1500, 40, 900, 2100], [1500, 40, 900, 700]),            # heads that no die has whole
+    (10, 5, 128, [700, 3000, 90, 5], [300, 64, 90, 1]),
+    (32, 16, 80, [2500, 800, 33], [65, 800, 33]),
+    (16, 8, 256, [4000, 100, 2000, 900, 1], [50, 9, 33, 60, 1]),          # a tile each, of unequal length
+    (16, 2, 128, [60 + 31 * i % 900 for i in range(70)],                  # both kernels
+     [1 if i % 7 else min(100, 60 + 31 * i % 900) for i in range(70)]),
+    (64, 8, 128, [500 + 17 * i for i in range(70)], [3] * 70),
+])
+def test_orders_of_tiles(ctx, dev, Hq, H, D, lens, new):
+    """Tiles listed longest first, dealt to the dies by heads or in turn, cut and whole: rows of
+    every request against fp64 (bounds as in test_many_tiles)."""
+    import torch
+    from kv_cases import UNIT
+    print(f"[gpu] kv orders Hq={Hq} H={H} D={D} requests {len(lens)}", flush=True)
+    c = Case(dev, lens, new, Hq, H, D, "bf16", seed=Hq + D)
+    got = c.run(ctx)
+    for r in range(0, len(lens), 1 + len(lens) // 12):
+        n, a = new[r], int(c.start[r])
+        rows = sorted({0, n // 2, n - 1})
+        out, lse, mass = _reference(c, r, rows)
+        err = (got["out"][a:a + n][rows].double() - out).abs()
+        tol = (2 * UNIT["bf16"] + 2.0 ** -17) * mass + lens[r] * 2.0 ** -25 * 8 + 2.0 ** -24
+        assert (err <= tol).all(), f"request {r}: {(err / tol).max().item():.3g} of the bound"
+        assert ((got["lse"][a:a + n][rows].double() - lse).abs() <= 2.0 ** -16 * (1 + lse.abs())).all()
+
+
+@pytest.mark.parametrize("lens,new", [([20_000, 70], [40, 70]), ([20_000], [1]), ([300, 300], [90, 1])])
+def test_infinities_in_long_and_cut_requests(ctx, dev, lens, new):
+    """An infinity and a NaN in the last token of a request: its last row alone has them, in
+    their components, whether the request is whole or cut."""
+    import torch
+    c = Case(dev, lens, new, 4, 2, 128, "bf16", seed=21)
+    ref = c.run(ctx)
+    L = lens[0]
+    b = int(c.table_h[0, (L - 1) // 16])
+    c.v[b, (L - 1) % 16, 0, 5] = float("inf")
+    c.v[b, (L - 1) % 16, 1, 9] = float("nan")
+    got = c.run(ctx)
+    hit = torch.zeros_like(ref["out"], dtype=torch.bool)
+    hit[new[0] - 1, :2, 5] = True
+    hit[new[0] - 1, 2:, 9] = True
+    assert not torch.isfinite(got["out"][hit]).any()
+    assert torch.equal(got["out"][~hit], ref["out"][~hit]) and torch.equal(got["lse"], ref["lse"])
