@@ -20,14 +20,12 @@ static __device__ uint64_t plan_scan(uint64_t x, uint64_t *part, uint64_t &total
     x = scan_wave(x);
     if (lane == 63) part[wave] = x;
     __syncthreads();
-    uint64_t before = 0;
-    total = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        if (w < wave) before += part[w];
-        total += part[w];
-    }
+    static_assert(kPlanThreads / 64 == 16, "a row of lanes");
+    const uint64_t waves = scan_row16(lane < 16 ? part[lane] : 0);  // the waves' sums, one a lane
+    total = lane_value(waves, 15);
+    if (wave) x += lane_value(waves, __builtin_amdgcn_readfirstlane(wave) - 1);
     __syncthreads();
-    return before + x;
+    return x;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs a, const KvCut cut, uint64_t *sums)
@@ -53,14 +51,26 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
 {
     __shared__ uint64_t part[kPlanThreads / 64];
     __shared__ uint32_t steps_at[kPlanThreads];
+    __shared__ uint32_t before_lds[kPlanThreads];  // up to a request a thread: a search in LDS
+    __shared__ KvShare share_lds[kPlanThreads];
+    const bool lds = a.R <= kPlanThreads;
     const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
     const int r0 = min((int)threadIdx.x * per, a.R), r1 = min(r0 + per, a.R);
     uint64_t own = 0, total;
-    for (int r = r0; r < r1; ++r) own += kv_share(a, cut, r).tiles;
-    uint64_t at = plan_scan(own, part, total) - own;
+    KvShare s0{};
     for (int r = r0; r < r1; ++r) {
-        before[r] = at;
-        at += kv_share(a, cut, r).tiles;
+        s0 = kv_share(a, cut, r);
+        own += s0.tiles;
+    }
+    uint64_t at = plan_scan(own, part, total) - own;
+    if (lds) {
+        before_lds[threadIdx.x] = (uint32_t)min(at, (uint64_t)0xffffffff);
+        share_lds[threadIdx.x] = s0;
+    } else {
+        for (int r = r0; r < r1; ++r) {
+            before[r] = at;
+            at += kv_share(a, cut, r).tiles;
+        }
     }
     __syncthreads();  // (makes `before` visible to the workgroup)
     const int n = (int)min(total, (uint64_t)most);
@@ -73,11 +83,11 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
             int lo = 0, hi = a.R;  // the last request with before[r] <= e: it has tiles
             while (hi - lo > 1) {
                 const int m = (lo + hi) >> 1;
-                if (before[m] <= (uint64_t)e) lo = m;
+                if ((lds ? before_lds[m] : before[m]) <= (uint64_t)e) lo = m;
                 else hi = m;
             }
-            const KvShare s = kv_share(a, cut, lo);
-            const int tile = max(s.tiles - 1 - (e - (int)before[lo]), 0);
+            const KvShare s = lds ? share_lds[lo] : kv_share(a, cut, lo);
+            const int tile = max(s.tiles - 1 - (e - (int)(lds ? before_lds[lo] : before[lo])), 0);
             steps = kv_tile_steps(a, s, lo, tile, cut.rows, keys);
             mine = KvTile{lo, tile, s.n, s.ctx, min(max(a.start[lo], 0), a.T), (int)steps, 0, 1, 0};
             tiles[e] = mine;
@@ -343,13 +353,14 @@ size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype)
 template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, int entries, int most_tiles, const KvWork &w, int DP,
                         hipStream_t st)
 {
-    // A few items may have many parts and are few among the entries: eight waves to a row, 32
-    // entries a workgroup.  Else a workgroup to an entry and as many rows as it joins at once.
-    // (Sixteen waves: a join of 30 us, the call 44; eight: the call 27, for 32 requests of 1000
-    // to 8000 keys, two tokens of eight heads to one key head of 64 components each.)
+    // Items so few that each may have more than 64 parts are few among the entries too: eight waves
+    // to a row, 32 entries a workgroup.  Else a workgroup to an entry or four and as many rows as
+    // it joins at once.  (Sixteen waves: a join of 30 us, the call 44; eight: the call 27,
+    // for 32 requests of 1000 to 8000 keys, two tokens of eight heads to one key head of 64
+    // components each.)
     const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));
     const int64_t items = (c.rows == 16 ? (int64_t)a.R : (int64_t)most_tiles) * a.H;
-    const bool few = items <= 64;
+    const bool few = items * 64 <= c.groups;
     const unsigned at_once = 4 * (256 / DP);  // rows of four waves
     const unsigned rows = (most + at_once - 1) / at_once;
     auto pick = [&](auto waves, auto per, unsigned y) {
