@@ -40,12 +40,17 @@ __global__ __launch_bounds__(64, decode_waves(DP * (int)sizeof(C))) void kv_deco
 
     const int lane = threadIdx.x, n16 = lane & 15, grp = lane >> 4;
 
-    if (pad) zero_rows<T>(a);
     KvSched sched;
     sched.init(a, cut, sums, lds);
     if (threadIdx.x == 0) joins[blockIdx.x].parts = 0;
     uint64_t unit = blockIdx.x * sched.run;
     const uint64_t end = min(unit + sched.run, sched.all);
+    if (pad && (gridDim.x - 1) * sched.run < sched.all) {
+        zero_rows<T>(a, blockIdx.x, gridDim.x);
+    } else if (pad && unit >= end) {
+        const uint32_t busy = (uint32_t)((sched.all + sched.run - 1) / sched.run);
+        zero_rows<T>(a, blockIdx.x - busy, gridDim.x - busy);
+    }
     while (unit < end) {
         const KvItem it = sched.item(a, cut, sums, lds, unit);
         const int go = (int)min(end - unit, (uint64_t)(it.steps - it.step));  // steps of this item

@@ -100,12 +100,14 @@ template <int N> __device__ __forceinline__ Words<N> load_words(const char *base
     return x;
 }
 
-// The rows of no request, by all workgroups.
-template <class T> __device__ __forceinline__ void zero_rows(const KvAttnArgs &a)
+// The rows of no request, by workgroup `nth` of `of`: those without other work, where there are
+// any, since the others' way to their first keys is a chain of loads already.
+template <class T> __device__ __forceinline__ void zero_rows(const KvAttnArgs &a, uint32_t nth, uint32_t of)
 {
     const int t0 = min(max(a.start[0], 0), a.T), t1 = min(max(a.start[a.R], 0), a.T);
     const int lost = t0 + a.T - t1;
-    for (int x = blockIdx.x; x < lost; x += gridDim.x) {
+    for (uint32_t y = nth; y < (uint32_t)lost; y += of) {
+        const int x = (int)y;
         const int t = x < t0 ? x : t1 + x - t0;
         for (int i = threadIdx.x; i < a.Hq * a.D; i += blockDim.x) {
             const int h = i / a.D;

@@ -116,7 +116,6 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n32 = lane & 31, half = lane >> 5;
     const int rw = wave % (4 / DS) * 32, dt0 = wave / (4 / DS) * ND;  // rows and component tiles from there on
-    if (pad) zero_rows<T>(a);
     if (!FULL) {  // pieces beyond the rows' ends are never written
         for (int i = threadIdx.x; i < Tile / 16; i += 256) {
             const u32x4 zero = {0, 0, 0, 0};
@@ -133,6 +132,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     const KvTileList list = *tiles.list;
     const uint32_t all1 = list.all, all = all1 * a.H;  // chunks of a head, and in all
     const bool by_head = a.H % kDies == 0;
+    if (pad && gridDim.x <= all) zero_rows<T>(a, blockIdx.x, gridDim.x);
+    else if (pad && blockIdx.x >= all) zero_rows<T>(a, blockIdx.x - all, gridDim.x - all);
     if (blockIdx.x == 0)  // places of no tile
         for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
     for (uint32_t unit = blockIdx.x; unit < all; unit += gridDim.x) {

@@ -432,6 +432,7 @@ def test_a_bound_that_does_not_hold_loses_no_request(ctx, dev):
     (16, 2, 128, [60 + 31 * i % 900 for i in range(70)],                  # both kernels
      [1 if i % 7 else min(100, 60 + 31 * i % 900) for i in range(70)]),
     (64, 8, 128, [500 + 17 * i for i in range(70)], [3] * 70),
+    (4, 2, 64, [90 + i % 9 for i in range(1100)], [60 if i % 92 == 0 else 1 for i in range(1100)]),  # a list in passes
 ])
 def test_orders_of_tiles(ctx, dev, Hq, H, D, lens, new):
     """Tiles listed longest first, dealt to the dies by heads or in turn, cut and whole: rows of
