@@ -93,6 +93,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 {
     constexpr int E = sizeof(C);
     constexpr bool F8 = E == 1;
+    constexpr bool LEAN = MODS || F8 || DP == 256;  // places in LDS and memory are not kept over the steps
     constexpr int KT = prefill_keys(DP);
     constexpr int S = DP / 16;           // steps of 16 components of a score
     // keys whose scores are in registers at once: 128 beside the changes of the scores spill
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         Words<2> reg[F8 ? UP * IP : 1];
         auto load = [&](auto odd_tile, int u) {
             int lane = threadIdx.x & 63;
-            asm volatile("" : "+v"(lane));  // (see `fresh`)
+            if constexpr (LEAN) asm volatile("" : "+v"(lane));  // (see `fresh`)
 #pragma unroll
             for (int j = 0; j < UP; ++j) {
                 const bool vals = (wave + 4 * j) / NG;
@@ -255,8 +256,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         };
         // Where a lane reads, for piece 0 of the keys and of the values; the others follow by an
-        // exclusive or and an offset.  Each step computes them anew: kept over the steps they take
-        // the registers of the queries, which then come back from memory behind the tile on its way.
+        // exclusive or and an offset.  Where registers are short (LEAN) each step computes them
+        // anew: kept over the steps they take the registers of the queries, which then come back
+        // from memory behind the tile on its way.
         auto key_place = [&](int lane) {
             return (uint32_t)((lane & 31) * Row + ((lane >> 5) ^ key_turn<DP>(lane & 31)) * 16);
         };
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 // pieces of the keys and of the values are read kAheadOf products before their
                 // use, the first of the values before the softmax
                 int fresh = lane;
-                asm volatile("" : "+v"(fresh));
+                if constexpr (LEAN) asm volatile("" : "+v"(fresh));
                 const uint32_t k_at = key_place(fresh), v_at = value_place(fresh);
                 auto key_frag = [&](int f) {
                     return *(const u32x4 *)&sk[(k_at ^ (f % S * 32)) + (sub + f / S * 32) * Row];
