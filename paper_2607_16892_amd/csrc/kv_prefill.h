@@ -48,21 +48,29 @@ template <class T> __device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f3
                                                       __builtin_bit_cast(Vec<f16, 8>, y), c, 0, 0, 0);
 }
 
+// The larger, a NaN aside.  (fmaxf first quiets operands that a matrix product made, an
+// operation each; the median with infinity does not.)
+__device__ __forceinline__ float max_raw(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
 __device__ __forceinline__ float max_halves(float x)
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
     auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    return max_raw(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
-// The larger, a NaN aside.  (fmaxf first quiets operands that a matrix product made, an
-// operation each; the median with infinity does not.)
-__device__ __forceinline__ float max_raw(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
-__device__ __forceinline__ float max_of(const f32x16 &x)
+template <int N> __device__ __forceinline__ float max_of(const f32x16 (&x)[N])
 {
-    float m[4] = {x[0], x[1], x[2], x[3]};
+    // four chains of steps that take two values each
+    float m[4];
 #pragma unroll
-    for (int i = 4; i < 16; ++i) m[i & 3] = max_raw(m[i & 3], x[i]);
-    return max_raw(max_raw(m[0], m[1]), max_raw(m[2], m[3]));
+    for (int c = 0; c < 4; ++c) {
+        m[c] = x[0][c];
+#pragma unroll
+        for (int i = 4; i < N * 16; i += 8) {
+            m[c] = max_raw(m[c], x[i / 16][i % 16 + c]);
+            if (i + 4 < N * 16) m[c] = max_raw(m[c], x[(i + 4) / 16][(i + 4) % 16 + c]);
+        }
+    }
+    return max_raw(max_raw(max_raw(m[0], m[1]), m[2]), m[3]);
 }
 
 __device__ __forceinline__ float sum_halves(float x)
@@ -405,9 +413,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                             s[t][i] = x;
                         }
                 }
-                float mt = max_of(s[0]);
-#pragma unroll
-                for (int t = 1; t < NT; ++t) mt = max_raw(mt, max_of(s[t]));
+                float mt = max_of(s);
                 const float by = MODS ? 1.0f : to_exp;
                 mt *= by;
                 mt = max_halves(mt);
