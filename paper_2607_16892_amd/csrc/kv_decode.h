@@ -10,7 +10,8 @@
 // transpose of 8 rows x 16 bytes inside each lane.  A workgroup is one wave with its own
 // run of steps: while one begins or ends an item, the other seven of the compute unit
 // read on.  (Four waves that shared a run and met in LDS after each item: 124 us for 64
-// requests of 50 to 8192 keys on 8 heads, 464 MB, against 103 now.)
+// requests of 50 to 8192 keys on 8 heads, 464 MB, against 101 now: 4.8 TB/s in
+// the kernel, and 5.3 from 128 requests of 1000 to 16,384 keys in 8 bits.)
 #pragma once
 
 #include "kv_math.h"

@@ -14,7 +14,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // Running maxima are raised only when a step exceeds them by 2^kSlack, so most steps
-// rescale nothing; weights stay below 2^kSlack.
+// rescale nothing; weights stay below 2^kSlack.  (With 0 a prompt of 8192 tokens, 64 heads on 8,
+// takes 1250 us where 8 takes 1168.)
 constexpr float kSlack = 8.0f;
 
 // 16 x 16 tile over 32 products.  First operand: lane holds row lane % 16, products

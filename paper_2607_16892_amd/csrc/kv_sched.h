@@ -5,7 +5,7 @@
 //
 // Few rows a request: a step is 32 keys of an item, and the steps of all items in order
 // are dealt to `groups` workgroups in equal runs, so requests of any lengths load them
-// alike.  A run that holds a whole item writes its rows; a run that begins or ends within
+// alike (few rows are bound by what they read, whoever reads it).  A run that holds a whole item writes its rows; a run that begins or ends within
 // an item leaves a partial result, at most two a workgroup, for the join.
 #pragma once
 
@@ -75,7 +75,9 @@ __device__ __forceinline__ uint64_t kv_units(const KvAttnArgs &a, const KvShare 
 }
 
 // steps a workgroup, for `all` steps, the longest of the wave's items having `longest`.  An
-// item of many steps alone would be cut so fine that the join takes longer than the steps.
+// item of many steps alone would be cut so fine that the join takes longer than the steps (one
+// request of 131,000 keys, 8 heads on one: 82 us with runs of two steps, 35 with eight; of
+// 16,000: 27 with one, 19 with two).
 __device__ __forceinline__ uint64_t kv_run(const KvCut &c, uint64_t all, uint32_t longest)
 {
     const uint64_t least = __any(longest >= 2048) ? 8 : __any(longest >= 512) ? 4 : __any(longest >= 128) ? 2 : 1;

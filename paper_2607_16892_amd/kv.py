@@ -192,7 +192,7 @@ def kv_block_tables(ctx: Context, pool: BlockPool, length: torch.Tensor, add: to
                                         ("start", R + 1, i32), ("pos", T, i32),
                                         ("slot", T, torch.int64), ("granted", R, torch.uint8))}
         else:  # one buffer for the 32-bit ones
-            parts = torch.empty(3 * R + 2 + T, dtype=i32, device=dev).split((R, 1, R, R + 1, T))
+            parts = torch.empty(3 * R + 2 + T, dtype=i32, device=dev).split_with_sizes((R, 1, R, R + 1, T))
             o = dict(zip(("held", "free", "context", "start", "pos"), parts))
             o["slot"] = torch.empty(T, dtype=torch.int64, device=dev)
             o["granted"] = torch.empty(R, dtype=torch.uint8, device=dev)
