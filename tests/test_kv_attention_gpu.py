@@ -171,6 +171,24 @@ def test_table_entries_outside_the_pool_are_not_followed(ctx, dev):
 
 
 @pytest.mark.parametrize("new", [1, 30])
+def test_starts_outside_the_rows_are_cut(ctx, dev, new):
+    """Starts below 0 and beyond T count as 0 and T; requests whose end is not behind their start
+    have no rows."""
+    import torch
+    c = Case(dev, [50, 60, 70], [new] * 3, 4, 2, 128, seed=2)
+    ref = c.run(ctx)
+    c.start = torch.tensor([-7, new, 2 * new, 2 ** 31 - 1], dtype=torch.int32, device=dev)
+    got = c.run(ctx)
+    assert torch.equal(got["out"], ref["out"]) and torch.equal(got["lse"], ref["lse"])
+    c.start = torch.tensor([0, new, new - 1, 3 * new], dtype=torch.int32, device=dev)
+    got = c.run(ctx)
+    assert torch.equal(got["out"][:new - 1], ref["out"][:new - 1])
+    c.start = torch.tensor([2 ** 31 - 1, -2 ** 31, 5, 0], dtype=torch.int32, device=dev)
+    c.run(ctx)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("new", [1, 30])
 def test_rows_of_no_request_are_zero(ctx, dev, new):
     import torch
     c = Case(dev, [50, 60], [new, new], 4, 2, 128, seed=2)
