@@ -297,6 +297,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
                 const bool seen = key >= see.lo && key < see.hi;
                 const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
                 const char *at = vp + (id * a.v_block + (int64_t)(key & in_block) * a.v_token) * E;
+                if (!row_nonfinite<C>(at, a.D * E)) continue;
                 int D = a.D;
                 asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
 #pragma unroll

@@ -74,6 +74,14 @@ template <class C> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w
         return ((((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15) * 0xffffu;
 }
 
+// Whether the `bytes` (a multiple of 4) of a value row at `p` hold an infinity or a NaN; by a wave.
+template <class C> __device__ __forceinline__ bool row_nonfinite(const char *p, int bytes)
+{
+    uint32_t bad = 0;
+    for (int i = (threadIdx.x & 63) * 4; i < bytes; i += 256) bad |= nonfinite_mask<C>(*(const uint32_t *)(p + i));
+    return __any(bad);
+}
+
 // N dwords at base + off, aligned to 8 elements of the cache's type: the base is the same
 // for the wave, so an address costs no 64-bit vector arithmetic.
 template <int N> struct Words {

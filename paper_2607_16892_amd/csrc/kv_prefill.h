@@ -324,16 +324,17 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             // added after the last step, to the rows that see them.
             const bool mixed = tile0 < bot.lo || tile0 + KT > top.hi;
             if (mixed) {
-                uint32_t bad = 0;
+                bool bad = false;
                 for (int i = threadIdx.x; i < Tile / 16; i += 256) {
                     u32x4 &y = ((u32x4 *)sv)[i];
                     u32x4 mask;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        mask[c] = nonfinite_mask<T>(y[c]);
-                        bad |= mask[c];
+                    for (int c = 0; c < 4; ++c) mask[c] = nonfinite_mask<T>(y[c]);
+                    if (mask[0] | mask[1] | mask[2] | mask[3]) {
+                        y &= ~mask;
+                        const int key = tile0 + i / NC;
+                        bad |= key >= top.lo && key < k1;  // (what no row sees may hold anything)
                     }
-                    if (mask[0] | mask[1] | mask[2] | mask[3]) y &= ~mask;
                 }
                 if (bad) found = 1;
                 __syncthreads();
@@ -473,6 +474,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
                 const char *at = (const char *)a.v +
                                  (id * a.v_block + (int64_t)(key & in_block) * a.v_token + (int64_t)h * a.v_head) * E;
+                if (!row_nonfinite<C>(at, a.D * E)) continue;
                 int D = a.D;
                 asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
 #pragma unroll
