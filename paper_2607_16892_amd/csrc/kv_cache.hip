@@ -21,8 +21,7 @@ namespace dro {
 
 struct KvRequest {
     long long n, after;
-    int held, blocks, back;
-    long long grow;
+    int held, blocks, back, grow;
     bool live;
 };
 
@@ -42,9 +41,11 @@ static __device__ __forceinline__ KvRequest kv_request(const KvTablesArgs &a, in
     return q;
 }
 
-// Inclusive sums over the workgroup's threads; `total` holds the last one's.
+// Inclusive sums over the workgroup's threads; `total` holds the last one's.  (Blocks: the tables
+// have fewer than 2^31 entries.)
 struct KvSums {
-    uint64_t n, back, grow;
+    uint64_t n;
+    uint32_t back, grow;
 };
 template <int THREADS> static __device__ KvSums scan_threads(KvSums x, KvSums *part, KvSums &total)
 {
@@ -58,7 +59,8 @@ template <int THREADS> static __device__ KvSums scan_threads(KvSums x, KvSums *p
     static_assert(THREADS / 64 <= 16, "a row of lanes");
     KvSums p{0, 0, 0};
     if (lane < THREADS / 64) p = part[lane];
-    const uint64_t n = scan_row16(p.n), back = scan_row16(p.back), grow = scan_row16(p.grow);
+    const uint64_t n = scan_row16(p.n);
+    const uint32_t back = scan_row16(p.back), grow = scan_row16(p.grow);
     total = KvSums{lane_value(n, 15), lane_value(back, 15), lane_value(grow, 15)};
     if (wave) {
         const int w = __builtin_amdgcn_readfirstlane(wave) - 1;
