@@ -513,7 +513,8 @@ int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, 
  * they hold.  Rows of no request (t outside [start[0], start[R])) are zero with
  * lse -infinity.  Products, sums and the softmax are kept in fp32 (the cap's tanh
  * to 2^-21 of the cap); the weights are rounded to q's type for the product with
- * the values.  Two calls with the same arguments give the same bits.
+ * the values (in f16 to within 2^-32 of the row's largest where they are small).
+ * Two calls with the same arguments give the same bits.
  * max_new bounds the rows of one request and picks the kernels (a larger request
  * is computed all the same). */
 typedef struct {

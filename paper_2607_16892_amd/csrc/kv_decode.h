@@ -219,8 +219,8 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             }
             float mt = fmaxf(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])), fmaxf(fmaxf(e[4], e[5]), fmaxf(e[6], e[7])));
             mt = max_groups(mt);
-            if (__any(mt > m + kSlack)) {
-                const float to = fmaxf(m, mt);
+            if (__any(has_to_raise<T>(mt, m))) {
+                const float to = fmaxf(m, mt - kUnit<T>);
                 const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
                 m = to;
                 l *= f;

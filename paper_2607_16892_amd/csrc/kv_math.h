@@ -14,9 +14,23 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // Running maxima are raised only when a step exceeds them by 2^kSlack, so most steps
-// rescale nothing; weights stay below 2^kSlack.  (With 0 a prompt of 8192 tokens, 64 heads on 8,
-// takes 1250 us where 8 takes 1168.)
+// rescale nothing; weights stay below 2^kSlack of that maximum's.  (With 0 a prompt of 8192 tokens,
+// 64 heads on 8, takes 1250 us where 8 takes 1168.)
 constexpr float kSlack = 8.0f;
+
+// The running maximum m is held 2^kUnit below the largest score, so the largest weight of a row is
+// 2^kUnit at least.  f16 weights are products' operands in f16, which ends at 2^-24: with a unit of
+// 1 those below 2^-25 of the largest were lost, 1.4 % of the tail of 131,072 keys that lie 14.5
+// below the first one's score.  With 2^7 the end is 2^-32 of the largest, and 2^(7 + kSlack) leaves
+// an octave below f16's largest number.
+template <class T> constexpr float kUnit = __is_same(T, f16) ? 7.0f : 0.0f;
+
+// Whether a step of scores up to `mt` has to raise m.  f16: where the scores' last places are half
+// an octave and more, always, so that the weights stay in range.
+template <class T> __device__ __forceinline__ bool has_to_raise(float mt, float m)
+{
+    return mt > m + (kSlack + kUnit<T>) || (__is_same(T, f16) && fabsf(mt) >= 0x1p23f);
+}
 
 // 16 x 16 tile over 32 products.  First operand: lane holds row lane % 16, products
 // (lane / 16) 8 .. + 8; second: column lane % 16, the same products; result: column

@@ -422,8 +422,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const float by = MODS ? 1.0f : to_exp;
                 mt *= by;
                 mt = max_halves(mt);
-                if (__any(mt > m + kSlack)) {
-                    const float to = fmaxf(m, mt);
+                if (__any(has_to_raise<T>(mt, m))) {
+                    const float to = fmaxf(m, mt - kUnit<T>);
                     const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
                     m = to;
                     l *= f;
