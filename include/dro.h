@@ -48,8 +48,10 @@
  *    are then: after any call on that ctx with another problem or on another
  *    stream, capture again.  (dro_cost_eval_noalloc has no such bond to its ctx.)
  *    kv_block_tables, kv_store and kv_attention enqueue kernels only as well, once
- *    the workspace is as large as they need: a replay stays right until a call on
- *    that ctx needs a larger one.
+ *    a call on the ctx has needed as large a workspace (one that has to grow it under
+ *    capture is DRO_EHIP and enqueues nothing).  The workspace that a captured
+ *    call was given stays until dro_destroy, whatever later calls need, so their
+ *    replays stay right.
  *  - Exactness limits (DRO_ELIMIT when exceeded): 0 <= x, eta <= L <= 2^15,
  *    N_c <= 2^26 samples per class, every lam, c_p, c_w in [2^-10, 2^7];
  *    K <= 2^15 + 1 grid points, M <= 65536 multipliers, K * M < 2^31 pairs,

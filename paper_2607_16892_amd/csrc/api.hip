@@ -421,7 +421,7 @@ void dro_destroy(dro_ctx *ctx)
     if (!ctx) return;
     DeviceGuard g(ctx->device);  // best effort: destroy returns nothing
     (void)hipDeviceSynchronize();
-    if (ctx->ws) (void)hipFree(ctx->ws);
+    free_ws(ctx);
     if (ctx->stage) (void)hipFree(ctx->stage);
     delete ctx;
 }

@@ -5,6 +5,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <new>
 #include <vector>
 
 #include "dro_internal.h"
@@ -15,6 +16,14 @@ struct dro_ctx {
     int dense_bpc = 1;  // resident dense blocks per compute unit
     void *ws = nullptr;
     size_t ws_size = 0;
+    // Workspaces that graphs captured on this context may replay on: once a call has
+    // been captured, one that is outgrown stays until the context's end.
+    struct Kept {
+        void *ws;
+        Kept *next;
+    };
+    bool captured = false;
+    Kept *kept = nullptr;
     void *scratch = nullptr;    // device address of this device's no-allocation scratch array
     // The host-validated offsets and segment map last staged on the device, and
     // the stream they were staged on: a call whose host arrays and stream match
@@ -97,16 +106,28 @@ inline size_t rup(size_t v) { return (v + 255) & ~size_t(255); }
 
 inline int ensure_ws(dro_ctx *ctx, size_t need, hipStream_t st)
 {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    const bool known = hipStreamIsCapturing(st, &capture) == hipSuccess;
+    if (!known) (void)hipGetLastError();
+    const bool capturing = !known || capture != hipStreamCaptureStatusNone;
+    ctx->captured |= capturing;
     if (need <= ctx->ws_size) return DRO_OK;
-    // earlier work may still read the old buffer: on this stream, or on another
-    // stream the context was used on before (growth is rare, so wait for all)
-    (void)st;
-    HIPCHK(hipDeviceSynchronize());
-    if (ctx->ws) {
+    if (capturing)  // growing it would end the capture
+        return fail(ctx, DRO_EHIP, "a captured call needs a workspace of %zu bytes and there are %zu: "
+                    "make the call once before its capture", need, ctx->ws_size);
+    dro_ctx::Kept *kept = nullptr;
+    if (ctx->ws && ctx->captured) {
+        kept = new (std::nothrow) dro_ctx::Kept{ctx->ws, ctx->kept};
+        if (!kept) return fail(ctx, DRO_ENOMEM, "no host memory for a workspace record");
+        ctx->kept = kept;
+    } else if (ctx->ws) {
+        // earlier work may still read the old buffer: on this stream, or on another
+        // stream the context was used on before (growth is rare, so wait for all)
+        HIPCHK(hipDeviceSynchronize());
         HIPCHK(hipFree(ctx->ws));
-        ctx->ws = nullptr;
-        ctx->ws_size = 0;
     }
+    ctx->ws = nullptr;
+    ctx->ws_size = 0;
     const size_t sz = need + need / 4 + (1u << 20);
     if (hipMalloc(&ctx->ws, sz) != hipSuccess) {
         (void)hipGetLastError();
@@ -115,6 +136,16 @@ inline int ensure_ws(dro_ctx *ctx, size_t need, hipStream_t st)
     }
     ctx->ws_size = sz;
     return DRO_OK;
+}
+
+inline void free_ws(dro_ctx *ctx)
+{
+    if (ctx->ws) (void)hipFree(ctx->ws);
+    while (dro_ctx::Kept *k = ctx->kept) {
+        ctx->kept = k->next;
+        (void)hipFree(k->ws);
+        delete k;
+    }
 }
 
 }  // namespace dro

@@ -1,6 +1,7 @@
 // C ABI of the paged cache: argument checks and launches of kv_block_tables,
 // kv_store and kv_attention.  Every entry point only enqueues work on the caller's
-// stream.
+// stream, except where the workspace has to grow: then the call waits for the device
+// first.
 #include <algorithm>
 #include <cmath>
 
