@@ -119,9 +119,10 @@ static __device__ void kv_write_row(const KvTablesArgs &a, int r, int free, int 
     const int4 q = a.rows[r];
     int32_t *row = a.table + r * a.table_stride;
     if (q.w) {  // ended
-        const int at = free + (int)a.backs[r];
-        for (int i = lane; i < q.x; i += 64)
-            if (at + i < top) a.free_list[at + i] = row[i];
+        // (rows that claim more blocks than the pool has may go beyond 2^31)
+        const int64_t at = (int64_t)free + a.backs[r];
+        const int n = (int)min((int64_t)q.x, max(top - at, (int64_t)0));
+        for (int i = lane; i < n; i += 64) a.free_list[at + i] = row[i];
     } else {
         for (int i0 = q.x; i0 < q.y; i0 += 64) {
             const int i = i0 + lane;
