@@ -58,6 +58,11 @@ def _need(t, dtype, name, device, n):
     return t.data_ptr()
 
 
+def _int32(x):
+    """x for a 32-bit field: beyond its ends, the end (ctypes would take the low 32 bits)."""
+    return min(max(x, -2 ** 31), 2 ** 31 - 1)
+
+
 def _need_table(t, device):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("table must be a CUDA tensor")
@@ -104,7 +109,7 @@ class BlockPool:
         R, width, stride = _need_table(self.table, None)
         dev, nb = self.table.device, self.free_list.numel()
         return _native.KvPoolStruct(
-            R, self.block, nb, width, stride, self.table.data_ptr(),
+            R, _int32(self.block), nb, width, stride, self.table.data_ptr(),
             _need(self.free_list, torch.int32, "free_list", dev, nb),
             _need(self.held, torch.int32, "held", dev, R),
             _need(self.free, torch.int32, "free", dev, 1))
@@ -259,8 +264,8 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     rows = _native.KvRowsStruct(
         DTYPES[q.dtype], R, Hq, T, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1],
         None if lse is None else lse.data_ptr(), start_p, context_p, table.data_ptr(), table_stride,
-        width, int(max_new), dim ** -0.5 if scale is None else scale, softcap, window, slopes_p,
-        prefix_p)
+        width, _int32(int(max_new)), dim ** -0.5 if scale is None else scale, softcap, _int32(window),
+        slopes_p, prefix_p)
     rc = ctx._lib.kv_attention(ctx.handle, ct.byref(cs), ct.byref(rows), _queue(stream, dev))
     if rc:
         ctx.check(rc, "kv_attention")
