@@ -58,6 +58,15 @@ def _need(t, dtype, name, device, n):
     return t.data_ptr()
 
 
+def _no_gradient(where, *tensors):
+    """The calls have no backward pass: rather an error than a gradient that is lost."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise RuntimeError(f"{where} has no backward pass, and an input requires grad: call it under "
+                                   "torch.no_grad() or on detached tensors")
+
+
 def _int32(x):
     """x for a 32-bit field: beyond its ends, the end (ctypes would take the low 32 bits)."""
     return min(max(x, -2 ** 31), 2 ** 31 - 1)
@@ -216,12 +225,14 @@ def kv_block_tables(ctx: Context, pool: BlockPool, length: torch.Tensor, add: to
 def kv_store(ctx: Context, cache: KvCache, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor,
              stream=None) -> None:
     """The keys and values [T, heads, dim] of T tokens into their slots of the cache (see
-    kv_store in dro.h); the tokens and heads may be strided (views of a joint projection)."""
+    kv_store in dro.h); the tokens and heads may be strided (views of a joint projection).
+    No backward pass: inputs that require grad are refused where gradients are recorded."""
     dev, cs = cache.device, cache._struct
     T, ks = _need_rows(k, "k", dev, cs.heads, cs.dim)
     Tv, vs = _need_rows(v, "v", dev, cs.heads, cs.dim)
     if v.dtype is not k.dtype or Tv != T:
         raise ValueError("k and v differ in shape or type")
+    _no_gradient("kv_store", k, v, cache.k, cache.v, cache.k_scale, cache.v_scale)
     rc = ctx._lib.kv_store(ctx.handle, ct.byref(cs), DTYPES[k.dtype], T, k.data_ptr(), ks[0], ks[1],
                            v.data_ptr(), vs[0], vs[1], _need(slot, torch.int64, "slot", dev, T),
                            _queue(stream, dev))
@@ -238,7 +249,8 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
                  stream=None) -> dict:
     """Attention of the rows q [T, Hq, dim] over the cache (see kv_attention in dro.h).  `table`
     is a BlockPool's, `start` and `context` come from kv_block_tables; max_new bounds the rows of
-    one request.  scale defaults to dim ** -0.5."""
+    one request.  scale defaults to dim ** -0.5.  No backward pass: inputs that require grad are
+    refused where gradients are recorded."""
     dev, cs = cache.device, cache._struct
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise TypeError("q must be a [T, Hq, dim] CUDA tensor")
@@ -249,6 +261,7 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     context_p = _need(context, torch.int32, "context", dev, R)
     prefix_p = None if prefix is None else _need(prefix, torch.int32, "prefix", dev, R)
     slopes_p = None if slopes is None else _need(slopes, torch.float32, "slopes", dev, Hq)
+    _no_gradient("kv_attention", q, slopes, cache.k, cache.v, cache.k_scale, cache.v_scale, out, lse)
     with nullcontext() if stream is None else torch.cuda.stream(stream):
         if out is None:
             out = torch.empty((T, Hq, dim), dtype=q.dtype, device=dev)

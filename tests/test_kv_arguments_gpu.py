@@ -37,3 +37,38 @@ def test_numbers_beyond_32_bits(ctx, dev, new):
     one = torch.ones(2, dtype=torch.int32, device=dev)
     with pytest.raises(dro.DroError):
         dro.kv_block_tables(ctx, pool, one, one, 2)
+
+
+def test_inputs_that_require_grad_are_refused(ctx, dev):
+    """There is no backward pass, so no gradient is dropped in silence; without gradients recorded
+    the same tensors are taken."""
+    import torch
+    import paper_2607_16892_amd as dro
+    c = Case(dev, [50, 60], [1, 20], 4, 2, 128, seed=3)
+    slopes = torch.zeros(4, device=dev, requires_grad=True)
+    ref = c.run(ctx, slopes=slopes.detach())
+    slot = torch.arange(3, device=dev)
+    x = torch.ones((3, 2, 128), dtype=torch.bfloat16, device=dev)
+    grad = x.clone().requires_grad_()
+    out = torch.full_like(ref["out"], 7.0)
+    before = c.k.clone(), c.v.clone()
+    for k, v in ((grad, x), (x, grad)):
+        with pytest.raises(RuntimeError, match="no backward"):
+            dro.kv_store(ctx, c.cache, k, v, slot)
+    with pytest.raises(RuntimeError, match="no backward"):
+        c.run(ctx, slopes=slopes, out=out)
+    q = c.q
+    c.q = q.clone().requires_grad_()
+    with pytest.raises(RuntimeError, match="no backward"):
+        c.run(ctx, out=out)
+    torch.cuda.synchronize()
+    assert (out == 7).all() and torch.equal(c.k, before[0]) and torch.equal(c.v, before[1])
+    for off in (torch.no_grad(), torch.inference_mode()):
+        with off:
+            got = c.run(ctx, slopes=slopes)
+            assert torch.equal(got["out"], ref["out"]) and torch.equal(got["lse"], ref["lse"])
+    with torch.no_grad():
+        dro.kv_store(ctx, c.cache, grad, grad, torch.full((3,), -1, device=dev))
+    c.q = c.q.detach()
+    got = c.run(ctx, slopes=slopes.detach())
+    assert torch.equal(got["out"], ref["out"])
