@@ -431,7 +431,8 @@ int dro_bcd_solve(dro_ctx *ctx, const dro_problem *p, const float *eps, const dr
  * the tokens of a block within 2^31 bytes.
  * Device data steers no read or write outside the arrays given: a block
  * outside the pool is read as the nearest one of the pool, a slot outside it
- * is not written, lengths and offsets are cut to the table and to T.
+ * is not written, lengths and offsets are cut to the table and to T.  R and T may
+ * be 0 (arrays of no entries may be NULL then): a step without requests or tokens.
  * ---------------------------------------------------------------------- */
 enum { DRO_BF16 = 0, DRO_F16 = 1, DRO_FP8_E4M3 = 2 };
 

@@ -36,10 +36,10 @@ int check_pool_size(dro_ctx *ctx, int block, int num_blocks)
 
 int check_table(dro_ctx *ctx, const int32_t *table, int R, int max_blocks, int64_t stride, int block)
 {
-    if (R <= 0 || max_blocks <= 0)
-        return fail(ctx, DRO_EINVAL, "R and max_blocks must be positive (R=%d max_blocks=%d)", R,
+    if (R < 0 || max_blocks <= 0)
+        return fail(ctx, DRO_EINVAL, "R=%d must not be negative, max_blocks=%d be positive", R,
                     max_blocks);
-    if (!table) return fail(ctx, DRO_EINVAL, "table is NULL");
+    if (R && !table) return fail(ctx, DRO_EINVAL, "table is NULL");
     if (stride < max_blocks)
         return fail(ctx, DRO_EINVAL, "table_stride=%lld is less than max_blocks=%d",
                     (long long)stride, max_blocks);
@@ -134,9 +134,9 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *p, const int32_t *len, cons
     if (rc) return rc;
     if ((rc = check_table(ctx, p->table, p->R, p->max_blocks, p->table_stride, p->block))) return rc;
     if ((rc = check_tokens(ctx, T, 1))) return rc;
-    if (!p->free_list || !p->held || !p->free_count || !len || !add)
+    if (!p->free_list || !p->free_count || (p->R && (!p->held || !len || !add)))
         return fail(ctx, DRO_EINVAL, "free_list, held, free_count, len or add is NULL");
-    if (!held_out || !free_out || !context || !start || !granted || (T && (!slot || !pos)))
+    if (!free_out || !start || (p->R && (!held_out || !context || !granted)) || (T && (!slot || !pos)))
         return fail(ctx, DRO_EINVAL, "a required output is NULL");
     ENTER_DEVICE(ctx);
     hipStream_t st = (hipStream_t)stream;
@@ -227,7 +227,7 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     if (q->T == 0) return DRO_OK;
     if ((rc = check_rows(ctx, "q", q->q, q->q_token, q->q_head))) return rc;
     if ((rc = check_rows(ctx, "out", q->out, q->out_token, q->out_head))) return rc;
-    if (!q->start || !q->context) return fail(ctx, DRO_EINVAL, "start or context is NULL");
+    if (!q->start || (q->R && !q->context)) return fail(ctx, DRO_EINVAL, "start or context is NULL");
     ENTER_DEVICE(ctx);
     KvAttnArgs a{};
     a.R = q->R;

@@ -255,16 +255,17 @@ hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st)
     // One launch where a wave has at most 16 rows and 256 tokens to write (its blocks are not
     // known here): 64 requests, 512 columns, 15.1 us a call and 17.6 by two launches; 256 requests
     // and 1024 tokens 17.1 and 17.6; 512 and 2000 29.8 and 18.3.
-    if (a.R <= 256 && a.T <= 1024) {
+    if (a.R > 0 && a.R <= 256 && a.T <= 1024) {
         kv_scan_kernel<1024, 1, true><<<1, 1024, 0, st>>>(a);
         return hipGetLastError();
     }
-    if (a.R <= 1024) kv_scan_kernel<1024, 1, false><<<1, 1024, 0, st>>>(a);
+    if (a.R == 0) kv_scan_kernel<1024, 0, false><<<1, 1024, 0, st>>>(a);  // (loads no request)
+    else if (a.R <= 1024) kv_scan_kernel<1024, 1, false><<<1, 1024, 0, st>>>(a);
     else if (a.R <= 4096) kv_scan_kernel<1024, 4, false><<<1, 1024, 0, st>>>(a);
     else kv_scan_kernel<1024, 0, false><<<1, 1024, 0, st>>>(a);
     const int rows = (a.R + kExpandThreads / 64 - 1) / (kExpandThreads / 64);
     const int toks = (a.T + kExpandThreads - 1) / kExpandThreads;
-    kv_expand_kernel<<<rows + toks, kExpandThreads, 0, st>>>(a, rows);
+    if (rows + toks) kv_expand_kernel<<<rows + toks, kExpandThreads, 0, st>>>(a, rows);
     return hipGetLastError();
 }
 

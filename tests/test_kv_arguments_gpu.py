@@ -72,3 +72,26 @@ def test_inputs_that_require_grad_are_refused(ctx, dev):
     c.q = c.q.detach()
     got = c.run(ctx, slopes=slopes.detach())
     assert torch.equal(got["out"], ref["out"])
+
+
+@pytest.mark.parametrize("T", [0, 1, 700, 5000])
+def test_a_step_without_requests(ctx, dev, T):
+    """R = 0: the pool stays as it is, every token is without a slot, every row zero."""
+    import torch
+    import paper_2607_16892_amd as dro
+    none = torch.empty(0, dtype=torch.int32, device=dev)
+    pool = dro.BlockPool.empty(0, 8, 20, 16, dev)
+    pool.free.fill_(7)
+    stack = pool.free_list.clone()
+    plan = dro.kv_block_tables(ctx, pool, none, none, T, reserve=none)
+    assert plan["free"].tolist() == [7] and plan["start"].tolist() == [0]
+    assert (plan["slot"] == -1).all() and (plan["pos"] == -1).all() and len(plan["slot"]) == T
+    assert torch.equal(pool.free_list, stack) and len(pool.take(plan)["held"]) == 0
+    cache = dro.KvCache.empty(20, 16, 2, 64, device=dev)
+    cache.k.fill_(float("nan")), cache.v.fill_(float("nan"))
+    for most in (0, 1, 500):
+        out = torch.full((T, 4, 64), 7.0, dtype=torch.bfloat16, device=dev)
+        got = dro.kv_attention(ctx, cache, torch.ones_like(out), pool.table, plan["start"], plan["context"],
+                               most, out=out)
+        assert (out == 0).all() and (got["lse"] == -torch.inf).all()
+    torch.cuda.synchronize()
