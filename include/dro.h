@@ -513,7 +513,10 @@ int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, 
  *   out = sum_j softmax(s)_j v_j,  lse = log sum_j exp s_j  over the keys seen.
  * A row that sees no key (or whose s are all -infinity) has out = 0 and lse =
  * -infinity; keys and values that a row does not see do not enter it, whatever
- * they hold.  Rows of no request (t outside [start[0], start[R])) are zero with
+ * they hold.  An infinite value that a row sees makes that component of the row
+ * infinite, or NaN where the key's weight rounds to zero (whether it does depends on
+ * which kernel and part of the work the key falls to, so on max_new as well).
+ * Rows of no request (t outside [start[0], start[R])) are zero with
  * lse -infinity.  Products, sums and the softmax are kept in fp32 (the cap's tanh
  * to 2^-21 of the cap); the weights are rounded to q's type for the product with
  * the values (in f16 to within 2^-32 of the row's largest where they are small).

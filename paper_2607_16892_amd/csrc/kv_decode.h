@@ -290,7 +290,9 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         }
 
         if (found) {
-            // whatever its weight, an infinity stays one, and a NaN
+            // An infinity stays one here whatever its weight, and a NaN.  (In steps that all rows
+            // see it goes through the product, where a weight that rounds to zero makes it NaN:
+            // looking at every value of every step would cost more than it is worth.)
             for (int key = k0; key < k1; ++key) {
                 const int step = k0 + ((key - k0) & ~(kStepKeys - 1));
                 if (step >= all_lo && step + kStepKeys <= min(all_hi, k1)) continue;  // not zeroed

@@ -466,7 +466,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         }
 
         if (steps && found && !idle) {  // (the steps' barriers order `found`)
-            // whatever its weight, an infinity stays one, and a NaN
+            // An infinity stays one here whatever its weight, and a NaN.  (In steps that all rows
+            // see it goes through the product, where a weight that rounds to zero makes it NaN:
+            // looking at every value of every step would cost more than it is worth.)
             for (int key = k0; key < k1; ++key) {
                 const int at_step = (key - k0) & ~(KT - 1);
                 if (k0 + at_step >= bot.lo && k0 + at_step + KT <= top.hi) continue;  // not zeroed
