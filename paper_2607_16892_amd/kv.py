@@ -58,13 +58,19 @@ def _need(t, dtype, name, device, n):
     return t.data_ptr()
 
 
-def _no_gradient(where, *tensors):
+# (Checks that nearly every call passes stand in the calls themselves, as one comparison: a decode
+# step makes a call a layer, and a Python call more takes a tenth of a microsecond.)
+def _other_device(ctx, device):
+    """The kernels run on the context's device: tensors of another one would be out of their reach."""
+    if device.index != (ctx.device.index or 0):
+        raise ValueError(f"the context is on {ctx.device}, the tensors are on {device}")
+
+
+def _no_gradient(where):
     """The calls have no backward pass: rather an error than a gradient that is lost."""
     if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise RuntimeError(f"{where} has no backward pass, and an input requires grad: call it under "
-                                   "torch.no_grad() or on detached tensors")
+        raise RuntimeError(f"{where} has no backward pass, and an input requires grad: call it under "
+                           "torch.no_grad() or on detached tensors")
 
 
 def _int32(x):
@@ -181,6 +187,8 @@ class KvCache:
             if t is not None:
                 setattr(s, name, _need(t, torch.float32, name, self.k.device, s.heads))
         object.__setattr__(self, "_struct", s)
+        object.__setattr__(self, "_grad", any(t is not None and t.requires_grad for t in
+                                              (self.k, self.v, self.k_scale, self.v_scale)))
 
     def struct(self) -> _native.KvCacheStruct:
         return self._struct
@@ -194,6 +202,8 @@ def kv_block_tables(ctx: Context, pool: BlockPool, length: torch.Tensor, add: to
     pool.take makes the pool's."""
     ps = pool.struct()
     dev, R, T = pool.device, ps.R, int(tokens)
+    if dev.index != ctx.device.index:
+        _other_device(ctx, dev)
     if T < 0:
         raise ValueError("tokens must not be negative")
     i32 = torch.int32
@@ -228,11 +238,14 @@ def kv_store(ctx: Context, cache: KvCache, k: torch.Tensor, v: torch.Tensor, slo
     kv_store in dro.h); the tokens and heads may be strided (views of a joint projection).
     No backward pass: inputs that require grad are refused where gradients are recorded."""
     dev, cs = cache.device, cache._struct
+    if dev.index != ctx.device.index:
+        _other_device(ctx, dev)
     T, ks = _need_rows(k, "k", dev, cs.heads, cs.dim)
     Tv, vs = _need_rows(v, "v", dev, cs.heads, cs.dim)
     if v.dtype is not k.dtype or Tv != T:
         raise ValueError("k and v differ in shape or type")
-    _no_gradient("kv_store", k, v, cache.k, cache.v, cache.k_scale, cache.v_scale)
+    if k.requires_grad or v.requires_grad or cache._grad:
+        _no_gradient("kv_store")
     rc = ctx._lib.kv_store(ctx.handle, ct.byref(cs), DTYPES[k.dtype], T, k.data_ptr(), ks[0], ks[1],
                            v.data_ptr(), vs[0], vs[1], _need(slot, torch.int64, "slot", dev, T),
                            _queue(stream, dev))
@@ -252,6 +265,8 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     one request.  scale defaults to dim ** -0.5.  No backward pass: inputs that require grad are
     refused where gradients are recorded."""
     dev, cs = cache.device, cache._struct
+    if dev.index != ctx.device.index:
+        _other_device(ctx, dev)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise TypeError("q must be a [T, Hq, dim] CUDA tensor")
     Hq, dim = q.shape[1], cs.dim
@@ -261,7 +276,10 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     context_p = _need(context, torch.int32, "context", dev, R)
     prefix_p = None if prefix is None else _need(prefix, torch.int32, "prefix", dev, R)
     slopes_p = None if slopes is None else _need(slopes, torch.float32, "slopes", dev, Hq)
-    _no_gradient("kv_attention", q, slopes, cache.k, cache.v, cache.k_scale, cache.v_scale, out, lse)
+    if q.requires_grad or cache._grad or (slopes is not None and slopes.requires_grad):
+        _no_gradient("kv_attention")
+    if not 0 <= window < 2 ** 31 or not 0 <= max_new < 2 ** 31:
+        window, max_new = _int32(window), _int32(max_new)
     with nullcontext() if stream is None else torch.cuda.stream(stream):
         if out is None:
             out = torch.empty((T, Hq, dim), dtype=q.dtype, device=dev)
@@ -277,8 +295,8 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     rows = _native.KvRowsStruct(
         DTYPES[q.dtype], R, Hq, T, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1],
         None if lse is None else lse.data_ptr(), start_p, context_p, table.data_ptr(), table_stride,
-        width, _int32(int(max_new)), dim ** -0.5 if scale is None else scale, softcap, _int32(window),
-        slopes_p, prefix_p)
+        width, int(max_new), dim ** -0.5 if scale is None else scale, softcap, window, slopes_p,
+        prefix_p)
     rc = ctx._lib.kv_attention(ctx.handle, ct.byref(cs), ct.byref(rows), _queue(stream, dev))
     if rc:
         ctx.check(rc, "kv_attention")

@@ -95,3 +95,22 @@ def test_a_step_without_requests(ctx, dev, T):
                                most, out=out)
         assert (out == 0).all() and (got["lse"] == -torch.inf).all()
     torch.cuda.synchronize()
+
+
+def test_a_context_of_another_device_is_refused(dev):
+    import torch
+    import paper_2607_16892_amd as dro
+    c = Case(dev, [50, 60], [1, 20], 4, 2, 128, seed=3)
+    pool = dro.BlockPool.empty(2, 8, 20, 16, dev)
+    one = torch.ones(2, dtype=torch.int32, device=dev)
+    x = torch.ones((3, 2, 128), dtype=torch.bfloat16, device=dev)
+    with dro.Context(dev.index or 0) as ctx:
+        ctx.device = torch.device("cuda", 7)         # as if it had been made there
+        with pytest.raises(ValueError, match="context"):
+            c.run(ctx)
+        with pytest.raises(ValueError, match="context"):
+            dro.kv_store(ctx, c.cache, x, x, torch.arange(3, device=dev))
+        with pytest.raises(ValueError, match="context"):
+            dro.kv_block_tables(ctx, pool, one, one, 2)
+        ctx.device = torch.device("cuda")            # the first one
+        c.check(c.run(ctx))
