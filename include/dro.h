@@ -511,6 +511,10 @@ int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, 
  *   s_j = scale q . k_j, then cap tanh(s_j / cap) if cap > 0,
  *   then s_j + slope_h (j - p) with slopes
  *   out = sum_j softmax(s)_j v_j,  lse = log sum_j exp s_j  over the keys seen.
+ * A slope's bias is signed: -slope times the distance for keys behind the row, and
+ * for keys ahead of it (of a prefix) the same line goes on upwards.  So the softmax is
+ * that of s_j + slope_h j, a bias by the key's place alone, for every row; a model
+ * trained with -slope |j - p| both ways cannot have it from slopes beside a prefix.
  * A row that sees no key (or whose s are all -infinity) has out = 0 and lse =
  * -infinity; keys and values that a row does not see do not enter it, whatever
  * they hold.  An infinite value that a row sees makes that component of the row
