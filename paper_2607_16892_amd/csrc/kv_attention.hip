@@ -98,8 +98,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
     const uint64_t share = kv_tile_share(cut, steps_all * a.H);
     // Where not all tiles run at once and one pass holds them, they go by quarters of a share, the
     // longest first, so that none of them is waited for alone (128 requests of 500 to 4000 keys, three
-    // tokens of 8 heads to each of 8: 210 us as they come, so 181; 31 single tokens beside 9 chunks:
-    // 92 and 87).
+    // tokens of 8 heads to each of 8: 206 us as they come, so 180; six prompts of 300 to 2000 tokens, 12
+    // heads of 64 components: 48 and 45; 31 single tokens beside 9 chunks: 59 and 60).
     const bool sort = n <= kPlanThreads &&
                       (__syncthreads_or(mine.steps + share / 4 >= 2 * share) || n * a.H > cut.groups);
     if (sort) {
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
 // from its partial results.  The kernel before left the entries.  Up to kFewParts parts
 // a wave joins as many rows as its lanes reach with 16 bytes each; more (a long request alone)
 // the waves share, a workgroup to a row (with 16 in its place 64 tokens of 8 heads over 8000 keys
-// took 49 us, now 35).  Bound by latency (the parts come from other dies' caches), so a wave asks
+// take 67 us, so 37).  Bound by latency (the parts come from other dies' caches), so a wave asks
 // for several parts at once.
 
 // The running join of a row's parts, V components a lane.
@@ -267,8 +267,8 @@ static int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 // Requests of up to this many rows a key head are the kernel's for few rows, others the other's:
 // one of its tiles.  Where the calls are small, two, as they have no list of tiles to wait for.
-// (128 requests of 500 to 4000 keys, 24 rows a key head: one tile 196 us, two 330; 32 of 1000 to
-// 8000, 32 rows: 53 and 76; one of 1000, 32 rows: 20 and 14.5.)
+// (128 requests of 500 to 4000 keys, 24 rows a key head: one tile 180 us, two 314; 32 of 1000 to
+// 8000, 32 rows: 58 and 75; one of 1000, 32 rows: 20 and 15.)
 static int few_rows(const KvAttnArgs &a) { return (int64_t)a.R * a.H < 16 ? 32 : 16; }
 
 constexpr int kFewRequests = 64;
@@ -285,9 +285,12 @@ static KvPlans plans(const KvAttnArgs &a, int cache_dtype)
     const bool all_few = a.max_new <= few;
     // The one kernel takes all with so many rows that each request has more than few (by max_new,
     // so that a bound that does not hold loses no request), and where there are few requests: the
-    // other's two launches and its reading beside no products cost more than it saves (31 single
-    // tokens beside 9 chunks of 33 to 300, 8 heads on 4 of 256 components: 83 us, so 61; 58 beside
-    // two of 512 over 500 to 8000 keys, 32 heads on 8: 224 and 194).
+    // other's two launches and its reading beside no products cost more than it mostly saves (31 single
+    // tokens beside 9 chunks of 33 to 300, 8 heads on 4 of 256 components: 78 us by both, so 60; 58
+    // beside two of 512 over 500 to 8000 keys, 32 heads on 8: 220 and 187; 30 beside 30: 812 and 786;
+    // 30 beside two of 100 to 300: 139 and 124).  It loses where a long chunk's tiles fill the compute
+    // units and a single token's tile waits for them: one beside a chunk of 500 over 60,000 keys, 546 us
+    // by both, so 722.  The contexts that tell the two apart are on the device.
     const bool all_many = !all_few && (a.R <= kFewRequests || a.T > (int64_t)(a.R - 1) * a.max_new + few);
     KvPlans p{};
     if (!all_many) {
@@ -356,7 +359,7 @@ template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, 
 {
     // Items so few that each may have more than 64 parts are few among the entries too: eight waves
     // to a row, 32 entries a workgroup.  Else a workgroup to an entry or four and as many rows as
-    // it joins at once.  (Sixteen waves: a join of 30 us, the call 44; eight: the call 27,
+    // it joins at once.  (The call with sixteen waves 32 us, with eight 24,
     // for 32 requests of 1000 to 8000 keys, two tokens of eight heads to one key head of 64
     // components each.)
     const unsigned most = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)a.max_new * a.G, c.rows));

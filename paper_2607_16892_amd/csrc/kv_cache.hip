@@ -17,7 +17,7 @@ namespace dro {
 // there is read there: a block that is handed out comes from the part of the stack that
 // was there before, or straight from the table row of the request that gave it back.
 // Bound by latency: requests are loaded at once, and searches take 64 probes a step.  64 requests
-// take 6 us; 4096 with 65,536 new tokens 11 and, for the second launch, 10.
+// take 5.3 us; 4096 with 65,536 new tokens 11.4 and, for the second launch, 9.0.
 
 struct KvRequest {
     long long n, after;
@@ -253,8 +253,8 @@ __global__ __launch_bounds__(kExpandThreads) void kv_expand_kernel(const KvTable
 hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st)
 {
     // One launch where a wave has at most 16 rows and 256 tokens to write (its blocks are not
-    // known here): 64 requests, 512 columns, 15.1 us a call and 17.6 by two launches; 256 requests
-    // and 1024 tokens 17.1 and 17.6; 512 and 2000 29.8 and 18.3.
+    // known here): 64 requests, 512 columns, 14.3 us a call and 16.4 by two launches; 256 requests
+    // and 1024 tokens 16.2 and 16.4; 512 and 2000 29.0 and 16.4.
     if (a.R > 0 && a.R <= 256 && a.T <= 1024) {
         kv_scan_kernel<1024, 1, true><<<1, 1024, 0, st>>>(a);
         return hipGetLastError();
@@ -275,8 +275,8 @@ hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st)
 // flight.  Bound by memory, if the indices and the divisions by the scale stay cheap: one
 // index for all of a thread's tokens, one reciprocal.
 
-// 8001 tokens of 8 heads of 128 components into 8 bits: 49 MB in 11.4 us; with one token in
-// flight 12.8, with eight 13.1.
+// 8001 tokens of 8 heads of 128 components into 8 bits: 49 MB in 11.3 us; with one token in
+// flight 12.5, with eight 12.8.
 
 constexpr int kStoreThreads = 256;
 constexpr int kStoreSteps = 4;

@@ -10,8 +10,8 @@
 // transpose of 8 rows x 16 bytes inside each lane.  A workgroup is one wave with its own
 // run of steps: while one begins or ends an item, the other seven of the compute unit
 // read on.  (Four waves that shared a run and met in LDS after each item: 124 us for 64
-// requests of 50 to 8192 keys on 8 heads, 464 MB, against 101 now: 4.8 TB/s in
-// the kernel, and 5.3 from 128 requests of 1000 to 16,384 keys in 8 bits.)
+// requests of 50 to 8192 keys on 8 heads, 464 MB, against 102 now: 4.7 TB/s in
+// the kernel, and 5.2 from 128 requests of 1000 to 16,384 keys in 8 bits.)
 #pragma once
 
 #include "kv_math.h"
@@ -23,8 +23,8 @@ constexpr int kDecodeRows = 16;
 
 // Waves a SIMD, so registers: the keys of the next step and this one's values (32 x 256 bytes
 // each) take 64 of a wave's, beside queries and sums.  With 256 components one wave has both on
-// their way where two had not: 64 requests of 50 to 8192 keys on 8 heads, 16 bits 206 -> 182 us, 8
-// bits 131 -> 117.
+// their way where two have not: 64 requests of 50 to 8192 keys on 8 heads, 16 bits 182 us and 245 with
+// two, 8 bits 117 and 129.
 constexpr int decode_waves(int DP, int E) { return DP == 256 ? 1 : DP * E >= 256 ? 2 : DP * E >= 128 ? 3 : 4; }
 
 template <class T, class C, int DP, bool FULL>

@@ -15,7 +15,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // Running maxima are raised only when a step exceeds them by 2^kSlack, so most steps
 // rescale nothing; weights stay below 2^kSlack of that maximum's.  (With 0 a prompt of 8192 tokens,
-// 64 heads on 8, takes 1250 us where 8 takes 1168.)
+// 64 heads on 8, takes 1136 us where 8 takes 1098.)
 constexpr float kSlack = 8.0f;
 
 // The running maximum m is held 2^kUnit below the largest score, so the largest weight of a row is

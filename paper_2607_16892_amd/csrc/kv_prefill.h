@@ -13,9 +13,9 @@
 // the rows and (transposed) across them, meet all banks.  16-bit caches go from memory to
 // LDS directly, the next tile while one is worked on.
 //
-// A prompt of 8192 tokens, 64 heads on 8 of 128 components: 1.10 ms, 1.0 PFLOP/s, the matrix
-// units busy 52 % of the cycles; four chunks of 512 over 4000 to 8192, 32 heads on 8: 245 us,
-// 900 TFLOP/s.
+// A prompt of 8192 tokens, 64 heads on 8 of 128 components: 1.06 to 1.15 ms from card to card, 0.96 to
+// 1.04 PFLOP/s, the matrix units busy 52 % of the cycles; four chunks of 512 over 4000 to 8192, 32 heads
+// on 8: 234 to 251 us, 880 to 940 TFLOP/s.
 #pragma once
 
 #include <type_traits>
@@ -28,7 +28,7 @@ namespace dro {
 // With 256 components the sums of 32 rows are half a wave's registers already, so two waves
 // share rows there: both compute the scores, each the sums of half the components.  (Whole
 // rows a wave went through scratch memory: 284 us for a mixed call of 40 requests, 8 heads on
-// 4, against 141.)
+// 4, against 141 side by side then.)
 constexpr int prefill_split(int DP) { return DP == 256 ? 2 : 1; }
 constexpr int prefill_rows(int DP) { return 128 / prefill_split(DP); }
 
@@ -532,7 +532,10 @@ void run_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsig
                     KvJoin *joins, hipStream_t st)
 {
     auto run = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
-    // (a head dimension between the padded ones takes the kernel of all score changes as well)
+    // A head dimension between the padded ones takes the kernel of all score changes as well.  Its
+    // instances beyond 64 components keep 76 to 97 registers in scratch memory, and so do those of 128
+    // with score changes (14, with 8 bits 49) and of 256 in 8 bits with them (4): read back in the
+    // steps, behind the next tile's loads.
     if (a.D != DP) run(kv_prefill_kernel<T, C, DP, true, false>);
     else if (a.cap > 0.0f || a.slopes || a.scale == 0.0f) run(kv_prefill_kernel<T, C, DP, true, true>);
     else run(kv_prefill_kernel<T, C, DP, false, true>);

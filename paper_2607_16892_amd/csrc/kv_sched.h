@@ -34,9 +34,9 @@ struct KvItem {
 // takes as long as several steps and workgroups do not run at one speed.  A tile is cut into
 // as many chunks as it has equal shares of all steps, a quarter aside: so one of less than 1.75
 // shares stays whole and no part of it is written or joined.  (Equal runs of steps, as above,
-// against this: a prompt of 8192 tokens, 64 heads on 8, 1546 against 1160 us; four prompts of
-// 2000 tokens, 32 heads on 8, 256 against 168; four chunks of 512 tokens over 4000 to 8192, 281
-// against 244, and 320 with every tile of more than one share cut.)
+// against this, side by side when it was chosen: a prompt of 8192 tokens, 64 heads on 8, 1546 against
+// 1160 us; four prompts of 2000 tokens, 32 heads on 8, 256 against 168; four chunks of 512 tokens over
+// 4000 to 8192, 281 against 244, and 320 with every tile of more than one share cut.)
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
@@ -76,7 +76,7 @@ __device__ __forceinline__ uint64_t kv_units(const KvAttnArgs &a, const KvShare 
 
 // steps a workgroup, for `all` steps, the longest of the wave's items having `longest`.  An
 // item of many steps alone would be cut so fine that the join takes longer than the steps (one
-// request of 131,000 keys, 8 heads on one: 82 us with runs of two steps, 35 with eight; of
+// request of 131,000 keys, 8 heads on one: 81 us with runs of one step, 34 with eight; of
 // 16,000: 27 with one, 19 with two).
 __device__ __forceinline__ uint64_t kv_run(const KvCut &c, uint64_t all, uint32_t longest)
 {
@@ -224,7 +224,7 @@ __device__ __forceinline__ uint32_t kv_tile_steps(const KvAttnArgs &a, const KvS
 }
 
 // An equal share of `all` steps, not below four: a part of a tile costs about as much as two
-// steps to write and join (64 tokens of 8 heads over 8000 keys: 49 us, and 65 with shares down
+// steps to write and join (64 tokens of 8 heads over 8000 keys: 37 us, and 60 with shares down
 // to one step).
 __device__ __forceinline__ uint64_t kv_tile_share(const KvCut &c, uint64_t all)
 {
