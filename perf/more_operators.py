@@ -11,7 +11,7 @@ Caches in shared scales hold a row's components in groups of 32, each group as a
 (a byte, 2^(byte - 127)) and 32 codes: "mx4" of 4 bits (values 0, .5, 1, 1.5, 2, 3, 4, 6 and a
 sign; byte i of a row holds the codes of components 2i, its low half, and 2i + 1) or "mx8" of 8
 (e4m3).  The power is the least that leaves the group's largest value nearest to the format's
-largest or below it.
+largest or below it, within the powers whose codes are all normal and finite in the type written.
 
 Sizes follow the package's own: blocks of 16 tokens, inputs of 50 to 2,000 tokens of which a
 part is shared, lengths up to 8192, 16,384 and 32,768; heads as one GPU of a tensor-parallel
@@ -180,6 +180,13 @@ def _power(e):
     return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
 
 
+def _powers(dtype, four):
+    """The least and the largest power of a group: the format's smallest value is a normal bf16
+    number there, its largest one finite in `dtype`."""
+    wide = dtype != torch.float16
+    return (-125, 125 if wide else 13) if four else (-117, 119 if wide else 7)
+
+
 def _encode(x, kind):
     """Codes (mx4: two a byte; mx8: e4m3) and powers' bytes of rows x [.., D]."""
     g = x.float().unflatten(-1, (-1, GROUP))
@@ -187,8 +194,8 @@ def _encode(x, kind):
     m, e = torch.frexp(top)
     four = kind == "mx4"
     e = e - 3 + (m > 0.875).int() if four else e - 9 + (m > 0.90625).int()
-    least = -125 if four else -117
-    e = torch.where(top > 0, e, least).clamp(min=least)
+    least, most = _powers(x.dtype, four)
+    e = torch.where(top > 0, e, least).clamp(least, most)
     y = (g * _power(-e)[..., None]).flatten(-2)
     byte = (e + 127).to(torch.uint8)
     if not four:
@@ -457,11 +464,12 @@ def _exact_nearest(x, kind):
     """Every component's nearest value (ties to the even code) in its group's power, in 64 bits."""
     g = x.double().unflatten(-1, (-1, GROUP))
     top = g.abs().amax(-1, keepdim=True)
-    big, half, least = (6.0, 1.0, -125) if kind == "mx4" else (448.0, 16.0, -117)
+    big, half = (6.0, 1.0) if kind == "mx4" else (448.0, 16.0)
+    least, most = _powers(x.dtype, kind == "mx4")
     # the least power whose largest value is half a step away at most
     e = torch.ceil(torch.log2(top / (big + half)))
     e = torch.where(top > (big + half) * torch.exp2(e), e + 1, e)
-    e = torch.where(top <= (big + half) * torch.exp2(e - 1), e - 1, e).clamp(min=least)
+    e = torch.where(top <= (big + half) * torch.exp2(e - 1), e - 1, e).clamp(least, most)
     a = g / torch.exp2(e)
     # steps: of a value in [2^n, 2^(n + 1)) 2^(n - mantissa bits), n at least the smallest normal's
     bits, low = (1, 0) if kind == "mx4" else (3, -6)
