@@ -322,7 +322,7 @@ def prepare(case, seed):
         import paper_2607_16892_amd as dro
         s["ctx"] = _context()
         s["cache"] = dro.KvCache(k=s["kc"], v=s["vc"], k_scale=s["ks"], v_scale=s["vs"],
-                                 k_exp=s["ke"], v_exp=s["ve"])
+                                 k_power=s["ke"], v_power=s["ve"])
         if c["kind"] == "shared":
             s["shared"] = dro.SharedPrefixes(first=s["first"], context=s["pre"][:-1],
                                              table=s["shared_table"], max_new=s["shared_new"])
