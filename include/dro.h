@@ -47,7 +47,7 @@
  *    correctly.  A replay uses the ctx's workspace and staged offsets as they
  *    are then: after any call on that ctx with another problem or on another
  *    stream, capture again.  (dro_cost_eval_noalloc has no such bond to its ctx.)
- *    kv_block_tables, kv_store and kv_attention enqueue kernels only as well, once
+ *    kv_block_tables, kv_store, kv_load and kv_attention enqueue kernels only as well, once
  *    a call on the ctx has needed as large a workspace (one that has to grow it under
  *    capture is DRO_EHIP and enqueues nothing).  The workspace that a captured
  *    call was given stays until dro_destroy, whatever later calls need, so their
@@ -421,7 +421,7 @@ int dro_bcd_solve(dro_ctx *ctx, const dro_problem *p, const float *eps, const dr
  * of the pool.  One step of a serving loop is kv_block_tables (blocks for the
  * step's new tokens and for the reservations r = L_in + eta of this library),
  * then per layer kv_store (the new tokens' keys and values into their slots)
- * and kv_attention (the new tokens' attention over the cache).
+ * and kv_attention (the new tokens' attention over the cache); kv_load reads back.
  *
  * Strides and lengths are in elements.  Limits (DRO_ELIMIT): blocks of 16 to
  * 1024 tokens, a power of two; head dimension a multiple of 8 up to 256; R up
@@ -434,7 +434,7 @@ int dro_bcd_solve(dro_ctx *ctx, const dro_problem *p, const float *eps, const dr
  * is not written, lengths and offsets are cut to the table and to T.  R and T may
  * be 0 (arrays of no entries may be NULL then): a step without requests or tokens.
  * ---------------------------------------------------------------------- */
-enum { DRO_BF16 = 0, DRO_F16 = 1, DRO_FP8_E4M3 = 2 };
+enum { DRO_BF16 = 0, DRO_F16 = 1, DRO_FP8_E4M3 = 2, DRO_MXFP4 = 3, DRO_MXFP8 = 4 };
 
 /* Block tables and slots of one step.  Request r holds len[r] tokens in
  * held[r] blocks and brings add[r] new ones (0: none; < 0: it ends and gives
@@ -483,7 +483,21 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *pool, const int32_t *len, c
  * of 8 elements, and k and v are aligned to 8 elements.  dtype DRO_FP8_E4M3 holds
  * key / k_scale[h] and value / v_scale[h], rounded to nearest even and saturated
  * at +-448 (NaN stays NaN); the scales ([heads], > 0) are NULL for the other
- * types. */
+ * types.
+ * DRO_MXFP4 and DRO_MXFP8 (dim a multiple of 32, strides multiples of 32 elements, k and
+ * v aligned to 16 bytes) need no scales beforehand: components 32 g .. 32 g + 31 of a row
+ * share the power of two 2^(y - 127), y the byte
+ *   k_power[b k_power_block + i k_power_token + h k_power_head + g]
+ * (255: the group is NaN), and are codes of 4 bits (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign,
+ * e2m1; component d in byte d / 2 of the row, the even one in its low half) or 8 (e4m3).
+ * kv_store takes for a group of largest magnitude top (an infinity counts as the largest
+ * finite number of its type, NaN aside) the least power with top <= 7 2^e (MXFP4) or
+ * 464 2^e (MXFP8), so that the largest is not cut by more than rounding changes it, but
+ * -125 <= e <= 125 or -117 <= e <= 119 (from DRO_F16 e <= 13 or 7: so that every code's
+ * value is a normal number of bf16, and finite in the type written), and rounds x / 2^e to
+ * nearest even, saturated at +-6 or +-448.  A NaN makes its MXFP4 group NaN; MXFP8 keeps it
+ * as such.  What is read is exact in bf16; in f16 it is rounded to that, beyond its range
+ * to an infinity.  The powers are read and written with these two types only. */
 typedef struct {
     int32_t dtype;
     int32_t heads, dim, block, num_blocks;
@@ -491,16 +505,28 @@ typedef struct {
     int64_t k_block, k_token, k_head;
     int64_t v_block, v_token, v_head;
     const float *k_scale, *v_scale;
+    uint8_t *k_power, *v_power;
+    int64_t k_power_block, k_power_token, k_power_head;
+    int64_t v_power_block, v_power_token, v_power_head;
 } dro_kv_cache;
 
 /* The keys and values of T tokens into their slots: token t, head h, component d
  * at k[t k_token + h k_head + d] (strides of this call, multiples of 8, k and v
  * aligned to 16 bytes) of type `dtype`, DRO_BF16 or DRO_F16, which the cache's
- * type is unless that is DRO_FP8_E4M3.  Slots outside [0, num_blocks * block)
+ * type is unless that is one of 8 or 4 bits.  Slots outside [0, num_blocks * block)
  * (-1: no slot) are skipped; of two tokens with one slot either may remain. */
 int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, const void *k,
              int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
              const int64_t *slot, dro_stream_t stream);
+
+/* The other way: the keys and values of T slots, as the cache holds them, into rows laid
+ * out and typed as kv_store's (a cache of 8 or 4 bits gives either type: code times scale,
+ * rounded once).  Rows of slots outside [0, num_blocks * block) are zero.  A prefix moves
+ * to another cache, of any type, by kv_load and kv_store.  k and v may not overlap the
+ * cache, nor rows each other. */
+int kv_load(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, void *k,
+            int64_t k_token, int64_t k_head, void *v, int64_t v_token, int64_t v_head,
+            const int64_t *slot, dro_stream_t stream);
 
 /* Attention of each request's last tokens over the cache.  Request r has
  * context[r] tokens in the cache, the last n = start[r+1] - start[r] of which

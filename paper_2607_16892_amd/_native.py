@@ -48,7 +48,9 @@ class KvCacheStruct(ct.Structure):
     _fields_ = [("dtype", i32), ("heads", i32), ("dim", i32), ("block", i32), ("num_blocks", i32),
                 ("k", P), ("v", P), ("k_block", i64), ("k_token", i64), ("k_head", i64),
                 ("v_block", i64), ("v_token", i64), ("v_head", i64), ("k_scale", P),
-                ("v_scale", P)]
+                ("v_scale", P), ("k_power", P), ("v_power", P), ("k_power_block", i64),
+                ("k_power_token", i64), ("k_power_head", i64), ("v_power_block", i64),
+                ("v_power_token", i64), ("v_power_head", i64)]
 
 
 class KvRowsStruct(ct.Structure):
@@ -92,6 +94,7 @@ EXPORTS = {
     "kv_block_tables": (ct.c_int, [P, ct.POINTER(KvPoolStruct), P, P, P, i64, P, P, P, P, P, P, P,
                                    P]),
     "kv_store": (ct.c_int, [P, ct.POINTER(KvCacheStruct), i32, i64, P, i64, i64, P, i64, i64, P, P]),
+    "kv_load": (ct.c_int, [P, ct.POINTER(KvCacheStruct), i32, i64, P, i64, i64, P, i64, i64, P, P]),
     "kv_attention": (ct.c_int, [P, ct.POINTER(KvCacheStruct), ct.POINTER(KvRowsStruct), P]),
 }
 

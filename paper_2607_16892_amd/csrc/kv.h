@@ -1,4 +1,4 @@
-// Launchers of the paged-cache kernels (block tables, store, attention).
+// Launchers of the paged-cache kernels (block tables, store, load, attention).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -26,19 +26,23 @@ struct KvTablesArgs {
 };
 hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t st);
 
-// ---- store --------------------------------------------------------------------
+// ---- store and load --------------------------------------------------------------------
 struct KvStoreArgs {
     int T, H, D;
     int shift;
     int64_t slots;                // num_blocks << shift
-    const void *x[2];             // keys, values
+    void *x[2];                   // keys, values
     int64_t x_token[2], x_head[2];
     void *c[2];                   // the cache's
     int64_t c_block[2], c_token[2], c_head[2];
     const float *scale[2];        // fp8 caches
+    uint8_t *power[2];            // caches in shared scales
+    int64_t p_block[2], p_token[2], p_head[2];
     const int64_t *slot;
 };
 hipError_t launch_kv_store(const KvStoreArgs &a, int dtype, int cache_dtype, hipStream_t st);
+// the other way: x written, the cache read
+hipError_t launch_kv_load(const KvStoreArgs &a, int dtype, int cache_dtype, hipStream_t st);
 
 // ---- attention ----------------------------------------------------------------
 struct KvAttnArgs {

@@ -1,5 +1,5 @@
 // C ABI of the paged cache: argument checks and launches of kv_block_tables,
-// kv_store and kv_attention.  Every entry point only enqueues work on the caller's
+// kv_store, kv_load and kv_attention.  Every entry point only enqueues work on the caller's
 // stream, except where the workspace has to grow: then the call waits for the device
 // first.
 #include <algorithm>
@@ -62,7 +62,9 @@ int check_tokens(dro_ctx *ctx, int64_t T, int heads)
     return DRO_OK;
 }
 
-int size_of(int dtype) { return dtype == DRO_FP8_E4M3 ? 1 : 2; }
+bool is_mx(int dtype) { return dtype == DRO_MXFP4 || dtype == DRO_MXFP8; }
+// bits of a component
+int bits_of(int dtype) { return dtype == DRO_MXFP4 ? 4 : dtype == DRO_FP8_E4M3 || dtype == DRO_MXFP8 ? 8 : 16; }
 
 bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
@@ -82,31 +84,41 @@ int check_cache(dro_ctx *ctx, const dro_kv_cache *c)
 {
     if (!ctx) return DRO_EINVAL;
     if (!c) return fail(ctx, DRO_EINVAL, "cache is NULL");
-    if (c->dtype != DRO_BF16 && c->dtype != DRO_F16 && c->dtype != DRO_FP8_E4M3)
+    if (c->dtype < DRO_BF16 || c->dtype > DRO_MXFP8)
         return fail(ctx, DRO_EINVAL, "cache type %d is unknown", c->dtype);
     if (c->heads <= 0 || c->dim <= 0)
         return fail(ctx, DRO_EINVAL, "heads and dim must be positive (heads=%d dim=%d)", c->heads,
                     c->dim);
-    if (c->dim % 8 || c->dim > 256)
-        return fail(ctx, DRO_ELIMIT, "dim=%d is not a multiple of 8 up to 256", c->dim);
+    const bool mx = is_mx(c->dtype);
+    const int step = mx ? 32 : 8, bits = bits_of(c->dtype), align = mx ? 16 : bits;
+    if (c->dim % step || c->dim > 256)
+        return fail(ctx, DRO_ELIMIT, "dim=%d is not a multiple of %d up to 256", c->dim, step);
     if (int rc = check_pool_size(ctx, c->block, c->num_blocks)) return rc;
-    const int bytes = size_of(c->dtype);
     const int64_t s[6] = {c->k_block, c->k_token, c->k_head, c->v_block, c->v_token, c->v_head};
     if (!c->k || !c->v) return fail(ctx, DRO_EINVAL, "the cache's k or v is NULL");
-    if (!aligned(c->k, 8 * bytes) || !aligned(c->v, 8 * bytes))
-        return fail(ctx, DRO_EINVAL, "the cache's k or v is not aligned to 8 elements");
+    if (!aligned(c->k, align) || !aligned(c->v, align))
+        return fail(ctx, DRO_EINVAL, "the cache's k or v is not aligned to %d bytes", align);
     for (int64_t x : s) {
-        if (x % 8) return fail(ctx, DRO_EINVAL, "a cache stride %lld is not a multiple of 8",
-                               (long long)x);
+        if (x % step) return fail(ctx, DRO_EINVAL, "a cache stride %lld is not a multiple of %d",
+                                  (long long)x, step);
         if (x < 0 || x > (1LL << 38))
             return fail(ctx, DRO_ELIMIT, "a cache stride %lld is outside [0, 2^38]", (long long)x);
     }
     // offsets of a token within its block are 32-bit in the kernels
-    if (std::max(c->k_token, c->v_token) * c->block * bytes > 0x7fffffffLL)
+    if (std::max(c->k_token, c->v_token) * c->block / 8 * bits > 0x7fffffffLL)
         return fail(ctx, DRO_ELIMIT, "the tokens of a block lie 2^31 bytes or more apart");
     const bool scaled = c->k_scale && c->v_scale;
     if (scaled != (c->dtype == DRO_FP8_E4M3) || (!c->k_scale) != (!c->v_scale))
         return fail(ctx, DRO_EINVAL, "k_scale and v_scale go with DRO_FP8_E4M3 and no other type");
+    if (!mx) return DRO_OK;  // (the fields behind are not read)
+    if (!c->k_power || !c->v_power) return fail(ctx, DRO_EINVAL, "the cache's k_power or v_power is NULL");
+    const int64_t t[6] = {c->k_power_block, c->k_power_token, c->k_power_head,
+                          c->v_power_block, c->v_power_token, c->v_power_head};
+    for (int64_t x : t)
+        if (x < 0 || x > (1LL << 38))
+            return fail(ctx, DRO_ELIMIT, "a stride %lld of the powers is outside [0, 2^38]", (long long)x);
+    if (std::max(c->k_power_token, c->v_power_token) * c->block > 0x7fffffffLL)
+        return fail(ctx, DRO_ELIMIT, "the powers of a block lie 2^31 bytes or more apart");
     return DRO_OK;
 }
 
@@ -114,8 +126,59 @@ int check_dtype(dro_ctx *ctx, int dtype, const dro_kv_cache *c)
 {
     if (dtype != DRO_BF16 && dtype != DRO_F16)
         return fail(ctx, DRO_EINVAL, "type %d is neither DRO_BF16 nor DRO_F16", dtype);
-    if (c->dtype != DRO_FP8_E4M3 && c->dtype != dtype)
+    if (bits_of(c->dtype) == 16 && c->dtype != dtype)
         return fail(ctx, DRO_EINVAL, "type %d differs from the cache's %d", dtype, c->dtype);
+    return DRO_OK;
+}
+
+// kv_store and kv_load: rows into the cache, or out of it.
+int move_rows(dro_ctx *ctx, const dro_kv_cache *c, int32_t dtype, int64_t T, void *k, int64_t k_token,
+              int64_t k_head, void *v, int64_t v_token, int64_t v_head, const int64_t *slot,
+              dro_stream_t stream, hipError_t (*launch)(const KvStoreArgs &, int, int, hipStream_t))
+{
+    int rc = check_cache(ctx, c);
+    if (rc) return rc;
+    if ((rc = check_dtype(ctx, dtype, c))) return rc;
+    if ((rc = check_tokens(ctx, T, c->heads))) return rc;
+    if (T == 0) return DRO_OK;
+    if ((rc = check_rows(ctx, "k", k, k_token, k_head))) return rc;
+    if ((rc = check_rows(ctx, "v", v, v_token, v_head))) return rc;
+    if (!slot) return fail(ctx, DRO_EINVAL, "slot is NULL");
+    ENTER_DEVICE(ctx);
+    KvStoreArgs a{};
+    a.T = (int)T;
+    a.H = c->heads;
+    a.D = c->dim;
+    a.shift = block_shift(c->block);
+    a.slots = (int64_t)c->num_blocks * c->block;
+    a.x[0] = k;
+    a.x[1] = v;
+    a.x_token[0] = k_token;
+    a.x_token[1] = v_token;
+    a.x_head[0] = k_head;
+    a.x_head[1] = v_head;
+    a.c[0] = c->k;
+    a.c[1] = c->v;
+    a.c_block[0] = c->k_block;
+    a.c_block[1] = c->v_block;
+    a.c_token[0] = c->k_token;
+    a.c_token[1] = c->v_token;
+    a.c_head[0] = c->k_head;
+    a.c_head[1] = c->v_head;
+    a.scale[0] = c->k_scale;
+    a.scale[1] = c->v_scale;
+    if (is_mx(c->dtype)) {
+        a.power[0] = c->k_power;
+        a.power[1] = c->v_power;
+        a.p_block[0] = c->k_power_block;
+        a.p_block[1] = c->v_power_block;
+        a.p_token[0] = c->k_power_token;
+        a.p_token[1] = c->v_power_token;
+        a.p_head[0] = c->k_power_head;
+        a.p_head[1] = c->v_power_head;
+    }
+    a.slot = slot;
+    HIPCHK(launch(a, dtype, c->dtype, (hipStream_t)stream));
     return DRO_OK;
 }
 
@@ -174,40 +237,15 @@ int kv_store(dro_ctx *ctx, const dro_kv_cache *c, int32_t dtype, int64_t T, cons
              int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
              const int64_t *slot, dro_stream_t stream)
 {
-    int rc = check_cache(ctx, c);
-    if (rc) return rc;
-    if ((rc = check_dtype(ctx, dtype, c))) return rc;
-    if ((rc = check_tokens(ctx, T, c->heads))) return rc;
-    if (T == 0) return DRO_OK;
-    if ((rc = check_rows(ctx, "k", k, k_token, k_head))) return rc;
-    if ((rc = check_rows(ctx, "v", v, v_token, v_head))) return rc;
-    if (!slot) return fail(ctx, DRO_EINVAL, "slot is NULL");
-    ENTER_DEVICE(ctx);
-    KvStoreArgs a{};
-    a.T = (int)T;
-    a.H = c->heads;
-    a.D = c->dim;
-    a.shift = block_shift(c->block);
-    a.slots = (int64_t)c->num_blocks * c->block;
-    a.x[0] = k;
-    a.x[1] = v;
-    a.x_token[0] = k_token;
-    a.x_token[1] = v_token;
-    a.x_head[0] = k_head;
-    a.x_head[1] = v_head;
-    a.c[0] = c->k;
-    a.c[1] = c->v;
-    a.c_block[0] = c->k_block;
-    a.c_block[1] = c->v_block;
-    a.c_token[0] = c->k_token;
-    a.c_token[1] = c->v_token;
-    a.c_head[0] = c->k_head;
-    a.c_head[1] = c->v_head;
-    a.scale[0] = c->k_scale;
-    a.scale[1] = c->v_scale;
-    a.slot = slot;
-    HIPCHK(launch_kv_store(a, dtype, c->dtype, (hipStream_t)stream));
-    return DRO_OK;
+    return move_rows(ctx, c, dtype, T, (void *)k, k_token, k_head, (void *)v, v_token, v_head, slot, stream,
+                     launch_kv_store);
+}
+
+int kv_load(dro_ctx *ctx, const dro_kv_cache *c, int32_t dtype, int64_t T, void *k, int64_t k_token,
+            int64_t k_head, void *v, int64_t v_token, int64_t v_head, const int64_t *slot,
+            dro_stream_t stream)
+{
+    return move_rows(ctx, c, dtype, T, k, k_token, k_head, v, v_token, v_head, slot, stream, launch_kv_load);
 }
 
 int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_stream_t stream)
@@ -215,6 +253,7 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     int rc = check_cache(ctx, c);
     if (rc) return rc;
     if (!q) return fail(ctx, DRO_EINVAL, "rows is NULL");
+    if (is_mx(c->dtype)) return fail(ctx, DRO_EINVAL, "cache type %d is not read by kv_attention", c->dtype);
     if ((rc = check_dtype(ctx, q->dtype, c))) return rc;
     if (q->Hq <= 0 || q->Hq % c->heads)
         return fail(ctx, DRO_EINVAL, "Hq=%d is not a multiple of the cache's %d heads", q->Hq, c->heads);

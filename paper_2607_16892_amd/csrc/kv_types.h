@@ -13,6 +13,22 @@ typedef _Float16 f16;
 struct fp8 {  // e4m3 with one NaN and no infinity (largest finite value 448)
     uint8_t bits;
 };
+// Shared scales: kGroup components of a row share a power of two, 2^(byte - 127), and are 4-bit
+// codes (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign; the even component in a byte's low half) or fp8.
+struct mx4 {
+    uint8_t pair;
+};
+struct mx8 {
+    uint8_t bits;
+};
+constexpr int kGroup = 32;
+template <class C> constexpr bool kMx = __is_same(C, mx4) || __is_same(C, mx8);
+
+// bytes of n components (mx4: n is even)
+template <class C, class N> __host__ __device__ constexpr N bytes_of(N n)
+{
+    return __is_same(C, mx4) ? n / 2 : n * (N)sizeof(C);
+}
 
 template <class T, int N> using Vec = T __attribute__((ext_vector_type(N)));
 
@@ -36,6 +52,43 @@ template <class T, bool kHigh> __device__ __forceinline__ uint32_t unpack_fp8(ui
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHigh));
     else
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHigh));
+}
+
+// Pair kPair of the components in a dword of codes of scale `s`, as packed T: exact in bf16 (in f16
+// rounded, infinite beyond its range), NaN where the group's byte is 255.
+__device__ __forceinline__ float group_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+template <class T, class C, int kPair> __device__ __forceinline__ uint32_t unpack_mx(uint32_t w, float s)
+{
+    if constexpr (__is_same(C, mx4)) {
+        if constexpr (__is_same(T, bf16))
+            return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, kPair));
+        else
+            return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, kPair));
+    } else {
+        if constexpr (__is_same(T, bf16))
+            return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, kPair));
+        else
+            return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, kPair));
+    }
+}
+// Eight components, in one dword of mx4 or two of mx8, as packed T.
+template <class T, class C> __device__ __forceinline__ Vec<uint32_t, 4> unpack_mx8of(const uint32_t *w, float s)
+{
+    if constexpr (__is_same(C, mx4))
+        return Vec<uint32_t, 4>{unpack_mx<T, C, 0>(w[0], s), unpack_mx<T, C, 1>(w[0], s), unpack_mx<T, C, 2>(w[0], s),
+                                unpack_mx<T, C, 3>(w[0], s)};
+    else
+        return Vec<uint32_t, 4>{unpack_mx<T, C, 0>(w[0], s), unpack_mx<T, C, 1>(w[0], s), unpack_mx<T, C, 0>(w[1], s),
+                                unpack_mx<T, C, 1>(w[1], s)};
+}
+
+// component d of a row of codes, as T
+template <class T, class C> __device__ __forceinline__ float mx_value_at(const char *row, const uint8_t *powers, int d)
+{
+    const uint32_t w = ((const uint8_t *)row)[bytes_of<C>(d & ~1)] |
+                       (__is_same(C, mx8) ? (uint32_t)((const uint8_t *)row)[d | 1] << 8 : 0u);
+    const uint32_t pair = unpack_mx<T, C, 0>(w, group_scale(powers[d / kGroup]));
+    return to_float(__builtin_bit_cast(T, (uint16_t)(pair >> (d & 1) * 16)));
 }
 
 // component d of a value row of the cache

@@ -1,4 +1,4 @@
-"""Binding of the paged-cache entry points (block tables, store, attention;
+"""Binding of the paged-cache entry points (block tables, store, load, attention;
 include/dro.h).  Argument checks and marshalling only."""
 from __future__ import annotations
 
@@ -130,23 +130,43 @@ class BlockPool:
             _need(self.free, torch.int32, "free", dev, 1))
 
 
+MXFP4, MXFP8 = 3, 4
+_GROUP = 32  # components that share a power of two
+
+
 @dataclass(frozen=True)
 class KvCache:
     """One layer's cache (field meanings as in dro_kv_cache): k and v are
     [num_blocks, block, heads, dim] tensors, strided as they like except for the
     contiguous components, in torch.bfloat16, torch.float16 or, with scales,
-    torch.float8_e4m3fn.  The tensors are checked once, here, and stay the cache's."""
+    torch.float8_e4m3fn.  With k_power and v_power, uint8 [num_blocks, block, heads,
+    dim / 32] whose groups lie next to one another, the cache is in shared scales: MXFP8 if
+    k and v are torch.float8_e4m3fn, MXFP4 if they are torch.uint8 [.., dim / 2], two
+    components a byte.  The tensors are checked once, here, and stay the cache's."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: Optional[torch.Tensor] = None   # float32 [heads]
     v_scale: Optional[torch.Tensor] = None
+    k_power: Optional[torch.Tensor] = None
+    v_power: Optional[torch.Tensor] = None
 
     @classmethod
     def empty(cls, num_blocks, block, heads, dim, dtype=torch.bfloat16, device="cuda",
               k_scale=None, v_scale=None):
-        """A zeroed cache whose blocks hold the tokens of a head next to one another."""
-        k, v = (torch.zeros((num_blocks, heads, block, dim), dtype=dtype, device=device)
-                .permute(0, 2, 1, 3) for _ in range(2))
+        """A zeroed cache whose blocks hold the tokens of a head next to one another; dtype is a
+        torch one, "mxfp4" or "mxfp8"."""
+        def zeros(width, t):
+            return torch.zeros((num_blocks, heads, block, width), dtype=t, device=device).permute(0, 2, 1, 3)
+
+        if dtype in ("mxfp4", "mxfp8"):
+            if k_scale is not None or v_scale is not None:
+                raise ValueError(f"{dtype} has no k_scale and v_scale")
+            if dim % _GROUP:
+                raise ValueError(f"dim={dim} is not a multiple of {_GROUP}, as {dtype} needs")
+            code = (dim // 2, torch.uint8) if dtype == "mxfp4" else (dim, torch.float8_e4m3fn)
+            return cls(zeros(*code), zeros(*code), k_power=zeros(dim // _GROUP, torch.uint8),
+                       v_power=zeros(dim // _GROUP, torch.uint8))
+        k, v = zeros(dim, dtype), zeros(dim, dtype)
         if dtype == torch.float8_e4m3fn:
             one = torch.ones(heads, dtype=torch.float32, device=device)
             k_scale = one if k_scale is None else k_scale
@@ -165,11 +185,21 @@ class KvCache:
     def dim(self) -> int:
         return self._struct.dim
 
+    @property
+    def tensors(self) -> tuple:
+        """The tensors that it is made of."""
+        return tuple(t for t in (self.k, self.v, self.k_scale, self.v_scale, self.k_power, self.v_power)
+                     if t is not None)
+
     def __post_init__(self):
+        mx = self.k_power is not None or self.v_power is not None
         for name, t in (("k", self.k), ("v", self.v)):
             if not isinstance(t, torch.Tensor) or not t.is_cuda:
                 raise TypeError(f"cache {name} must be a CUDA tensor")
-            if t.dtype not in DTYPES:
+            if mx and t.dtype not in (torch.uint8, torch.float8_e4m3fn):
+                raise TypeError(f"cache {name} must be uint8 (MXFP4) or float8_e4m3fn (MXFP8) beside its "
+                                f"powers, got {t.dtype}")
+            if not mx and t.dtype not in DTYPES:
                 raise TypeError(f"cache {name} must be bfloat16, float16 or float8_e4m3fn, got {t.dtype}")
             if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
                 raise ValueError(f"cache {name} must be [num_blocks, block, heads, dim] with "
@@ -177,18 +207,34 @@ class KvCache:
         if self.v.shape != self.k.shape or self.v.dtype != self.k.dtype or self.v.device != self.k.device:
             raise ValueError("cache k and v differ in shape, type or device")
         s = _native.KvCacheStruct()
-        s.dtype = DTYPES[self.k.dtype]
+        four = self.k.dtype is torch.uint8
+        s.dtype = DTYPES[self.k.dtype] if not mx else MXFP4 if four else MXFP8
         s.num_blocks, s.block, s.heads, s.dim = self.k.shape
         s.k, s.v = self.k.data_ptr(), self.v.data_ptr()
-        s.k_block, s.k_token, s.k_head = self.k.stride()[:3]
-        s.v_block, s.v_token, s.v_head = self.v.stride()[:3]
+        of = 2 if four else 1  # (strides are in components)
+        s.dim *= of
+        s.k_block, s.k_token, s.k_head = (of * x for x in self.k.stride()[:3])
+        s.v_block, s.v_token, s.v_head = (of * x for x in self.v.stride()[:3])
+        if mx:
+            if s.dim % _GROUP:
+                raise ValueError(f"dim={s.dim} is not a multiple of {_GROUP}, as shared scales need")
+            shape = tuple(self.k.shape[:3]) + (s.dim // _GROUP,)
+            for name in ("k_power", "v_power"):
+                t = getattr(self, name)
+                if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or t.device != self.k.device:
+                    raise TypeError(f"{name} must be a uint8 tensor on {self.k.device}")
+                if tuple(t.shape) != shape or (shape[3] > 1 and t.stride(3) != 1):
+                    raise ValueError(f"{name} must have shape {shape} with the groups of a row next to "
+                                     f"one another, got {tuple(t.shape)}")
+            s.k_power, s.v_power = self.k_power.data_ptr(), self.v_power.data_ptr()
+            s.k_power_block, s.k_power_token, s.k_power_head = self.k_power.stride()[:3]
+            s.v_power_block, s.v_power_token, s.v_power_head = self.v_power.stride()[:3]
         for name in ("k_scale", "v_scale"):
             t = getattr(self, name)
             if t is not None:
                 setattr(s, name, _need(t, torch.float32, name, self.k.device, s.heads))
         object.__setattr__(self, "_struct", s)
-        object.__setattr__(self, "_grad", any(t is not None and t.requires_grad for t in
-                                              (self.k, self.v, self.k_scale, self.v_scale)))
+        object.__setattr__(self, "_grad", any(t.requires_grad for t in self.tensors))
 
     def struct(self) -> _native.KvCacheStruct:
         return self._struct
@@ -252,7 +298,46 @@ def kv_store(ctx: Context, cache: KvCache, k: torch.Tensor, v: torch.Tensor, slo
     if rc:
         ctx.check(rc, "kv_store")
     if stream is not None:
-        _share(stream, dev, cache.k, cache.v, cache.k_scale, cache.v_scale, k, v, slot)
+        _share(stream, dev, *cache.tensors, k, v, slot)
+
+
+def kv_load(ctx: Context, cache: KvCache, slot: torch.Tensor, dtype=None, k=None, v=None,
+            stream=None) -> dict:
+    """The keys and values of the slots [T] out of the cache, as rows [T, heads, dim] (see kv_load
+    in dro.h): of torch.bfloat16 or torch.float16, a 16-bit cache of its own type (the default; of
+    a cache of 8 or 4 bits torch.bfloat16).  k and v are written if given, strided as kv_store's.
+    No backward pass: inputs that require grad are refused where gradients are recorded."""
+    dev, cs = cache.device, cache._struct
+    if dev.index != ctx.device.index:
+        _other_device(ctx, dev)
+    if not isinstance(slot, torch.Tensor):
+        raise TypeError("slot must be a CUDA tensor")
+    T = slot.numel()
+    if dtype is None:
+        given = k if k is not None else v
+        dtype = (given.dtype if given is not None else
+                 torch.bfloat16 if cs.dtype not in (0, 1) else cache.k.dtype)
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        raise TypeError(f"dtype must be torch.bfloat16 or torch.float16, got {dtype}")
+    slot_p = _need(slot, torch.int64, "slot", dev, T)
+    with nullcontext() if stream is None else torch.cuda.stream(stream):
+        out = []
+        for name, t in (("k", k), ("v", v)):
+            if t is None:
+                t = torch.empty((T, cs.heads, cs.dim), dtype=dtype, device=dev)
+            elif t.dtype is not dtype or t.shape[:1] != (T,):
+                raise ValueError(f"{name} must hold {T} rows of {dtype}")
+            out.append((t, _need_rows(t, name, dev, cs.heads, cs.dim)[1]))
+    (k, ks), (v, vs) = out
+    if k.requires_grad or v.requires_grad or cache._grad:
+        _no_gradient("kv_load")
+    rc = ctx._lib.kv_load(ctx.handle, ct.byref(cs), DTYPES[dtype], T, k.data_ptr(), ks[0], ks[1],
+                          v.data_ptr(), vs[0], vs[1], slot_p, _queue(stream, dev))
+    if rc:
+        ctx.check(rc, "kv_load")
+    if stream is not None:
+        _share(stream, dev, *cache.tensors, k, v, slot)
+    return dict(k=k, v=v)
 
 
 def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Tensor,
@@ -301,6 +386,5 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     if rc:
         ctx.check(rc, "kv_attention")
     if stream is not None:
-        _share(stream, dev, cache.k, cache.v, cache.k_scale, cache.v_scale, q, table, start, context,
-               slopes, prefix, out, lse)
+        _share(stream, dev, *cache.tensors, q, table, start, context, slopes, prefix, out, lse)
     return dict(out=out, lse=lse)
