@@ -59,6 +59,8 @@ struct KvAttnArgs {
     const void *k, *v;
     int64_t k_block, k_token, k_head, v_block, v_token, v_head;
     const float *k_scale, *v_scale;  // fp8 caches
+    const uint8_t *k_power, *v_power;  // caches in shared scales
+    int64_t kp_block, kp_token, kp_head, vp_block, vp_token, vp_head;
     float scale, cap;
     int window;
     const float *slopes;

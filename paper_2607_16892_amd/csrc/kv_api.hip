@@ -253,7 +253,6 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     int rc = check_cache(ctx, c);
     if (rc) return rc;
     if (!q) return fail(ctx, DRO_EINVAL, "rows is NULL");
-    if (is_mx(c->dtype)) return fail(ctx, DRO_EINVAL, "cache type %d is not read by kv_attention", c->dtype);
     if ((rc = check_dtype(ctx, q->dtype, c))) return rc;
     if (q->Hq <= 0 || q->Hq % c->heads)
         return fail(ctx, DRO_EINVAL, "Hq=%d is not a multiple of the cache's %d heads", q->Hq, c->heads);
@@ -301,6 +300,16 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_
     a.v_head = c->v_head;
     a.k_scale = c->k_scale;
     a.v_scale = c->v_scale;
+    if (is_mx(c->dtype)) {
+        a.k_power = c->k_power;
+        a.v_power = c->v_power;
+        a.kp_block = c->k_power_block;
+        a.kp_token = c->k_power_token;
+        a.kp_head = c->k_power_head;
+        a.vp_block = c->v_power_block;
+        a.vp_token = c->v_power_token;
+        a.vp_head = c->v_power_head;
+    }
     a.scale = q->scale;
     a.cap = q->softcap;
     // a window as long as the table hides nothing

@@ -14,6 +14,8 @@
 // the kernel, and 5.2 from 128 requests of 1000 to 16,384 keys in 8 bits.)
 #pragma once
 
+#include <type_traits>
+
 #include "kv_math.h"
 #include "kv_sched.h"
 
@@ -27,20 +29,33 @@ constexpr int kDecodeRows = 16;
 // two, 8 bits 117 and 129.
 constexpr int decode_waves(int DP, int E) { return DP == 256 ? 1 : DP * E >= 256 ? 2 : DP * E >= 128 ? 3 : 4; }
 
+// Caches in shared scales.  A lane reads 16 bytes of a key row at a time, so its codes of 4 bits are
+// one whole group (with 64 components half of one), of 8 bits half a group: one power a read.  They
+// are widened by one instruction a pair that takes the power as well, to exactly what they stand
+// for (in f16 rounded), and from there on are values of T like any other.
+
 template <class T, class C, int DP, bool FULL>
 __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decode_kernel(
     const KvAttnArgs a, const KvCut cut, const uint64_t *sums, bool pad, float *part_o, float2 *part_ml,
     KvJoin *joins)
 {
-    constexpr int E = sizeof(C);
     constexpr int S = DP / 32;             // steps of 32 components of a score
     constexpr int VW = DP / 16;            // components a lane reads of a value row
-    constexpr bool F8 = sizeof(C) == 1;
-    constexpr int KWords = F8 ? S * 2 : S * 4;   // dwords a lane reads of a key row
-    constexpr int VWords = F8 ? VW / 4 : VW / 2; // and of a value row
+    constexpr bool F8 = __is_same(C, fp8), MX = kMx<C>, FOUR = __is_same(C, mx4);
+    constexpr int KWords = FOUR ? S : sizeof(C) == 1 ? S * 2 : S * 4;  // dwords a lane reads of a key row
+    constexpr int VWords = F8 ? VW / 4 : VW / 2;  // and of a value row (shared scales: widened to T)
+    constexpr int KReads = FOUR ? (S + 3) / 4 : S / 2;  // shared scales: reads of a key row, a power each
+    constexpr int VRaw = FOUR ? (VW + 7) / 8 : VW / 4;  // and dwords of a value row before they are widened
+    using VC = std::conditional_t<MX, T, C>;            // what the values' dwords hold
     __shared__ KvLds lds;
 
     const int lane = threadIdx.x, n16 = lane & 15, grp = lane >> 4;
+    // the first of the 8 components that this lane multiplies in step x of a score
+    auto component = [&](int x) {
+        if constexpr (FOUR) return DP == 64 ? grp * 16 + x * 8 : (x >> 2) * 128 + grp * 32 + (x & 3) * 8;
+        else if constexpr (F8 || MX) return (x >> 1) * 64 + grp * 16 + (x & 1) * 8;
+        else return x * 32 + grp * 8;
+    };
 
     KvSched sched;
     sched.init(a, cut, sums, lds);
@@ -80,7 +95,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             const char *p = (const char *)a.q + 2 * ((int64_t)(it.first_token + token) * a.q_token + hq * a.q_head);
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                const int d = F8 ? (s >> 1) * 64 + grp * 16 + (s & 1) * 8 : s * 32 + grp * 8;
+                const int d = component(s);
                 q[s] = FULL || d < a.D ? *(const u32x4 *)(p + 2 * d) : u32x4{0, 0, 0, 0};
             }
         }
@@ -91,11 +106,11 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         const float cap = a.cap * kLog2e, to_exp = a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
         const int p_row = it.ctx - it.n + token;
 
-        const char *kp = (const char *)a.k + (int64_t)h * a.k_head * E;
-        const char *vp = (const char *)a.v + (int64_t)h * a.v_head * E;
+        const char *kp = (const char *)a.k + bytes_of<C>((int64_t)h * a.k_head);
+        const char *vp = (const char *)a.v + bytes_of<C>((int64_t)h * a.v_head);
         const int in_block = (1 << a.shift) - 1;
-        const uint32_t k_lane = (uint32_t)(n16 * (int)a.k_token + (F8 ? grp * 16 : grp * 8)) * E;
-        const uint32_t v_lane = (uint32_t)(grp * 4 * (int)a.v_token + n16 * VW) * E;
+        const uint32_t k_lane = bytes_of<C>((uint32_t)(n16 * (int)a.k_token + component(0)));
+        const uint32_t v_lane = bytes_of<C>((uint32_t)(grp * 4 * (int)a.v_token + n16 * VW));
         const int32_t *table = a.table + (int64_t)r * a.table_stride;
 
         float m = -INFINITY, l = 0.0f;
@@ -111,17 +126,36 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             const int key = k0 + (u + (lane >> 1)) * kStepKeys + (lane & 1) * 16;
             ids = min(max(table[min(key, k1 - 1) >> a.shift], 0), a.num_blocks - 1);
         };
-        auto base_of = [&](const char *p, int64_t block_stride, int64_t token_stride, int u, int t) {
+        auto place_of = [&](int64_t block_stride, int64_t token_stride, int u, int t) {
             const int id = __builtin_amdgcn_readlane(ids, 2 * (u & 31) + t);
             const int key = k0 + u * kStepKeys + t * 16;
-            return p + ((int64_t)id * block_stride + (int64_t)(key & in_block) * token_stride) * E;
+            return (int64_t)id * block_stride + (int64_t)(key & in_block) * token_stride;
+        };
+        auto base_of = [&](const char *p, int64_t block_stride, int64_t token_stride, int u, int t) {
+            return p + bytes_of<C>(place_of(block_stride, token_stride, u, t));
         };
         Words<KWords> k[2];
+        uint32_t k_pow[MX ? 2 : 1][MX ? KReads : 1];
         auto load_k = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const char *p = base_of(kp, a.k_block, a.k_token, u, t);
-                if constexpr (FULL) {
+                if constexpr (MX) {
+                    constexpr int N = KWords / KReads;
+                    const uint8_t *pw = a.k_power + h * a.kp_head + place_of(a.kp_block, a.kp_token, u, t);
+#pragma unroll
+                    for (int x = 0; x < KReads; ++x) {
+                        const int d = component(x * (S / KReads));
+                        Words<N> y{};
+                        k_pow[t][x] = 127;
+                        if (FULL || d < a.D) {
+                            y = load_words<N>(p + x * 64, k_lane);
+                            k_pow[t][x] = pw[(uint32_t)(n16 * (int)a.kp_token + d / kGroup)];
+                        }
+#pragma unroll
+                        for (int j = 0; j < N; ++j) k[t].w[N * x + j] = y.w[j];
+                    }
+                } else if constexpr (FULL) {
                     constexpr int L = F8 ? S / 2 : S;  // 16-byte loads
 #pragma unroll
                     for (int s = 0; s < L; ++s) {
@@ -133,7 +167,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
                         constexpr int N = F8 ? 2 : 4;
-                        const int d = F8 ? (s >> 1) * 64 + grp * 16 + (s & 1) * 8 : s * 32 + grp * 8;
+                        const int d = component(s);
                         Words<N> x{};
                         if (d < a.D) x = load_words<N>(p + (F8 ? (s >> 1) * 64 + (s & 1) * 8 : s * 64), k_lane);
 #pragma unroll
@@ -151,21 +185,34 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             const int key0 = k0 + u * kStepKeys;
             const bool edge = key0 < all_lo || key0 + kStepKeys > min(all_hi, k1);
             Words<VWords> v[8];
+            Words<MX ? VRaw : 1> raw[MX ? 8 : 1];
+            uint32_t v_pow[MX ? 8 : 1];
             auto load_v = [&]() {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const char *p = base_of(vp, a.v_block, a.v_token, u, t);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const char *at = p + (int64_t)i * a.v_token * E;
-                        if constexpr (FULL) {
+                        const char *at = p + bytes_of<C>((int64_t)i * a.v_token);
+                        if constexpr (MX) {
+                            const uint8_t *pw = a.v_power + h * a.vp_head + place_of(a.vp_block, a.vp_token, u, t) +
+                                                i * a.vp_token;
+                            Words<VRaw> &y = raw[t * 4 + i];
+                            y = Words<VRaw>{};
+                            v_pow[t * 4 + i] = 127;
+                            if (FULL || n16 * VW < a.D) {
+                                if constexpr (FOUR && VW == 4) y.w[0] = *(const uint16_t *)(at + v_lane);
+                                else y = load_words<VRaw>(at, v_lane);
+                                v_pow[t * 4 + i] = pw[(uint32_t)(grp * 4 * (int)a.vp_token + n16 * VW / kGroup)];
+                            }
+                        } else if constexpr (FULL) {
                             v[t * 4 + i] = load_words<VWords>(at, v_lane);
                         } else {
                             constexpr int N = F8 ? 2 : 4, P = VWords < N ? VWords : N;
 #pragma unroll
                             for (int x = 0; x < VWords; x += P) {
                                 Words<P> y{};
-                                if (n16 * VW + x * (4 / E) < a.D) y = load_words<P>(at + 4 * x, v_lane);
+                                if (n16 * VW + x * (F8 ? 4 : 2) < a.D) y = load_words<P>(at + 4 * x, v_lane);
 #pragma unroll
                                 for (int j = 0; j < P; ++j) v[t * 4 + i].w[x + j] = y.w[j];
                             }
@@ -182,7 +229,10 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
 #pragma unroll
                 for (int x = 0; x < S; ++x) {
                     u32x4 kf;
-                    if constexpr (F8) {
+                    if constexpr (MX) {
+                        const float ps = group_scale(k_pow[t][x / (S / KReads)]);
+                        kf = unpack_mx8of<T, C>(&k[t].w[x * KWords / S], ps);
+                    } else if constexpr (F8) {
                         kf = u32x4{unpack_fp8<T, false>(k[t].w[2 * x]), unpack_fp8<T, true>(k[t].w[2 * x]),
                                    unpack_fp8<T, false>(k[t].w[2 * x + 1]), unpack_fp8<T, true>(k[t].w[2 * x + 1])};
                     } else {
@@ -235,6 +285,23 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             }
             const u32x4 w = {pack2<T>(e[0], e[1]), pack2<T>(e[2], e[3]), pack2<T>(e[4], e[5]), pack2<T>(e[6], e[7])};
 
+            if constexpr (MX) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float ps = group_scale(v_pow[i]);
+                    if constexpr (VW == 4) {
+                        v[i].w[0] = unpack_mx<T, C, 0>(raw[i].w[0], ps);
+                        v[i].w[1] = unpack_mx<T, C, 1>(raw[i].w[0], ps);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < VW / 8; ++j) {
+                            const u32x4 y = unpack_mx8of<T, C>(&raw[i].w[j * VRaw * 8 / VW], ps);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) v[i].w[4 * j + c] = y[c];
+                        }
+                    }
+                }
+            }
             if (edge) {
                 // a weight of zero does not silence an infinity or a NaN: values that no row of
                 // the tile sees become zero, and those that some see are added after the last
@@ -247,7 +314,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
 #pragma unroll
                     for (int j = 0; j < VWords; ++j) {
                         v[i].w[j] = keep ? v[i].w[j] : 0;
-                        odd |= nonfinite_mask<C>(v[i].w[j]);
+                        odd |= nonfinite_mask<VC>(v[i].w[j]);
                     }
                 }
                 if (__any(odd)) {
@@ -255,7 +322,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int j = 0; j < VWords; ++j) v[i].w[j] &= ~nonfinite_mask<C>(v[i].w[j]);
+                        for (int j = 0; j < VWords; ++j) v[i].w[j] &= ~nonfinite_mask<VC>(v[i].w[j]);
                 }
             }
             // V^T: dword y of column j holds rows 2y and 2y + 1
@@ -298,8 +365,14 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
                 if (step >= all_lo && step + kStepKeys <= min(all_hi, k1)) continue;  // not zeroed
                 const bool seen = key >= see.lo && key < see.hi;
                 const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
-                const char *at = vp + (id * a.v_block + (int64_t)(key & in_block) * a.v_token) * E;
-                if (!row_nonfinite<C>(at, a.D * E)) continue;
+                const char *at = vp + bytes_of<C>(id * a.v_block + (int64_t)(key & in_block) * a.v_token);
+                const uint8_t *pw = nullptr;
+                if constexpr (MX) {
+                    pw = a.v_power + id * a.vp_block + (int64_t)(key & in_block) * a.vp_token + h * a.vp_head;
+                    if (!mx_row_nonfinite<T, C>(at, pw, a.D)) continue;
+                } else {
+                    if (!row_nonfinite<C>(at, bytes_of<C>(a.D))) continue;
+                }
                 int D = a.D;
                 asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
 #pragma unroll
@@ -307,7 +380,9 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
 #pragma unroll
                     for (int j = 0; j < VW; ++j) {
                         const int d = VW * (grp * 4 + c) + j;
-                        const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
+                        float y;
+                        if constexpr (MX) y = mx_value_at<T, C>(at, pw, FULL ? d : min(d, D - 1));
+                        else y = value_at<C>(at, FULL ? d : min(d, D - 1));
                         if (seen && !__builtin_isfinite(y)) o[j][c] += y;
                         __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
                     }
@@ -376,6 +451,8 @@ void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums,
                       bool pad, float *o, float2 *ml, KvJoin *joins, hipStream_t st)
 {
     if (cache_dtype == DRO_FP8_E4M3) run_kv_decode<T, fp8>(a, c, sums, DP, pad, o, ml, joins, st);
+    else if (cache_dtype == DRO_MXFP4) run_kv_decode<T, mx4>(a, c, sums, DP, pad, o, ml, joins, st);
+    else if (cache_dtype == DRO_MXFP8) run_kv_decode<T, mx8>(a, c, sums, DP, pad, o, ml, joins, st);
     else run_kv_decode<T, T>(a, c, sums, DP, pad, o, ml, joins, st);
 }
 

@@ -96,6 +96,14 @@ template <class C> __device__ __forceinline__ bool row_nonfinite(const char *p, 
     return __any(bad);
 }
 
+// The same of a row of codes in shared scales, as T: an infinity beyond f16's range, or a NaN.
+template <class T, class C> __device__ __forceinline__ bool mx_row_nonfinite(const char *p, const uint8_t *powers, int D)
+{
+    bool bad = false;
+    for (int d = threadIdx.x & 63; d < D; d += 64) bad |= !__builtin_isfinite(mx_value_at<T, C>(p, powers, d));
+    return __any(bad);
+}
+
 // N dwords at base + off, aligned to 8 elements of the cache's type: the base is the same
 // for the wave, so an address costs no 64-bit vector arithmetic.
 template <int N> struct Words {

@@ -103,9 +103,10 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     const KvAttnArgs a, const KvCut cut, const KvTiles tiles, bool pad, float *part_o, float2 *part_ml,
     KvJoin *joins)
 {
-    constexpr int E = sizeof(C);
-    constexpr bool F8 = E == 1;
-    constexpr bool LEAN = MODS || F8 || DP == 256;  // places in LDS and memory are not kept over the steps
+    constexpr bool F8 = __is_same(C, fp8), MX = kMx<C>;
+    constexpr bool REG = F8 || MX;  // widened on the way to LDS, through registers
+    constexpr int PW = __is_same(C, mx4) ? 1 : 2;  // dwords of a piece then
+    constexpr bool LEAN = MODS || REG || DP == 256;  // places in LDS and memory are not kept over the steps
     constexpr int KT = prefill_keys(DP);
     constexpr int S = DP / 16;           // steps of 16 components of a score
     // keys whose scores are in registers at once: 128 beside the changes of the scores spill
@@ -213,7 +214,8 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             for (int j = 0; j < UP; ++j)
                 ids[j] = table[min(k0 + u * KT + (wave + 4 * j) % NG * 16, k1 - 1) >> a.shift];
         };
-        Words<2> reg[F8 ? UP * IP : 1];
+        Words<PW> reg[REG ? UP * IP : 1];
+        uint32_t power[MX ? UP * IP : 1];
         auto load = [&](auto odd_tile, int u) {
             int lane = threadIdx.x & 63;
             if constexpr (LEAN) asm volatile("" : "+v"(lane));  // (see `fresh`)
@@ -222,19 +224,26 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const bool vals = (wave + 4 * j) / NG;
                 const int group = (wave + 4 * j) % NG;
                 const int64_t s_token = vals ? a.v_token : a.k_token;
-                const char *base = (vals ? (const char *)a.v + h * a.v_head * E : (const char *)a.k + h * a.k_head * E) +
-                                   ((int64_t)min(max(ids[j], 0), a.num_blocks - 1) * (vals ? a.v_block : a.k_block) +
-                                    ((k0 + u * KT + group * 16) & in_block) * s_token) * E;
+                const int64_t id = min(max(ids[j], 0), a.num_blocks - 1);
+                const int in = (k0 + u * KT + group * 16) & in_block;
+                const char *base = (vals ? (const char *)a.v + bytes_of<C>(h * a.v_head) : (const char *)a.k + bytes_of<C>(h * a.k_head)) +
+                                   bytes_of<C>(id * (vals ? a.v_block : a.k_block) + in * s_token);
+                const int64_t p_token = vals ? a.vp_token : a.kp_token;
+                const uint8_t *pw = nullptr;
+                if constexpr (MX)
+                    pw = vals ? a.v_power + h * a.vp_head + id * a.vp_block + in * p_token
+                              : a.k_power + h * a.kp_head + id * a.kp_block + in * p_token;
 #pragma unroll
                 for (int i = 0; i < IP; ++i) {
                     const int rr = i * RP + lane / NC;
                     const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
-                    const uint32_t off = (uint32_t)(lane / NC * (int)s_token + c * 8) * E;
-                    const char *p = base + i * RP * s_token * E;
+                    const uint32_t off = bytes_of<C>((uint32_t)(lane / NC * (int)s_token + c * 8));
+                    const char *p = base + bytes_of<C>(i * RP * s_token);
                     if (FULL || c * 8 < a.D) {
-                        if constexpr (F8)
-                            reg[j * IP + i] = load_words<2>(p, off);
-                        else if (vals)
+                        if constexpr (REG) reg[j * IP + i] = load_words<PW>(p, off);
+                        if constexpr (MX) power[j * IP + i] = pw[i * RP * p_token + (uint32_t)(lane / NC * (int)p_token + c / 4)];
+                        if constexpr (REG) continue;
+                        if (vals)
                             __builtin_amdgcn_global_load_lds(
                                 (GlobalPtr)(p + off),
                                 (LdsPtr)((decltype(odd_tile)::value ? v_odd : v_even) + group * 16 * Row + i * 1024), 16, 0, 0);
@@ -246,23 +255,27 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 }
             }
         };
-        auto store = [&](auto odd_tile) {  // fp8: widened on the way
-            if constexpr (F8) {
+        auto store = [&](auto odd_tile) {  // fewer bits: widened on the way
+            if constexpr (REG) {
 #pragma unroll
                 for (int j = 0; j < UP; ++j) {
                     const bool vals = (wave + 4 * j) / NG;
                     const int group = (wave + 4 * j) % NG;
 #pragma unroll
                     for (int i = 0; i < IP; ++i) {
-                        const Words<2> &x = reg[j * IP + i];
+                        const Words<PW> &x = reg[j * IP + i];
                         const int rr = i * RP + lane / NC;
                         const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
-                        if (FULL || c * 8 < a.D)
+                        if (FULL || c * 8 < a.D) {
+                            u32x4 y;
+                            if constexpr (MX) y = unpack_mx8of<T, C>(x.w, group_scale(power[j * IP + i]));
+                            else
+                                y = u32x4{unpack_fp8<T, false>(x.w[0]), unpack_fp8<T, true>(x.w[0]),
+                                          unpack_fp8<T, false>(x.w[1]), unpack_fp8<T, true>(x.w[1])};
                             *(u32x4 *)((vals ? (decltype(odd_tile)::value ? v_odd : v_even)
                                               : (decltype(odd_tile)::value ? k_odd : k_even)) +
-                                        group * 16 * Row + i * 1024 + lane * 16) =
-                                u32x4{unpack_fp8<T, false>(x.w[0]), unpack_fp8<T, true>(x.w[0]),
-                                      unpack_fp8<T, false>(x.w[1]), unpack_fp8<T, true>(x.w[1])};
+                                        group * 16 * Row + i * 1024 + lane * 16) = y;
+                        }
                     }
                 }
             }
@@ -474,9 +487,15 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 if (k0 + at_step >= bot.lo && k0 + at_step + KT <= top.hi) continue;  // not zeroed
                 const bool seen = key >= see.lo && key < see.hi;
                 const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
-                const char *at = (const char *)a.v +
-                                 (id * a.v_block + (int64_t)(key & in_block) * a.v_token + (int64_t)h * a.v_head) * E;
-                if (!row_nonfinite<C>(at, a.D * E)) continue;
+                const char *at = (const char *)a.v + bytes_of<C>(id * a.v_block + (int64_t)(key & in_block) * a.v_token +
+                                                                 (int64_t)h * a.v_head);
+                const uint8_t *pw = nullptr;
+                if constexpr (MX) {
+                    pw = a.v_power + id * a.vp_block + (int64_t)(key & in_block) * a.vp_token + h * a.vp_head;
+                    if (!mx_row_nonfinite<T, C>(at, pw, a.D)) continue;
+                } else {
+                    if (!row_nonfinite<C>(at, bytes_of<C>(a.D))) continue;
+                }
                 int D = a.D;
                 asm volatile("" : "+s"(D));  // compared with anew: 64 addresses would not fit
 #pragma unroll
@@ -484,7 +503,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-                        const float y = value_at<C>(at, FULL ? d : min(d, D - 1));
+                        float y;
+                        if constexpr (MX) y = mx_value_at<T, C>(at, pw, FULL ? d : min(d, D - 1));
+                        else y = value_at<C>(at, FULL ? d : min(d, D - 1));
                         if (seen && !__builtin_isfinite(y)) o[j][i] += y;
                         __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
                     }
@@ -545,10 +566,15 @@ template <class T>
 void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
                        float *o, float2 *ml, KvJoin *joins, hipStream_t st)
 {
-    const bool f8 = cache_dtype == DRO_FP8_E4M3;
-    if (DP == 64) (f8 ? run_kv_prefill<T, fp8, 64> : run_kv_prefill<T, T, 64>)(a, c, t, grid, pad, o, ml, joins, st);
-    else if (DP == 128) (f8 ? run_kv_prefill<T, fp8, 128> : run_kv_prefill<T, T, 128>)(a, c, t, grid, pad, o, ml, joins, st);
-    else (f8 ? run_kv_prefill<T, fp8, 256> : run_kv_prefill<T, T, 256>)(a, c, t, grid, pad, o, ml, joins, st);
+    auto run = [&](auto c0) {
+        using C = decltype(c0);
+        (DP == 64 ? run_kv_prefill<T, C, 64> : DP == 128 ? run_kv_prefill<T, C, 128> : run_kv_prefill<T, C, 256>)(
+            a, c, t, grid, pad, o, ml, joins, st);
+    };
+    if (cache_dtype == DRO_FP8_E4M3) run(fp8{});
+    else if (cache_dtype == DRO_MXFP4) run(mx4{});
+    else if (cache_dtype == DRO_MXFP8) run(mx8{});
+    else run(T{});
 }
 
 }  // namespace dro
