@@ -47,7 +47,7 @@
  *    correctly.  A replay uses the ctx's workspace and staged offsets as they
  *    are then: after any call on that ctx with another problem or on another
  *    stream, capture again.  (dro_cost_eval_noalloc has no such bond to its ctx.)
- *    kv_block_tables, kv_store, kv_load and kv_attention enqueue kernels only as well, once
+ *    the calls of the paged cache (kv_*) enqueue kernels only as well, once
  *    a call on the ctx has needed as large a workspace (one that has to grow it under
  *    capture is DRO_EHIP and enqueues nothing).  The workspace that a captured
  *    call was given stays until dro_destroy, whatever later calls need, so their
@@ -577,6 +577,32 @@ typedef struct {
 
 int kv_attention(dro_ctx *ctx, const dro_kv_cache *cache, const dro_kv_rows *rows,
                  dro_stream_t stream);
+
+/* The same behind shared prefixes, which the cache holds once for each group of requests
+ * (a system prompt, a document, a class's L_pre tokens) and the call reads once for the
+ * group.  Group g is the requests first[g] .. first[g+1] - 1 (requests before first[0] and
+ * from first[groups] on have no prefix); its S = context[g] shared tokens lie in the blocks of
+ * its own table row, at positions 0 .. S-1 of each of its requests, whose own tokens (their
+ * context, table and new rows, as in kv_attention) follow at S, S+1, ...  So row i of request r is
+ * at position p = S + rows.context[r] - n + i and sees shared key j < S if
+ * window = 0 or p - j < window (rows that lie before the first own token too), and its own keys as in kv_attention, with windows and slopes by
+ * these positions (rows.prefix counts a request's own tokens).  out and lse are those of one
+ * softmax over all keys seen.  A prefix is a request of the pool that brings tokens but has no
+ * rows here: kv_block_tables and kv_store fill it like any other, and it ends after the last of
+ * its group.  Two calls with the same arguments give the same bits; the rows differ in rounding
+ * from kv_attention's over tables that name the prefix's blocks for each request. */
+typedef struct {
+    int32_t groups;
+    const int32_t *first;       /* [groups+1] ascending                                   */
+    const int32_t *context;     /* [groups] tokens of the prefix                          */
+    const int32_t *table;       /* [groups][max_blocks]                                   */
+    int64_t table_stride;
+    int32_t max_blocks;
+    int32_t max_new;            /* bounds the rows of a group, as rows.max_new a request's */
+} dro_kv_shared;
+
+int kv_shared_attention(dro_ctx *ctx, const dro_kv_cache *cache, const dro_kv_rows *rows,
+                        const dro_kv_shared *shared, dro_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -61,6 +61,11 @@ class KvRowsStruct(ct.Structure):
                 ("softcap", ct.c_float), ("window", i32), ("slopes", P), ("prefix", P)]
 
 
+class KvSharedStruct(ct.Structure):
+    _fields_ = [("groups", i32), ("first", P), ("context", P), ("table", P), ("table_stride", i64),
+                ("max_blocks", i32), ("max_new", i32)]
+
+
 EXPORTS = {
     "dro_strerror": (ct.c_char_p, [ct.c_int]),
     "dro_create": (ct.c_int, [ct.c_int, ct.POINTER(P)]),
@@ -96,6 +101,8 @@ EXPORTS = {
     "kv_store": (ct.c_int, [P, ct.POINTER(KvCacheStruct), i32, i64, P, i64, i64, P, i64, i64, P, P]),
     "kv_load": (ct.c_int, [P, ct.POINTER(KvCacheStruct), i32, i64, P, i64, i64, P, i64, i64, P, P]),
     "kv_attention": (ct.c_int, [P, ct.POINTER(KvCacheStruct), ct.POINTER(KvRowsStruct), P]),
+    "kv_shared_attention": (ct.c_int, [P, ct.POINTER(KvCacheStruct), ct.POINTER(KvRowsStruct),
+                                       ct.POINTER(KvSharedStruct), P]),
 }
 
 

@@ -65,9 +65,29 @@ struct KvAttnArgs {
     int window;
     const float *slopes;
     const int32_t *prefix;
+    // Over shared prefixes the requests are the groups: every row sees all keys, but for a window.
+    float2 *raw_ml;            // null: not over prefixes.  [T][Hq] maxima and sums of the weights,
+    float *raw_o;              // and sums of the values, DP floats a row, as they are
+    const int32_t *row_pos;    // [T] the rows' places among their requests' own tokens
+    const int2 *ends;          // [R], null: no window.  The first key that some row of the group sees,
+    int prefix_window;         // and the first from which on all do
+    // Behind shared prefixes: such results, to be joined with.
+    const float2 *with_ml;     // null: none
+    const float *with_o;
 };
 // bytes of scratch that a call needs
 size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype);
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st);
+
+// The shared prefixes of groups of requests.
+struct KvSharedArgs {
+    int groups, W;             // W = table columns
+    int max_new, window;
+    const int32_t *first, *context, *table;
+    int64_t table_stride;
+};
+size_t kv_shared_bytes(const KvAttnArgs &a, const KvSharedArgs &s, int cache_dtype);
+hipError_t launch_kv_shared(const KvAttnArgs &a, const KvSharedArgs &s, int dtype, int cache_dtype, void *ws,
+                            hipStream_t st);
 
 }  // namespace dro

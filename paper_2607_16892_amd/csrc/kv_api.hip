@@ -1,5 +1,5 @@
 // C ABI of the paged cache: argument checks and launches of kv_block_tables,
-// kv_store, kv_load and kv_attention.  Every entry point only enqueues work on the caller's
+// kv_store, kv_load, kv_attention and kv_shared_attention.  Every entry point only enqueues work on the caller's
 // stream, except where the workspace has to grow: then the call waits for the device
 // first.
 #include <algorithm>
@@ -182,6 +182,103 @@ int move_rows(dro_ctx *ctx, const dro_kv_cache *c, int32_t dtype, int64_t T, voi
     return DRO_OK;
 }
 
+// kv_attention, and kv_shared_attention where `shared` is given.
+int attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, const dro_kv_shared *shared,
+              dro_stream_t stream)
+{
+    int rc = check_cache(ctx, c);
+    if (rc) return rc;
+    if (!q) return fail(ctx, DRO_EINVAL, "rows is NULL");
+    if ((rc = check_dtype(ctx, q->dtype, c))) return rc;
+    if (q->Hq <= 0 || q->Hq % c->heads)
+        return fail(ctx, DRO_EINVAL, "Hq=%d is not a multiple of the cache's %d heads", q->Hq, c->heads);
+    if ((rc = check_table(ctx, q->table, q->R, q->max_blocks, q->table_stride, c->block))) return rc;
+    if ((rc = check_tokens(ctx, q->T, q->Hq))) return rc;
+    if (!std::isfinite(q->scale) || !std::isfinite(q->softcap) || q->softcap < 0 || q->window < 0 ||
+        q->max_new < 0)
+        return fail(ctx, DRO_EINVAL, "scale=%g must be finite, softcap=%g, window=%d and max_new=%d "
+                    "finite and not negative", q->scale, q->softcap, q->window, q->max_new);
+    if (shared) {
+        if ((rc = check_table(ctx, shared->table, shared->groups, shared->max_blocks, shared->table_stride, c->block)))
+            return rc;
+        if (shared->max_new < 0)
+            return fail(ctx, DRO_EINVAL, "max_new=%d of the shared prefixes is negative", shared->max_new);
+        if (shared->groups && (!shared->first || !shared->context))
+            return fail(ctx, DRO_EINVAL, "first or context of the shared prefixes is NULL");
+    }
+    if (q->T == 0) return DRO_OK;
+    if ((rc = check_rows(ctx, "q", q->q, q->q_token, q->q_head))) return rc;
+    if ((rc = check_rows(ctx, "out", q->out, q->out_token, q->out_head))) return rc;
+    if (!q->start || (q->R && !q->context)) return fail(ctx, DRO_EINVAL, "start or context is NULL");
+    ENTER_DEVICE(ctx);
+    KvAttnArgs a{};
+    a.R = q->R;
+    a.T = (int)q->T;
+    a.Hq = q->Hq;
+    a.H = c->heads;
+    a.G = q->Hq / c->heads;
+    a.D = c->dim;
+    a.shift = block_shift(c->block);
+    a.num_blocks = c->num_blocks;
+    a.W = q->max_blocks;
+    a.max_new = q->max_new;
+    a.num_cu = ctx->num_cu;
+    a.q = q->q;
+    a.q_token = q->q_token;
+    a.q_head = q->q_head;
+    a.out = q->out;
+    a.out_token = q->out_token;
+    a.out_head = q->out_head;
+    a.lse = q->lse;
+    a.start = q->start;
+    a.context = q->context;
+    a.table = q->table;
+    a.table_stride = q->table_stride;
+    a.k = c->k;
+    a.v = c->v;
+    a.k_block = c->k_block;
+    a.k_token = c->k_token;
+    a.k_head = c->k_head;
+    a.v_block = c->v_block;
+    a.v_token = c->v_token;
+    a.v_head = c->v_head;
+    a.k_scale = c->k_scale;
+    a.v_scale = c->v_scale;
+    if (is_mx(c->dtype)) {
+        a.k_power = c->k_power;
+        a.v_power = c->v_power;
+        a.kp_block = c->k_power_block;
+        a.kp_token = c->k_power_token;
+        a.kp_head = c->k_power_head;
+        a.vp_block = c->v_power_block;
+        a.vp_token = c->v_power_token;
+        a.vp_head = c->v_power_head;
+    }
+    a.scale = q->scale;
+    a.cap = q->softcap;
+    // a window as long as the table hides nothing
+    a.window = q->window < (int64_t)q->max_blocks * c->block ? q->window : 0;
+    a.slopes = q->slopes;
+    a.prefix = q->prefix;
+    if (!shared || !shared->groups || !q->R) {
+        if ((rc = ensure_ws(ctx, kv_attention_bytes(a, c->dtype), (hipStream_t)stream))) return rc;
+        HIPCHK(launch_kv_attention(a, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
+        return DRO_OK;
+    }
+    KvSharedArgs s{};
+    s.groups = shared->groups;
+    s.W = shared->max_blocks;
+    s.max_new = shared->max_new;
+    s.window = q->window < ((int64_t)q->max_blocks + shared->max_blocks) * c->block ? q->window : 0;
+    s.first = shared->first;
+    s.context = shared->context;
+    s.table = shared->table;
+    s.table_stride = shared->table_stride;
+    if ((rc = ensure_ws(ctx, kv_shared_bytes(a, s, c->dtype), (hipStream_t)stream))) return rc;
+    HIPCHK(launch_kv_shared(a, s, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
+    return DRO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -250,75 +347,14 @@ int kv_load(dro_ctx *ctx, const dro_kv_cache *c, int32_t dtype, int64_t T, void 
 
 int kv_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, dro_stream_t stream)
 {
-    int rc = check_cache(ctx, c);
-    if (rc) return rc;
-    if (!q) return fail(ctx, DRO_EINVAL, "rows is NULL");
-    if ((rc = check_dtype(ctx, q->dtype, c))) return rc;
-    if (q->Hq <= 0 || q->Hq % c->heads)
-        return fail(ctx, DRO_EINVAL, "Hq=%d is not a multiple of the cache's %d heads", q->Hq, c->heads);
-    if ((rc = check_table(ctx, q->table, q->R, q->max_blocks, q->table_stride, c->block))) return rc;
-    if ((rc = check_tokens(ctx, q->T, q->Hq))) return rc;
-    if (!std::isfinite(q->scale) || !std::isfinite(q->softcap) || q->softcap < 0 || q->window < 0 ||
-        q->max_new < 0)
-        return fail(ctx, DRO_EINVAL, "scale=%g must be finite, softcap=%g, window=%d and max_new=%d "
-                    "finite and not negative", q->scale, q->softcap, q->window, q->max_new);
-    if (q->T == 0) return DRO_OK;
-    if ((rc = check_rows(ctx, "q", q->q, q->q_token, q->q_head))) return rc;
-    if ((rc = check_rows(ctx, "out", q->out, q->out_token, q->out_head))) return rc;
-    if (!q->start || (q->R && !q->context)) return fail(ctx, DRO_EINVAL, "start or context is NULL");
-    ENTER_DEVICE(ctx);
-    KvAttnArgs a{};
-    a.R = q->R;
-    a.T = (int)q->T;
-    a.Hq = q->Hq;
-    a.H = c->heads;
-    a.G = q->Hq / c->heads;
-    a.D = c->dim;
-    a.shift = block_shift(c->block);
-    a.num_blocks = c->num_blocks;
-    a.W = q->max_blocks;
-    a.max_new = q->max_new;
-    a.num_cu = ctx->num_cu;
-    a.q = q->q;
-    a.q_token = q->q_token;
-    a.q_head = q->q_head;
-    a.out = q->out;
-    a.out_token = q->out_token;
-    a.out_head = q->out_head;
-    a.lse = q->lse;
-    a.start = q->start;
-    a.context = q->context;
-    a.table = q->table;
-    a.table_stride = q->table_stride;
-    a.k = c->k;
-    a.v = c->v;
-    a.k_block = c->k_block;
-    a.k_token = c->k_token;
-    a.k_head = c->k_head;
-    a.v_block = c->v_block;
-    a.v_token = c->v_token;
-    a.v_head = c->v_head;
-    a.k_scale = c->k_scale;
-    a.v_scale = c->v_scale;
-    if (is_mx(c->dtype)) {
-        a.k_power = c->k_power;
-        a.v_power = c->v_power;
-        a.kp_block = c->k_power_block;
-        a.kp_token = c->k_power_token;
-        a.kp_head = c->k_power_head;
-        a.vp_block = c->v_power_block;
-        a.vp_token = c->v_power_token;
-        a.vp_head = c->v_power_head;
-    }
-    a.scale = q->scale;
-    a.cap = q->softcap;
-    // a window as long as the table hides nothing
-    a.window = q->window < (int64_t)q->max_blocks * c->block ? q->window : 0;
-    a.slopes = q->slopes;
-    a.prefix = q->prefix;
-    if ((rc = ensure_ws(ctx, kv_attention_bytes(a, c->dtype), (hipStream_t)stream))) return rc;
-    HIPCHK(launch_kv_attention(a, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
-    return DRO_OK;
+    return attention(ctx, c, q, nullptr, stream);
+}
+
+int kv_shared_attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, const dro_kv_shared *shared,
+                        dro_stream_t stream)
+{
+    if (ctx && !shared) return fail(ctx, DRO_EINVAL, "shared is NULL");
+    return attention(ctx, c, q, shared, stream);
 }
 
 }  // extern "C"

@@ -159,10 +159,8 @@ template <int V> struct RowSum {
     __device__ __forceinline__ void add(float2 x, const float *z)
     {
         if (x.y == 0.0f) return;  // no key that the row sees
-        const float to = fmaxf(m, x.x), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - to);
-        m = to;
-        l = l * by + f * x.y;
+        float f;
+        const float by = join_scales(m, l, x, f);
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] = o[j] * by + f * z[j];
     }
@@ -191,11 +189,29 @@ template <int V> struct RowSum {
                 }
         }
     }
-    template <class T>
-    __device__ __forceinline__ void write(const KvAttnArgs &a, const KvJoin &it, int y, int d) const
+    template <class T, int DP>
+    __device__ __forceinline__ void write(const KvAttnArgs &a, const KvJoin &it, int y, int d)
     {
         const int row = it.row0 + y, token = row / a.G, hq = it.head * a.G + row - token * a.G;
-        const int64_t t = it.first_token + token;
+        const int64_t t = it.first_token + token, row_at = t * a.Hq + hq;
+        if (a.with_ml) {  // behind a shared prefix
+            const float2 x = a.with_ml[row_at];
+            if (x.y != 0.0f) {
+                const Vec<float, V> z = *(const Vec<float, V> *)(a.with_o + row_at * DP + d);
+                float w[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) w[j] = ((const float *)&z)[j];
+                add(x, w);
+            }
+        }
+        if (a.raw_ml) {  // over one
+            Vec<float, V> z;
+#pragma unroll
+            for (int j = 0; j < V; ++j) ((float *)&z)[j] = o[j];
+            *(Vec<float, V> *)(a.raw_o + row_at * DP + d) = z;
+            if (d == 0) a.raw_ml[row_at] = make_float2(m, l);
+            return;
+        }
         const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[it.head] : 1.0f) / l;
         T *out = (T *)a.out + t * a.out_token + hq * a.out_head + d;
         if constexpr (V == 4) {  // (the dimension is a multiple of 8)
@@ -207,7 +223,7 @@ template <int V> struct RowSum {
             for (int j = 0; j < V; ++j)
                 if (d + j < a.D) out[j] = (T)(l == 0.0f ? 0.0f : o[j] * inv);
         }
-        if (a.lse && d == 0) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        if (a.lse && d == 0) a.lse[row_at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 };
 
@@ -240,7 +256,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
             s.clear();
             if (it.parts <= 2) s.sum<DP, 2>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
             else s.sum<DP, 8>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
-            s.write<T>(a, it, y, d);
+            s.template write<T, DP>(a, it, y, d);
         }
     }
     for (; many; many &= many - 1) {
@@ -254,7 +270,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
             __syncthreads();
             if (wave == 0) {
                 for (int w = 1; w < WAVES; ++w) s.add(red[w], &acc[w][lane * V]);
-                s.template write<T>(a, it, y, lane * V);
+                s.template write<T, DP>(a, it, y, lane * V);
             }
             __syncthreads();
         }
@@ -379,29 +395,156 @@ template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, 
 }
 
 template <class T>
-static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w, int cache_dtype, hipStream_t st)
+static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w, int cache_dtype, bool pad, hipStream_t st)
 {
     const int DP = padded_dim(a.D);
     if (p.many.groups) {
         kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles,
                                                     w.before, w.tile_sums, w.tiles, w.list);
         const KvTiles t{w.tile_sums, w.tiles, w.list};
-        launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
+        launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, pad, w.o, w.ml, w.joins, st);
         launch_join<T>(a, p.many, 2 * p.many.groups, p.most_tiles, w, DP, st);
     }
     if (!p.few.groups) return;
     if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);
-    launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, !p.many.groups, w.o, w.ml, w.joins, st);
+    launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, pad && !p.many.groups, w.o, w.ml, w.joins, st);
     launch_join<T>(a, p.few, p.few.groups, 0, w, DP, st);
+}
+
+static hipError_t attend(const KvAttnArgs &a, int dtype, int cache_dtype, bool pad, void *ws, hipStream_t st)
+{
+    const KvPlans p = plans(a, cache_dtype);
+    const KvWork w = work_of(a, p, ws);
+    if (dtype == DRO_BF16) run_attention<bf16>(a, p, w, cache_dtype, pad, st);
+    else run_attention<f16>(a, p, w, cache_dtype, pad, st);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st)
 {
-    const KvPlans p = plans(a, cache_dtype);
-    const KvWork w = work_of(a, p, ws);
-    if (dtype == DRO_BF16) run_attention<bf16>(a, p, w, cache_dtype, st);
-    else run_attention<f16>(a, p, w, cache_dtype, st);
-    return hipGetLastError();
+    return attend(a, dtype, cache_dtype, true, ws, st);
+}
+
+// ---- shared prefixes --------------------------------------------------------------------
+//
+// The softmax over a row's keys is that over the prefix joined with that over its own, by their
+// maxima and sums.  All rows of a group see the same keys of the prefix, so first the groups are
+// attended like requests whose rows these are (a row of any of them is as good as another in a tile),
+// and the prefix is read once a tile instead of once a request; the sums stay as they are, in 32
+// bits.  Then each request's own keys are, and whoever finishes a row joins it with its sums.
+
+constexpr int kSharedThreads = 256;
+
+// The groups' rows, each row's place among its request's own tokens, sums of nothing for all rows,
+// and, below a window, where a group's rows begin to see its prefix.
+__global__ __launch_bounds__(kSharedThreads) void kv_shared_rows_kernel(const KvAttnArgs a, const KvSharedArgs s,
+                                                                        int32_t *start, int32_t *row_pos, int2 *ends,
+                                                                        float2 *ml)
+{
+    const uint32_t me = blockIdx.x * kSharedThreads + threadIdx.x, all = gridDim.x * kSharedThreads;
+    const int64_t rows = (int64_t)a.T * a.Hq;
+    for (int64_t i = me; i < rows; i += all) ml[i] = make_float2(-INFINITY, 0.0f);
+    auto at = [&](int r) { return min(max(a.start[r], 0), a.T); };
+    auto context = [&](int r) { return (int)min((long long)max(a.context[r], 0), (long long)a.W << a.shift); };
+    for (uint32_t t = me; t < (uint32_t)a.T; t += all) {
+        int lo = 0, hi = a.R;  // the last request that begins at t or before
+        while (hi - lo > 1) {
+            const int m = (lo + hi) >> 1;
+            if (at(m) <= (int)t) lo = m;
+            else hi = m;
+        }
+        row_pos[t] = a.R ? context(lo) - at(lo + 1) + (int)t : 0;
+    }
+    auto request = [&](int g) { return min(max(s.first[g], 0), a.R); };
+    for (uint32_t g = me; g <= (uint32_t)s.groups; g += all) start[g] = at(request(g));
+    if (!ends) return;
+    const int lane = threadIdx.x & 63;
+    for (uint32_t g = me >> 6; g < (uint32_t)s.groups; g += all >> 6) {  // a wave to a group
+        const int S = (int)min((long long)max(s.context[g], 0), (long long)s.W << a.shift), r1 = request(g + 1);
+        int lo = S, hi = 0;
+        for (int r = request(g) + lane; r < r1; r += 64) {
+            const int ctx = context(r), n = at(r + 1) - at(r);
+            if (n <= 0) continue;
+            const long long from = (long long)S + ctx - s.window;  // of its last row
+            lo = min(lo, (int)max(from - n + 1, 0LL));
+            hi = max(hi, (int)min(max(from, 0LL), (long long)S));
+        }
+        for (int d = 32; d; d >>= 1) {
+            lo = min(lo, __shfl_xor(lo, d));
+            hi = max(hi, __shfl_xor(hi, d));
+        }
+        if (lane == 0) ends[g] = make_int2(lo, max(lo, hi));
+    }
+}
+
+struct KvSharedWork {
+    float *o;
+    float2 *ml;
+    int32_t *row_pos, *start;
+    int2 *ends;
+    void *rest;
+    size_t bytes;  // without the rest
+};
+
+static KvSharedWork shared_work(const KvAttnArgs &a, const KvSharedArgs &s, void *ws)
+{
+    KvSharedWork w{};
+    char *at = (char *)ws;
+    auto take = [&](size_t bytes) {
+        char *q = at;
+        at += (bytes + 255) & ~size_t(255);
+        return q;
+    };
+    const size_t rows = (size_t)a.T * a.Hq;
+    w.o = (float *)take(rows * padded_dim(a.D) * 4);
+    w.ml = (float2 *)take(rows * 8);
+    w.row_pos = (int32_t *)take((size_t)a.T * 4);
+    w.start = (int32_t *)take(((size_t)s.groups + 1) * 4);
+    w.ends = (int2 *)take((size_t)s.groups * 8);
+    w.rest = at;
+    w.bytes = at - (char *)ws;
+    return w;
+}
+
+static KvAttnArgs over_prefixes(const KvAttnArgs &a, const KvSharedArgs &s, const KvSharedWork &w)
+{
+    KvAttnArgs p = a;
+    p.R = s.groups;
+    p.W = s.W;
+    p.max_new = s.max_new;
+    p.start = w.start;
+    p.context = s.context;
+    p.table = s.table;
+    p.table_stride = s.table_stride;
+    p.window = 0;
+    p.prefix = nullptr;
+    p.raw_ml = w.ml;
+    p.raw_o = w.o;
+    p.row_pos = w.row_pos;
+    p.ends = s.window ? w.ends : nullptr;
+    p.prefix_window = s.window;
+    return p;
+}
+
+size_t kv_shared_bytes(const KvAttnArgs &a, const KvSharedArgs &s, int cache_dtype)
+{
+    const KvSharedWork w = shared_work(a, s, nullptr);
+    return w.bytes + std::max(kv_attention_bytes(over_prefixes(a, s, w), cache_dtype), kv_attention_bytes(a, cache_dtype));
+}
+
+hipError_t launch_kv_shared(const KvAttnArgs &a, const KvSharedArgs &s, int dtype, int cache_dtype, void *ws,
+                            hipStream_t st)
+{
+    const KvSharedWork w = shared_work(a, s, ws);
+    const KvAttnArgs p = over_prefixes(a, s, w);
+    const int64_t items = std::max((int64_t)a.T * std::max(a.Hq / 4, 1), (int64_t)s.groups * 64);
+    const unsigned blocks = (unsigned)std::min<int64_t>((items + kSharedThreads) / kSharedThreads, 4 * a.num_cu);
+    kv_shared_rows_kernel<<<blocks, kSharedThreads, 0, st>>>(a, s, w.start, w.row_pos, s.window ? w.ends : nullptr, w.ml);
+    if (hipError_t e = attend(p, dtype, cache_dtype, false, w.rest, st)) return e;
+    KvAttnArgs own = a;
+    own.with_ml = w.ml;
+    own.with_o = w.o;
+    return attend(own, dtype, cache_dtype, true, w.rest, st);
 }
 
 }  // namespace dro

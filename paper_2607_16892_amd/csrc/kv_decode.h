@@ -80,10 +80,10 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         // this lane's row
         const int row = row0 + min(n16, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
-        const KvRange see = kv_row_range(a, it.ctx, it.n, token, prefix);
+        const KvRange see = kv_see(a, it.ctx, it.n, token, prefix, it.first_token + token);
         // the tile's keys: those that some row sees, and those that every row sees
-        const KvRange top = kv_row_range(a, it.ctx, it.n, row0 / a.G, prefix);
-        const KvRange bot = kv_row_range(a, it.ctx, it.n, (row0 + rows - 1) / a.G, prefix);
+        const KvRange top = kv_first(a, r, it.ctx, it.n, row0 / a.G, prefix);
+        const KvRange bot = kv_last(a, r, it.ctx, it.n, (row0 + rows - 1) / a.G, prefix);
         const int all_lo = bot.lo, all_hi = top.hi;
         const int base = top.lo & ~(kStepKeys - 1);
         const int k0 = min(base + it.step * kStepKeys, bot.hi);
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         // to_exp leads to the exponent of its tanh
         const float slope = a.slopes ? a.slopes[hq] * kLog2e : 0.0f;
         const float cap = a.cap * kLog2e, to_exp = a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
-        const int p_row = it.ctx - it.n + token;
+        const int p_row = a.slopes ? kv_row_place(a, it.ctx, it.n, token, it.first_token + token) : 0;
 
         const char *kp = (const char *)a.k + bytes_of<C>((int64_t)h * a.k_head);
         const char *vp = (const char *)a.v + bytes_of<C>((int64_t)h * a.v_head);
@@ -393,24 +393,41 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         if (n16 < rows) {
             const int64_t t = it.first_token + token;
             const int64_t at = (int64_t)kv_part(blockIdx.x, it.step == 0) * kDecodeRows + n16;
+            const int64_t row_at = t * a.Hq + hq;
+            if (whole && a.with_ml) {  // behind a shared prefix
+                float by;
+                const float f = join_scales(m, l, a.with_ml[row_at], by);
+                const float *z = a.with_o + row_at * DP;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < VW; j += 4) {
+                        if (by == 0.0f) continue;  // (and what is there may be anything)
+                        const f32x4 y = *(const f32x4 *)(z + VW * (grp * 4 + c) + j);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[j + i][c] = o[j + i][c] * f + by * y[i];
+                    }
+            }
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
+            const bool raw = !whole || a.raw_ml;
+            float *to = whole ? a.raw_o + row_at * DP : part_o + at * DP;
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int j = 0; j < VW; j += 4) {
                     const int d = VW * (grp * 4 + c) + j;
                     const f32x4 x = {o[j][c], o[j + 1][c], o[j + 2][c], o[j + 3][c]};
-                    if (!whole)
-                        *(f32x4 *)&part_o[at * DP + d] = x;
+                    if (raw)
+                        *(f32x4 *)&to[d] = x;
                     else if (FULL || d < a.D)
                         *(uint2 *)(out + d) = l == 0.0f ? make_uint2(0, 0)
                                                         : make_uint2(pack2<T>(x[0] * inv, x[1] * inv),
                                                                      pack2<T>(x[2] * inv, x[3] * inv));
                 }
             if (grp == 0) {
-                if (!whole) part_ml[at] = make_float2(m, l);
-                else if (a.lse) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+                if (raw) (whole ? a.raw_ml + row_at : part_ml + at)[0] = make_float2(m, l);
+                else if (a.lse) a.lse[row_at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }
         }
         if (!whole && it.step == 0 && lane == 0) {

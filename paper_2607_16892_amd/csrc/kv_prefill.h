@@ -166,21 +166,21 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         const int row0 = tile * Rows;
         const int rows = min(rt.n * a.G - row0, Rows);
         const int prefix = a.prefix ? a.prefix[r] : 0;
-        const KvRange top = kv_row_range(a, rt.ctx, rt.n, row0 / a.G, prefix);
-        const KvRange bot = kv_row_range(a, rt.ctx, rt.n, (row0 + rows - 1) / a.G, prefix);
+        const KvRange top = kv_first(a, r, rt.ctx, rt.n, row0 / a.G, prefix);
+        const KvRange bot = kv_last(a, r, rt.ctx, rt.n, (row0 + rows - 1) / a.G, prefix);
         const int base = top.lo & ~31;
         const int k0 = min(base + step0 * KT, bot.hi), k1 = min(base + (step0 + go) * KT, bot.hi);
         const int steps = (k1 - k0 + KT - 1) / KT;
 
         // this wave's rows, and this lane's
         const int wrow = min(rw, rows - 1), wlast = min(rw + 31, rows - 1);
-        const KvRange wtop = kv_row_range(a, rt.ctx, rt.n, (row0 + wrow) / a.G, prefix);
-        const KvRange wbot = kv_row_range(a, rt.ctx, rt.n, (row0 + wlast) / a.G, prefix);
+        const KvRange wtop = kv_first(a, r, rt.ctx, rt.n, (row0 + wrow) / a.G, prefix);
+        const KvRange wbot = kv_last(a, r, rt.ctx, rt.n, (row0 + wlast) / a.G, prefix);
         const bool idle = rw >= rows;
         const int row = row0 + min(rw + n32, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
-        const KvRange see = kv_row_range(a, rt.ctx, rt.n, token, prefix);
-        const int p_row = rt.ctx - rt.n + token;
+        const KvRange see = kv_see(a, rt.ctx, rt.n, token, prefix, first_token + token);
+        const int p_row = MODS ? kv_row_place(a, rt.ctx, rt.n, token, first_token + token) : 0;
 
         u32x4 q[S];
         {
@@ -515,23 +515,41 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         if (rw + n32 < rows) {
             const int64_t t = first_token + token;
             const int64_t at = (int64_t)place * Rows + rw + n32;
+            const int64_t row_at = t * a.Hq + hq;
+            const bool first = half == 0 && dt0 == 0;
+            if (whole && a.with_ml) {  // behind a shared prefix
+                float by;
+                const float f = join_scales(m, l, a.with_ml[row_at], by);
+                const float *z = a.with_o + row_at * DP;
+#pragma unroll
+                for (int j = 0; j < ND; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        if (by == 0.0f) continue;  // (and what is there may be anything)
+                        const f32x4 y = *(const f32x4 *)(z + (dt0 + j) * 32 + (i >> 2) * 8 + half * 4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[j][i + e] = o[j][i + e] * f + by * y[e];
+                    }
+            }
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
+            const bool raw = !whole || a.raw_ml;
+            float *to = whole ? a.raw_o + row_at * DP : part_o + at * DP;
 #pragma unroll
             for (int j = 0; j < ND; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4;
-                    if (!whole)
-                        *(f32x4 *)&part_o[at * DP + d] = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
+                    if (raw)
+                        *(f32x4 *)&to[d] = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
                     else if (FULL || d < a.D)
                         *(uint2 *)(out + d) = l == 0.0f ? make_uint2(0, 0)
                                                         : make_uint2(pack2<T>(o[j][i] * inv, o[j][i + 1] * inv),
                                                                      pack2<T>(o[j][i + 2] * inv, o[j][i + 3] * inv));
                 }
-            if (half == 0 && dt0 == 0) {
-                if (!whole) part_ml[at] = make_float2(m, l);
-                else if (a.lse) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+            if (first) {
+                if (raw) (whole ? a.raw_ml + row_at : part_ml + at)[0] = make_float2(m, l);
+                else if (a.lse) a.lse[row_at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }
         }
         if (!whole && threadIdx.x == 0) {

@@ -62,6 +62,7 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs &a, const KvCut &c,
     if (a.window && !a.prefix)  // a tile's rows lie within rows / G + 2 tokens
         s.span = (int)min((long long)s.ctx,
                           (long long)a.window + min(c.rows / a.G + 2, n) + kStepKeys);
+    if (a.ends) s.span = s.ctx - (a.ends[r].x & ~(kStepKeys - 1));
     return s;
 }
 
@@ -182,11 +183,38 @@ struct KvRange {
 };
 __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, int n, int token, int prefix)
 {
+    KvRange v{0, ctx};
+    if (a.raw_ml) return v;
     const int p = ctx - n + token;  // negative where the cache holds fewer tokens than there are rows
-    KvRange v;
     v.hi = min(max(p + 1, prefix), ctx);
     v.lo = a.window ? max(p - a.window + 1, 0) : 0;
     return v;
+}
+// The same of the row itself, t of the call's (a prefix's keys have a window by the row's place), and
+// of the first and the last of some rows: up to where no row of them sees keys, and from where on
+// all do.
+__device__ __forceinline__ KvRange kv_see(const KvAttnArgs &a, int ctx, int n, int token, int prefix, int t)
+{
+    KvRange v = kv_row_range(a, ctx, n, token, prefix);
+    if (a.ends) v.lo = (int)min(max((long long)ctx + a.row_pos[t] - a.prefix_window + 1, 0LL), (long long)ctx);
+    return v;
+}
+__device__ __forceinline__ KvRange kv_first(const KvAttnArgs &a, int r, int ctx, int n, int token, int prefix)
+{
+    KvRange v = kv_row_range(a, ctx, n, token, prefix);
+    if (a.ends) v.lo = a.ends[r].x;
+    return v;
+}
+__device__ __forceinline__ KvRange kv_last(const KvAttnArgs &a, int r, int ctx, int n, int token, int prefix)
+{
+    KvRange v = kv_row_range(a, ctx, n, token, prefix);
+    if (a.ends) v.lo = a.ends[r].y;
+    return v;
+}
+// The row's place, for a bias by distance.
+__device__ __forceinline__ int kv_row_place(const KvAttnArgs &a, int ctx, int n, int token, int t)
+{
+    return a.raw_ml ? ctx + a.row_pos[t] : ctx - n + token;
 }
 
 // ---- many rows a request ------------------------------------------------------------
@@ -218,7 +246,7 @@ __device__ __forceinline__ uint32_t kv_tile_steps(const KvAttnArgs &a, const KvS
 {
     const int prefix = a.prefix ? a.prefix[r] : 0, row0 = tile * rows;
     const int last = min(s.n - 1, (row0 + rows - 1) / a.G);
-    const int lo = kv_row_range(a, s.ctx, s.n, row0 / a.G, prefix).lo & ~31;
+    const int lo = kv_first(a, r, s.ctx, s.n, row0 / a.G, prefix).lo & ~31;
     const int hi = kv_row_range(a, s.ctx, s.n, last, prefix).hi;
     return (uint32_t)max((hi - lo + keys - 1) / keys, 1);
 }

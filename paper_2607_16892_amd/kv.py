@@ -1,5 +1,5 @@
-"""Binding of the paged-cache entry points (block tables, store, load, attention;
-include/dro.h).  Argument checks and marshalling only."""
+"""Binding of the paged-cache entry points (block tables, store, load, attention, attention
+behind shared prefixes; include/dro.h).  Argument checks and marshalling only."""
 from __future__ import annotations
 
 import ctypes as ct
@@ -78,14 +78,14 @@ def _int32(x):
     return min(max(x, -2 ** 31), 2 ** 31 - 1)
 
 
-def _need_table(t, device):
+def _need_table(t, device, name="table"):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("table must be a CUDA tensor")
+        raise TypeError(f"{name} must be a CUDA tensor")
     if device is not None and t.device != device:
-        raise TypeError(f"table is on {t.device}, expected {device}")
+        raise TypeError(f"{name} is on {t.device}, expected {device}")
     shape, stride = t.shape, t.stride()
     if t.dtype is not torch.int32 or len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
-        raise ValueError("table must be an int32 [R, max_blocks] tensor with contiguous rows")
+        raise ValueError(f"{name} must be an int32 [R, max_blocks] tensor with contiguous rows")
     return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1]
 
 
@@ -340,6 +340,22 @@ def kv_load(ctx: Context, cache: KvCache, slot: torch.Tensor, dtype=None, k=None
     return dict(k=k, v=v)
 
 
+@dataclass
+class SharedPrefixes:
+    """Prefixes that groups of consecutive requests share (field meanings as in dro_kv_shared)."""
+    first: torch.Tensor        # int32 [groups + 1] first request of each group, and the end
+    context: torch.Tensor      # int32 [groups] tokens of each prefix
+    table: torch.Tensor        # int32 [groups, max_blocks] its blocks, rows may be strided
+    max_new: int               # bounds the rows of a group
+
+    def struct(self, device) -> _native.KvSharedStruct:
+        groups, width, stride = _need_table(self.table, device, "the table of the shared prefixes")
+        return _native.KvSharedStruct(
+            groups, _need(self.first, torch.int32, "first", device, groups + 1),
+            _need(self.context, torch.int32, "context of the shared prefixes", device, groups),
+            self.table.data_ptr(), stride, width, _int32(self.max_new))
+
+
 def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Tensor,
                  start: torch.Tensor, context: torch.Tensor, max_new: int, scale=None,
                  softcap: float = 0.0, window: int = 0, slopes: Optional[torch.Tensor] = None,
@@ -349,6 +365,27 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     is a BlockPool's, `start` and `context` come from kv_block_tables; max_new bounds the rows of
     one request.  scale defaults to dim ** -0.5.  No backward pass: inputs that require grad are
     refused where gradients are recorded."""
+    return _attention(ctx, cache, q, table, start, context, max_new, None, scale, softcap, window,
+                      slopes, prefix, out, lse, want_lse, stream)
+
+
+def kv_shared_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Tensor,
+                        start: torch.Tensor, context: torch.Tensor, max_new: int,
+                        shared: SharedPrefixes, scale=None, softcap: float = 0.0, window: int = 0,
+                        slopes: Optional[torch.Tensor] = None,
+                        prefix: Optional[torch.Tensor] = None, out=None, lse=None,
+                        want_lse: bool = True, stream=None) -> dict:
+    """kv_attention behind prefixes that the cache holds, and the call reads, once for a group of
+    requests (see kv_shared_attention in dro.h): `table`, `context` and `prefix` are of the
+    requests' own tokens, which follow the group's in `shared`."""
+    if not isinstance(shared, SharedPrefixes):
+        raise TypeError("shared must be SharedPrefixes")
+    return _attention(ctx, cache, q, table, start, context, max_new, shared, scale, softcap, window,
+                      slopes, prefix, out, lse, want_lse, stream)
+
+
+def _attention(ctx, cache, q, table, start, context, max_new, shared, scale, softcap, window, slopes,
+               prefix, out, lse, want_lse, stream):
     dev, cs = cache.device, cache._struct
     if dev.index != ctx.device.index:
         _other_device(ctx, dev)
@@ -362,7 +399,7 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
     prefix_p = None if prefix is None else _need(prefix, torch.int32, "prefix", dev, R)
     slopes_p = None if slopes is None else _need(slopes, torch.float32, "slopes", dev, Hq)
     if q.requires_grad or cache._grad or (slopes is not None and slopes.requires_grad):
-        _no_gradient("kv_attention")
+        _no_gradient("kv_attention" if shared is None else "kv_shared_attention")
     if not 0 <= window < 2 ** 31 or not 0 <= max_new < 2 ** 31:
         window, max_new = _int32(window), _int32(max_new)
     with nullcontext() if stream is None else torch.cuda.stream(stream):
@@ -382,9 +419,15 @@ def kv_attention(ctx: Context, cache: KvCache, q: torch.Tensor, table: torch.Ten
         None if lse is None else lse.data_ptr(), start_p, context_p, table.data_ptr(), table_stride,
         width, int(max_new), dim ** -0.5 if scale is None else scale, softcap, window, slopes_p,
         prefix_p)
-    rc = ctx._lib.kv_attention(ctx.handle, ct.byref(cs), ct.byref(rows), _queue(stream, dev))
+    if shared is None:
+        rc = ctx._lib.kv_attention(ctx.handle, ct.byref(cs), ct.byref(rows), _queue(stream, dev))
+    else:
+        prefixes = shared.struct(dev)
+        rc = ctx._lib.kv_shared_attention(ctx.handle, ct.byref(cs), ct.byref(rows), ct.byref(prefixes),
+                                          _queue(stream, dev))
     if rc:
-        ctx.check(rc, "kv_attention")
+        ctx.check(rc, "kv_attention" if shared is None else "kv_shared_attention")
     if stream is not None:
-        _share(stream, dev, *cache.tensors, q, table, start, context, slopes, prefix, out, lse)
+        _share(stream, dev, *cache.tensors, q, table, start, context, slopes, prefix, out, lse,
+               *(() if shared is None else (shared.first, shared.context, shared.table)))
     return dict(out=out, lse=lse)
