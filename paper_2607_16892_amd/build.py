@@ -37,6 +37,10 @@ UNITS = {
     "kv_decode_f16.hip": [],
     "kv_prefill_bf16.hip": [],
     "kv_prefill_f16.hip": [],
+    "kv_shared_decode_bf16.hip": [],
+    "kv_shared_decode_f16.hip": [],
+    "kv_shared_prefill_bf16.hip": [],
+    "kv_shared_prefill_f16.hip": [],
 }
 
 

@@ -211,7 +211,7 @@ int attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, const d
     if ((rc = check_rows(ctx, "out", q->out, q->out_token, q->out_head))) return rc;
     if (!q->start || (q->R && !q->context)) return fail(ctx, DRO_EINVAL, "start or context is NULL");
     ENTER_DEVICE(ctx);
-    KvAttnArgs a{};
+    KvSharedArgs a{};
     a.R = q->R;
     a.T = (int)q->T;
     a.Hq = q->Hq;
@@ -265,17 +265,16 @@ int attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, const d
         HIPCHK(launch_kv_attention(a, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
         return DRO_OK;
     }
-    KvSharedArgs s{};
-    s.groups = shared->groups;
-    s.W = shared->max_blocks;
-    s.max_new = shared->max_new;
-    s.window = q->window < ((int64_t)q->max_blocks + shared->max_blocks) * c->block ? q->window : 0;
-    s.first = shared->first;
-    s.context = shared->context;
-    s.table = shared->table;
-    s.table_stride = shared->table_stride;
-    if ((rc = ensure_ws(ctx, kv_shared_bytes(a, s, c->dtype), (hipStream_t)stream))) return rc;
-    HIPCHK(launch_kv_shared(a, s, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
+    a.groups = shared->groups;
+    a.p_W = shared->max_blocks;
+    a.p_max_new = shared->max_new;
+    a.p_window = q->window < ((int64_t)q->max_blocks + shared->max_blocks) * c->block ? q->window : 0;
+    a.first = shared->first;
+    a.p_context = shared->context;
+    a.p_table = shared->table;
+    a.p_stride = shared->table_stride;
+    if ((rc = ensure_ws(ctx, kv_shared_bytes(a, c->dtype), (hipStream_t)stream))) return rc;
+    HIPCHK(launch_kv_shared(a, q->dtype, c->dtype, ctx->ws, (hipStream_t)stream));
     return DRO_OK;
 }
 

@@ -28,34 +28,59 @@ static __device__ uint64_t plan_scan(uint64_t x, uint64_t *part, uint64_t &total
     return x;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs a, const KvCut cut, uint64_t *sums)
+// The sums [n + 1] of the requests' steps; behind shared prefixes, where they are of all sources of
+// keys, the steps of a workgroup after them.
+template <class A> static __device__ __forceinline__ void plan_sums(const A &a, const KvCut &cut, uint64_t *sums, uint64_t *part)
 {
-    __shared__ uint64_t part[kPlanThreads / 64];
-    const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
-    const int r0 = min((int)threadIdx.x * per, a.R), r1 = min(r0 + per, a.R);
+    const int n = kv_requests(a), per = (n + kPlanThreads - 1) / kPlanThreads;
+    const int r0 = min((int)threadIdx.x * per, n), r1 = min(r0 + per, n);
     uint64_t units = 0, total;
-    for (int r = r0; r < r1; ++r) units += kv_units(a, kv_share(a, cut, r));
+    uint32_t longest = 0;
+    for (int r = r0; r < r1; ++r) {
+        const KvShare s = kv_share(a, cut, r);
+        units += kv_units(a, s);
+        longest = max(longest, kv_steps(s));
+    }
     uint64_t at = plan_scan(units, part, total) - units;
     for (int r = r0; r < r1; ++r) {
         sums[r] = at;
         at += kv_units(a, kv_share(a, cut, r));
     }
-    if (threadIdx.x == 0) sums[a.R] = total;
+    if constexpr (kShared<A>) {
+        const uint64_t least = __syncthreads_or(longest >= 2048) ? 8 : __syncthreads_or(longest >= 512) ? 4
+                             : __syncthreads_or(longest >= 128) ? 2 : 1;
+        if (threadIdx.x == 0) sums[n + 1] = kv_run_of(cut, total, least);
+    }
+    if (threadIdx.x == 0) sums[n] = total;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvAttnArgs a, const KvCut cut, uint64_t *sums)
+{
+    __shared__ uint64_t part[kPlanThreads / 64];
+    plan_sums(a, cut, sums, part);
 }
 
 // The tiles of the requests of many rows and the sums of their chunks: first the tiles before
 // each request, then the list and its steps, then the chunks, 1024 tiles at a time.
-__global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs a, const KvCut cut, int keys, int most,
-                                                                uint64_t *before, uint32_t *sums, KvTile *tiles,
-                                                                KvTileList *list)
+struct KvTileLds {
+    uint64_t part[kPlanThreads / 64];
+    uint32_t steps_at[kPlanThreads];
+    uint32_t before[kPlanThreads];  // up to a request a thread: a search in LDS
+    uint32_t nth_at[kPlanThreads];  // behind shared prefixes
+    KvShare share[kPlanThreads];
+};
+
+// (behind shared prefixes also `where`: of each tile, as they are listed before they are sorted, its
+// first partial result, of head 0, and its chunks)
+template <class A>
+static __device__ __forceinline__ void plan_tiles(const A &a, const KvCut &cut, int keys, int most, uint64_t *before,
+                                                  uint32_t *sums, KvTile *tiles, KvTileList *list, int2 *where, KvTileLds &l)
 {
-    __shared__ uint64_t part[kPlanThreads / 64];
-    __shared__ uint32_t steps_at[kPlanThreads];
-    __shared__ uint32_t before_lds[kPlanThreads];  // up to a request a thread: a search in LDS
-    __shared__ KvShare share_lds[kPlanThreads];
-    const bool lds = a.R <= kPlanThreads;
-    const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
-    const int r0 = min((int)threadIdx.x * per, a.R), r1 = min(r0 + per, a.R);
+    uint64_t *part = l.part;
+    const int requests = kv_requests(a);
+    const bool lds = requests <= kPlanThreads;
+    const int per = (requests + kPlanThreads - 1) / kPlanThreads;
+    const int r0 = min((int)threadIdx.x * per, requests), r1 = min(r0 + per, requests);
     uint64_t own = 0, total;
     KvShare s0{};
     for (int r = r0; r < r1; ++r) {
@@ -64,9 +89,10 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
     }
     uint64_t at = plan_scan(own, part, total) - own;
     if (lds) {
-        before_lds[threadIdx.x] = (uint32_t)min(at, (uint64_t)0xffffffff);
-        share_lds[threadIdx.x] = s0;
-    } else {
+        l.before[threadIdx.x] = (uint32_t)min(at, (uint64_t)0xffffffff);
+        l.share[threadIdx.x] = s0;
+    }
+    if (!lds || kShared<A>) {
         for (int r = r0; r < r1; ++r) {
             before[r] = at;
             at += kv_share(a, cut, r).tiles;
@@ -80,16 +106,16 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
         const int e = e0 + threadIdx.x;
         uint32_t steps = 0;
         if (e < n) {
-            int lo = 0, hi = a.R;  // the last request with before[r] <= e: it has tiles
+            int lo = 0, hi = requests;  // the last request with before[r] <= e: it has tiles
             while (hi - lo > 1) {
                 const int m = (lo + hi) >> 1;
-                if ((lds ? before_lds[m] : before[m]) <= (uint64_t)e) lo = m;
+                if ((lds ? l.before[m] : before[m]) <= (uint64_t)e) lo = m;
                 else hi = m;
             }
-            const KvShare s = lds ? share_lds[lo] : kv_share(a, cut, lo);
-            const int tile = max(s.tiles - 1 - (e - (int)(lds ? before_lds[lo] : before[lo])), 0);
+            const KvShare s = lds ? l.share[lo] : kv_share(a, cut, lo);
+            const int tile = max(s.tiles - 1 - (e - (int)(lds ? l.before[lo] : before[lo])), 0);
             steps = kv_tile_steps(a, s, lo, tile, cut.rows, keys);
-            mine = KvTile{lo, tile, s.n, s.ctx, min(max(a.start[lo], 0), a.T), (int)steps, 0, 1, 0};
+            mine = KvTile{lo, tile, s.n, s.ctx, kv_first_token(a, lo), (int)steps, 0, 1, 0};
             tiles[e] = mine;
         }
         plan_scan(steps, part, total);
@@ -110,7 +136,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
         for (int s = 0; s < shift; s += 16) to += (uint32_t)(total >> s) & 0xffff;
         if (is) {
             tiles[to] = mine;
-            steps_at[to] = mine.steps;
+            l.steps_at[to] = mine.steps;
+            if constexpr (kShared<A>) l.nth_at[to] = threadIdx.x;
         }
         __syncthreads();
     }
@@ -119,7 +146,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
     uint32_t all = 0, parts = 0;
     for (int e0 = 0; e0 < n; e0 += kPlanThreads) {
         const int e = e0 + threadIdx.x;
-        const uint32_t steps = e >= n ? 0 : sort ? steps_at[e] : tiles[e].steps;  // (tiles: this thread's)
+        const uint32_t steps = e >= n ? 0 : sort ? l.steps_at[e] : tiles[e].steps;  // (tiles: this thread's)
         const uint64_t chunks = e < n ? max((steps + share / 4) / share, (uint64_t)1) : 0;
         const uint64_t count = chunks > 1 ? chunks | chunks << 32 : chunks;
         const uint64_t upto = plan_scan(count, part, total) - count;
@@ -127,6 +154,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
             sums[e] = tiles[e].before = all + (uint32_t)upto;
             tiles[e].part = (int)(parts + (uint32_t)(upto >> 32));
             tiles[e].chunks = (int)chunks;
+            if constexpr (kShared<A>)
+                where[sort ? l.nth_at[e] : e] = make_int2((int)(parts + (uint32_t)(upto >> 32)), (int)chunks);
         }
         all += (uint32_t)total;
         parts += (uint32_t)(total >> 32);
@@ -135,6 +164,14 @@ __global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs
         sums[n] = all;
         *list = KvTileList{n, (int)parts, all};
     }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void kv_tiles_kernel(const KvAttnArgs a, const KvCut cut, int keys, int most,
+                                                                uint64_t *before, uint32_t *sums, KvTile *tiles,
+                                                                KvTileList *list)
+{
+    __shared__ KvTileLds lds;
+    plan_tiles(a, cut, keys, most, before, sums, tiles, list, nullptr, lds);
 }
 
 // ---- join -------------------------------------------------------------------------
@@ -159,8 +196,10 @@ template <int V> struct RowSum {
     __device__ __forceinline__ void add(float2 x, const float *z)
     {
         if (x.y == 0.0f) return;  // no key that the row sees
-        float f;
-        const float by = join_scales(m, l, x, f);
+        const float to = fmaxf(m, x.x), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - to);
+        m = to;
+        l = l * by + f * x.y;
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] = o[j] * by + f * z[j];
     }
@@ -189,30 +228,16 @@ template <int V> struct RowSum {
                 }
         }
     }
-    template <class T, int DP>
-    __device__ __forceinline__ void write(const KvAttnArgs &a, const KvJoin &it, int y, int d)
+    template <class T>
+    __device__ __forceinline__ void write(const KvAttnArgs &a, const KvJoin &it, int y, int d) const
     {
         const int row = it.row0 + y, token = row / a.G, hq = it.head * a.G + row - token * a.G;
-        const int64_t t = it.first_token + token, row_at = t * a.Hq + hq;
-        if (a.with_ml) {  // behind a shared prefix
-            const float2 x = a.with_ml[row_at];
-            if (x.y != 0.0f) {
-                const Vec<float, V> z = *(const Vec<float, V> *)(a.with_o + row_at * DP + d);
-                float w[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) w[j] = ((const float *)&z)[j];
-                add(x, w);
-            }
-        }
-        if (a.raw_ml) {  // over one
-            Vec<float, V> z;
-#pragma unroll
-            for (int j = 0; j < V; ++j) ((float *)&z)[j] = o[j];
-            *(Vec<float, V> *)(a.raw_o + row_at * DP + d) = z;
-            if (d == 0) a.raw_ml[row_at] = make_float2(m, l);
-            return;
-        }
-        const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[it.head] : 1.0f) / l;
+        write_row<T>(a, it.first_token + token, it.head, hq, d);
+    }
+    template <class T>
+    __device__ __forceinline__ void write_row(const KvAttnArgs &a, int64_t t, int head, int hq, int d) const
+    {
+        const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[head] : 1.0f) / l;
         T *out = (T *)a.out + t * a.out_token + hq * a.out_head + d;
         if constexpr (V == 4) {  // (the dimension is a multiple of 8)
             if (d < a.D)
@@ -223,7 +248,7 @@ template <int V> struct RowSum {
             for (int j = 0; j < V; ++j)
                 if (d + j < a.D) out[j] = (T)(l == 0.0f ? 0.0f : o[j] * inv);
         }
-        if (a.lse && d == 0) a.lse[row_at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        if (a.lse && d == 0) a.lse[t * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 };
 
@@ -256,7 +281,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
             s.clear();
             if (it.parts <= 2) s.sum<DP, 2>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
             else s.sum<DP, 8>(it, tile_rows, part_o, part_ml, y, d, 0, 1);
-            s.template write<T, DP>(a, it, y, d);
+            s.write<T>(a, it, y, d);
         }
     }
     for (; many; many &= many - 1) {
@@ -270,7 +295,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(const KvAttnArgs a,
             __syncthreads();
             if (wave == 0) {
                 for (int w = 1; w < WAVES; ++w) s.add(red[w], &acc[w][lane * V]);
-                s.template write<T, DP>(a, it, y, lane * V);
+                s.template write<T>(a, it, y, lane * V);
             }
             __syncthreads();
         }
@@ -340,28 +365,33 @@ struct KvWork {
     size_t bytes;
 };
 
+// Cuts a workspace up; from a null one, sizes.
+struct KvTake {
+    char *at;
+    template <class U> void operator()(U *&p, size_t count)
+    {
+        p = (U *)at;
+        at += (count * sizeof(U) + 255) & ~size_t(255);
+    }
+};
+
 static KvWork work_of(const KvAttnArgs &a, const KvPlans &p, void *ws)
 {
     KvWork w{};
-    char *at = (char *)ws;
-    auto take = [&](size_t bytes) {
-        char *q = at;
-        at += (bytes + 255) & ~size_t(255);
-        return q;
-    };
+    KvTake take{(char *)ws};
     // the kernels run one after the other: their partial results share one place
     const size_t rows = (size_t)2 * std::max((size_t)p.few.groups * p.few.rows, (size_t)p.many.groups * p.many.rows);
-    w.o = (float *)take(rows * padded_dim(a.D) * 4);
-    w.ml = (float2 *)take(rows * 8);
-    w.joins = (KvJoin *)take(std::max(p.few.groups, 2 * p.many.groups) * sizeof(KvJoin));
-    w.sums = (uint64_t *)take(((size_t)a.R + 1) * 8);
+    take(w.o, rows * padded_dim(a.D));
+    take(w.ml, rows);
+    take(w.joins, std::max(p.few.groups, 2 * p.many.groups));
+    take(w.sums, (size_t)a.R + 1);
     if (p.many.groups) {
-        w.before = (uint64_t *)take((size_t)a.R * 8);
-        w.tile_sums = (uint32_t *)take(((size_t)p.most_tiles + 1) * 4);
-        w.tiles = (KvTile *)take((size_t)p.most_tiles * sizeof(KvTile));
-        w.list = (KvTileList *)take(sizeof(KvTileList));
+        take(w.before, a.R);
+        take(w.tile_sums, (size_t)p.most_tiles + 1);
+        take(w.tiles, p.most_tiles);
+        take(w.list, 1);
     }
-    w.bytes = at - (char *)ws;
+    w.bytes = take.at - (char *)ws;
     return w;
 }
 
@@ -395,156 +425,260 @@ template <class T> static void launch_join(const KvAttnArgs &a, const KvCut &c, 
 }
 
 template <class T>
-static void run_attention(const KvAttnArgs &a, const KvPlans &p, const KvWork &w, int cache_dtype, bool pad, hipStream_t st)
+static void run_attention(const KvMxArgs &a, const KvPlans &p, const KvWork &w, int cache_dtype, hipStream_t st)
 {
     const int DP = padded_dim(a.D);
     if (p.many.groups) {
         kv_tiles_kernel<<<1, kPlanThreads, 0, st>>>(a, p.many, kv_prefill_keys(DP), p.most_tiles,
                                                     w.before, w.tile_sums, w.tiles, w.list);
         const KvTiles t{w.tile_sums, w.tiles, w.list};
-        launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, pad, w.o, w.ml, w.joins, st);
+        launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
         launch_join<T>(a, p.many, 2 * p.many.groups, p.most_tiles, w, DP, st);
     }
     if (!p.few.groups) return;
     if (a.R > kInlineRequests) kv_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, w.sums);
-    launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, pad && !p.many.groups, w.o, w.ml, w.joins, st);
+    launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, !p.many.groups, w.o, w.ml, w.joins, st);
     launch_join<T>(a, p.few, p.few.groups, 0, w, DP, st);
 }
 
-static hipError_t attend(const KvAttnArgs &a, int dtype, int cache_dtype, bool pad, void *ws, hipStream_t st)
+hipError_t launch_kv_attention(const KvMxArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st)
 {
     const KvPlans p = plans(a, cache_dtype);
     const KvWork w = work_of(a, p, ws);
-    if (dtype == DRO_BF16) run_attention<bf16>(a, p, w, cache_dtype, pad, st);
-    else run_attention<f16>(a, p, w, cache_dtype, pad, st);
+    if (dtype == DRO_BF16) run_attention<bf16>(a, p, w, cache_dtype, st);
+    else run_attention<f16>(a, p, w, cache_dtype, st);
     return hipGetLastError();
-}
-
-hipError_t launch_kv_attention(const KvAttnArgs &a, int dtype, int cache_dtype, void *ws, hipStream_t st)
-{
-    return attend(a, dtype, cache_dtype, true, ws, st);
 }
 
 // ---- shared prefixes --------------------------------------------------------------------
 //
-// The softmax over a row's keys is that over the prefix joined with that over its own, by their
-// maxima and sums.  All rows of a group see the same keys of the prefix, so first the groups are
-// attended like requests whose rows these are (a row of any of them is as good as another in a tile),
-// and the prefix is read once a tile instead of once a request; the sums stay as they are, in 32
-// bits.  Then each request's own keys are, and whoever finishes a row joins it with its sums.
+// The softmax over a row's keys is that over its group's prefix joined with that over its own tokens,
+// by their maxima and sums.  All rows of a group see the same keys of its prefix, so it is attended
+// like one request whose rows these are: a tile takes rows of several requests, and reads the
+// prefix once for them.  One launch of a workgroup plans both (the same lists, over the groups
+// and then the requests), the kernels of few and of many rows leave sums, and one launch joins
+// each row's, up to the order of the sources and of their keys.
 
-constexpr int kSharedThreads = 256;
-
-// The groups' rows, each row's place among its request's own tokens, sums of nothing for all rows,
-// and, below a window, where a group's rows begin to see its prefix.
-__global__ __launch_bounds__(kSharedThreads) void kv_shared_rows_kernel(const KvAttnArgs a, const KvSharedArgs s,
-                                                                        int32_t *start, int32_t *row_pos, int2 *ends,
-                                                                        float2 *ml)
+// Each row's place among its request's own tokens.
+constexpr int kPlaceThreads = 256;
+__global__ __launch_bounds__(kPlaceThreads) void kv_places_kernel(const KvSharedArgs a)
 {
-    const uint32_t me = blockIdx.x * kSharedThreads + threadIdx.x, all = gridDim.x * kSharedThreads;
-    const int64_t rows = (int64_t)a.T * a.Hq;
-    for (int64_t i = me; i < rows; i += all) ml[i] = make_float2(-INFINITY, 0.0f);
-    auto at = [&](int r) { return min(max(a.start[r], 0), a.T); };
-    auto context = [&](int r) { return (int)min((long long)max(a.context[r], 0), (long long)a.W << a.shift); };
-    for (uint32_t t = me; t < (uint32_t)a.T; t += all) {
+    for (uint32_t t = blockIdx.x * kPlaceThreads + threadIdx.x; t < (uint32_t)a.T; t += gridDim.x * kPlaceThreads) {
         int lo = 0, hi = a.R;  // the last request that begins at t or before
         while (hi - lo > 1) {
             const int m = (lo + hi) >> 1;
-            if (at(m) <= (int)t) lo = m;
+            if (a.start[m] <= (int)t) lo = m;
             else hi = m;
         }
-        row_pos[t] = a.R ? context(lo) - at(lo + 1) + (int)t : 0;
+        a.row_pos[t] = kv_context(a, a.groups + lo) - kv_end_token(a, a.groups + lo) + (int)t;
     }
-    auto request = [&](int g) { return min(max(s.first[g], 0), a.R); };
-    for (uint32_t g = me; g <= (uint32_t)s.groups; g += all) start[g] = at(request(g));
-    if (!ends) return;
-    const int lane = threadIdx.x & 63;
-    for (uint32_t g = me >> 6; g < (uint32_t)s.groups; g += all >> 6) {  // a wave to a group
-        const int S = (int)min((long long)max(s.context[g], 0), (long long)s.W << a.shift), r1 = request(g + 1);
-        int lo = S, hi = 0;
-        for (int r = request(g) + lane; r < r1; r += 64) {
-            const int ctx = context(r), n = at(r + 1) - at(r);
-            if (n <= 0) continue;
-            const long long from = (long long)S + ctx - s.window;  // of its last row
-            lo = min(lo, (int)max(from - n + 1, 0LL));
-            hi = max(hi, (int)min(max(from, 0LL), (long long)S));
+}
+
+static __device__ __forceinline__ int group_request(const KvSharedArgs &a, int g) { return min(max(a.first[g], 0), a.R); }
+
+__global__ __launch_bounds__(kPlanThreads) void kv_shared_plan_kernel(const KvSharedArgs a, const KvCut few, const KvCut many,
+                                                                      int keys, int most, uint64_t *sums, uint64_t *before,
+                                                                      uint32_t *tile_sums, KvTile *tiles, KvTileList *list,
+                                                                      int2 *where)
+{
+    __shared__ KvTileLds lds;
+    for (int g = threadIdx.x; g <= a.groups; g += kPlanThreads)
+        a.p_start[g] = min(max(a.start[group_request(a, g)], 0), a.T);
+    if (a.ends) {
+        const int lane = threadIdx.x & 63;
+        for (int g = threadIdx.x >> 6; g < a.groups; g += kPlanThreads / 64) {  // a wave to a group
+            const int S = kv_context(a, g), r1 = group_request(a, g + 1);
+            int lo = S, hi = 0;
+            for (int r = group_request(a, g) + lane; r < r1; r += 64) {
+                const int n = kv_end_token(a, a.groups + r) - kv_first_token(a, a.groups + r);
+                if (n <= 0) continue;
+                const long long from = (long long)S + kv_context(a, a.groups + r) - a.p_window;  // of its last row
+                lo = min(lo, (int)max(from - n + 1, 0LL));
+                hi = max(hi, (int)min(max(from, 0LL), (long long)S));
+            }
+            for (int d = 32; d; d >>= 1) {
+                lo = min(lo, __shfl_xor(lo, d));
+                hi = max(hi, __shfl_xor(hi, d));
+            }
+            if (lane == 0) a.ends[g] = make_int2(lo, max(lo, hi));
         }
-        for (int d = 32; d; d >>= 1) {
-            lo = min(lo, __shfl_xor(lo, d));
-            hi = max(hi, __shfl_xor(hi, d));
-        }
-        if (lane == 0) ends[g] = make_int2(lo, max(lo, hi));
     }
+    __syncthreads();  // (both are there for the workgroup)
+    if (few.groups) plan_sums(a, few, sums, lds.part);
+    __syncthreads();
+    if (many.groups) plan_tiles(a, many, keys, most, before, tile_sums, tiles, list, where, lds);
 }
 
 struct KvSharedWork {
-    float *o;
-    float2 *ml;
-    int32_t *row_pos, *start;
-    int2 *ends;
-    void *rest;
-    size_t bytes;  // without the rest
+    float *o[2];       // partial results of the kernels of few and of many rows
+    float2 *ml[2];
+    uint64_t *sums, *before;
+    uint32_t *tile_sums;
+    KvTile *tiles;
+    KvTileList *list;
+    int2 *where;
+    size_t bytes;
 };
 
-static KvSharedWork shared_work(const KvAttnArgs &a, const KvSharedArgs &s, void *ws)
+// A wave to the rows of a token that share a key head, as many as its lanes reach with 16 bytes each.
+constexpr int kRowsWaves = 4;
+template <class T, int DP>
+__global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const KvSharedArgs a, const KvCut few, const KvCut many,
+                                                                         const KvSharedWork w, uint32_t units, uint32_t per)
 {
-    KvSharedWork w{};
-    char *at = (char *)ws;
-    auto take = [&](size_t bytes) {
-        char *q = at;
-        at += (bytes + 255) & ~size_t(255);
-        return q;
-    };
-    const size_t rows = (size_t)a.T * a.Hq;
-    w.o = (float *)take(rows * padded_dim(a.D) * 4);
-    w.ml = (float2 *)take(rows * 8);
-    w.row_pos = (int32_t *)take((size_t)a.T * 4);
-    w.start = (int32_t *)take(((size_t)s.groups + 1) * 4);
-    w.ends = (int2 *)take((size_t)s.groups * 8);
-    w.rest = at;
-    w.bytes = at - (char *)ws;
-    return w;
+    constexpr int Lanes = DP / 4, Rows = 64 / Lanes;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = lane % Lanes * 4;
+    KvTileList list{0, 0, 0};
+    if (many.groups) list = *w.list;
+    for (uint32_t unit = blockIdx.x * kRowsWaves + wave; unit < units; unit += gridDim.x * kRowsWaves) {
+        const uint32_t part = unit % per, th = unit / per;
+        const int t = th / (uint32_t)a.H, h = th - (uint32_t)t * a.H;
+        const int j = part * Rows + lane / Lanes;  // query head of the key head
+        const int r = __builtin_amdgcn_readfirstlane(kv_find(a.start, a.R, t));
+        const bool own = a.start[r] <= t && t < a.start[r + 1];
+        const int g = __builtin_amdgcn_readfirstlane(kv_find(a.first, a.groups, r));
+        const bool behind = own && a.first[g] <= r && r < a.first[g + 1] && a.p_start[g] <= t && t < a.p_start[g + 1];
+        if (j >= a.G) continue;
+        const int hq = h * a.G + j;
+        const int64_t row_at = (int64_t)t * a.Hq + hq;
+        RowSum<4> s;
+        s.clear();
+        auto add = [&](int i, int source) {
+            const int first = kv_first_token(a, i), n = kv_end_token(a, i) - first, row = (t - first) * a.G + j;
+            KvJoin it{};
+            int kind = 0, y;
+            if (few.groups && n <= few.few) {
+                const KvShare x = kv_share(a, few, i);
+                const int tile = row / few.rows;
+                y = row - tile * few.rows;
+                const uint64_t run = w.sums[a.groups + a.R + 1];
+                const uint64_t u0 = w.sums[i] + ((uint64_t)h * x.tiles + tile) * kv_steps(x), u1 = u0 + kv_steps(x) - 1;
+                const bool small = u1 < 0xffffffffu;  // (then the run is)
+                const uint32_t b0 = small ? (uint32_t)u0 / (uint32_t)run : (uint32_t)(u0 / run);
+                const uint32_t b1 = small ? (uint32_t)u1 / (uint32_t)run : (uint32_t)(u1 / run);
+                it.parts = (int)(b1 - b0) + 1;
+                it.first = kv_part(b0, true);
+                it.next = kv_part(b0 + 1, false);
+                it.stride = 2;
+            } else {
+                kind = 1;
+                const int tile = row / many.rows;
+                y = row - tile * many.rows;
+                const int tiles = (int)(((long long)n * a.G + many.rows - 1) / many.rows);
+                const uint64_t nth = w.before[i] + (tiles - 1 - tile);  // (listed last tile first)
+                if (nth >= (uint64_t)list.count) return;  // (starts that are not ascending)
+                const int2 x = w.where[nth];
+                it.parts = x.y;
+                it.first = x.x + list.parts * h;
+                it.next = it.first + 1;
+                it.stride = 1;
+            }
+            if (it.parts == 1) {
+                const Vec<float, 4> z = *(const Vec<float, 4> *)(a.raw_o[source] + row_at * DP + d);
+                const float x[4] = {z[0], z[1], z[2], z[3]};
+                s.add(a.raw_ml[source][row_at], x);
+            } else if (it.parts == 2) {
+                s.template sum<DP, 2>(it, kind ? many.rows : few.rows, w.o[kind], w.ml[kind], y, d, 0, 1);
+            } else {
+                s.template sum<DP, 8>(it, kind ? many.rows : few.rows, w.o[kind], w.ml[kind], y, d, 0, 1);
+            }
+        };
+        if (behind) add(g, 0);
+        if (own) add(a.groups + r, 1);
+        s.template write_row<T>(a, t, h, hq, d);
+    }
 }
 
-static KvAttnArgs over_prefixes(const KvAttnArgs &a, const KvSharedArgs &s, const KvSharedWork &w)
+static KvPlans shared_plans(const KvSharedArgs &a, int cache_dtype)
 {
-    KvAttnArgs p = a;
-    p.R = s.groups;
-    p.W = s.W;
-    p.max_new = s.max_new;
-    p.start = w.start;
-    p.context = s.context;
-    p.table = s.table;
-    p.table_stride = s.table_stride;
-    p.window = 0;
-    p.prefix = nullptr;
-    p.raw_ml = w.ml;
-    p.raw_o = w.o;
-    p.row_pos = w.row_pos;
-    p.ends = s.window ? w.ends : nullptr;
-    p.prefix_window = s.window;
+    const int DP = padded_dim(a.D), requests = a.groups + a.R;
+    const int few = std::max(((int64_t)requests * a.H < 16 ? 32 : 16) / a.G, 1);
+    // As without prefixes, but single tokens keep their kernel beside groups of many rows, whose
+    // tiles are few and long.
+    const bool all_few = a.max_new <= few && a.p_max_new <= few;
+    const bool all_many = a.max_new > few && (a.R <= kFewRequests || a.T > (int64_t)(a.R - 1) * a.max_new + few);
+    KvPlans p{};
+    if (!all_many) {
+        p.few.rows = 16;
+        p.few.groups = a.num_cu * 4 * kv_decode_waves(cache_dtype, DP);
+        p.few.few = all_few ? 0x7fffffff : few;
+        p.few.below = true;
+    }
+    if (!all_few) {
+        p.many.rows = kv_prefill_rows(DP);
+        p.many.groups = a.num_cu * kv_prefill_groups(DP) / kDies * kDies;
+        p.many.few = all_many ? 0 : few;
+        p.many.below = false;
+        const int64_t longer = all_many ? a.T : a.T / (few + 1) + 1;  // sources that have tiles
+        p.most_tiles = (int)(2 * ((int64_t)a.T * a.G / p.many.rows) + std::min<int64_t>(a.groups, longer) +
+                             std::min<int64_t>(a.R, longer));
+        const int64_t items = (int64_t)p.most_tiles * a.H;
+        p.grid = (unsigned)std::min<int64_t>((items + 2 * p.many.groups + kDies) / kDies * kDies, 1 << 23);
+    }
     return p;
 }
 
-size_t kv_shared_bytes(const KvAttnArgs &a, const KvSharedArgs &s, int cache_dtype)
+// Also sets the scratch of the arguments.
+static KvSharedWork shared_work(KvSharedArgs &a, const KvPlans &p, void *ws)
 {
-    const KvSharedWork w = shared_work(a, s, nullptr);
-    return w.bytes + std::max(kv_attention_bytes(over_prefixes(a, s, w), cache_dtype), kv_attention_bytes(a, cache_dtype));
+    KvSharedWork w{};
+    KvTake take{(char *)ws};
+    const int DP = padded_dim(a.D);
+    const size_t rows = (size_t)a.T * a.Hq, requests = (size_t)a.groups + a.R;
+    for (int i = 0; i < 2; ++i) {
+        take(a.raw_o[i], rows * DP);
+        take(a.raw_ml[i], rows);
+        const KvCut &c = i ? p.many : p.few;
+        take(w.o[i], (size_t)2 * c.groups * c.rows * DP);
+        take(w.ml[i], (size_t)2 * c.groups * c.rows);
+    }
+    take(a.p_start, (size_t)a.groups + 1);
+    take(a.ends, a.groups);
+    take(a.row_pos, a.T);
+    take(w.sums, requests + 2);
+    take(w.before, requests);
+    take(w.tile_sums, (size_t)p.most_tiles + 1);
+    take(w.tiles, p.most_tiles);
+    take(w.where, p.most_tiles);
+    take(w.list, 1);
+    if (!a.p_window) a.ends = nullptr;
+    if (!a.p_window && !a.slopes) a.row_pos = nullptr;
+    w.bytes = take.at - (char *)ws;
+    return w;
 }
 
-hipError_t launch_kv_shared(const KvAttnArgs &a, const KvSharedArgs &s, int dtype, int cache_dtype, void *ws,
-                            hipStream_t st)
+size_t kv_shared_bytes(const KvSharedArgs &a, int cache_dtype)
 {
-    const KvSharedWork w = shared_work(a, s, ws);
-    const KvAttnArgs p = over_prefixes(a, s, w);
-    const int64_t items = std::max((int64_t)a.T * std::max(a.Hq / 4, 1), (int64_t)s.groups * 64);
-    const unsigned blocks = (unsigned)std::min<int64_t>((items + kSharedThreads) / kSharedThreads, 4 * a.num_cu);
-    kv_shared_rows_kernel<<<blocks, kSharedThreads, 0, st>>>(a, s, w.start, w.row_pos, s.window ? w.ends : nullptr, w.ml);
-    if (hipError_t e = attend(p, dtype, cache_dtype, false, w.rest, st)) return e;
-    KvAttnArgs own = a;
-    own.with_ml = w.ml;
-    own.with_o = w.o;
-    return attend(own, dtype, cache_dtype, true, w.rest, st);
+    KvSharedArgs b = a;
+    return shared_work(b, shared_plans(a, cache_dtype), nullptr).bytes;
+}
+
+template <class T> static void run_shared(const KvSharedArgs &a, const KvPlans &p, const KvSharedWork &w, int cache_dtype, hipStream_t st)
+{
+    const int DP = padded_dim(a.D);
+    if (a.row_pos)
+        kv_places_kernel<<<std::min((a.T + kPlaceThreads - 1) / kPlaceThreads, 4 * a.num_cu), kPlaceThreads, 0, st>>>(a);
+    kv_shared_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, p.many, kv_prefill_keys(DP), p.most_tiles, w.sums, w.before,
+                                                      w.tile_sums, w.tiles, w.list, w.where);
+    if (p.many.groups) {
+        const KvTiles t{w.tile_sums, w.tiles, w.list};
+        launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, false, w.o[1], w.ml[1], nullptr, st);
+    }
+    if (p.few.groups) launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, false, w.o[0], w.ml[0], nullptr, st);
+    const int rows = 64 / (DP / 4);  // of a wave
+    const uint32_t per = (uint32_t)(a.G + rows - 1) / rows, units = (uint32_t)a.T * a.H * per;
+    const unsigned blocks = std::min((units + kRowsWaves - 1) / kRowsWaves, 1u << 20);
+    auto kernel = DP == 64 ? kv_shared_join_kernel<T, 64> : DP == 128 ? kv_shared_join_kernel<T, 128> : kv_shared_join_kernel<T, 256>;
+    kernel<<<blocks, kRowsWaves * 64, 0, st>>>(a, p.few, p.many, w, units, per);
+}
+
+hipError_t launch_kv_shared(KvSharedArgs a, int dtype, int cache_dtype, void *ws, hipStream_t st)
+{
+    const KvPlans p = shared_plans(a, cache_dtype);
+    const KvSharedWork w = shared_work(a, p, ws);
+    if (dtype == DRO_BF16) run_shared<bf16>(a, p, w, cache_dtype, st);
+    else run_shared<f16>(a, p, w, cache_dtype, st);
+    return hipGetLastError();
 }
 
 }  // namespace dro

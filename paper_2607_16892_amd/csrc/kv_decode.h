@@ -34,9 +34,9 @@ constexpr int decode_waves(int DP, int E) { return DP == 256 ? 1 : DP * E >= 256
 // are widened by one instruction a pair that takes the power as well, to exactly what they stand
 // for (in f16 rounded), and from there on are values of T like any other.
 
-template <class T, class C, int DP, bool FULL>
+template <class T, class C, int DP, bool FULL, class A>
 __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decode_kernel(
-    const KvAttnArgs a, const KvCut cut, const uint64_t *sums, bool pad, float *part_o, float2 *part_ml,
+    const A a, const KvCut cut, const uint64_t *sums, bool pad, float *part_o, float2 *part_ml,
     KvJoin *joins)
 {
     constexpr int S = DP / 32;             // steps of 32 components of a score
@@ -57,9 +57,9 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         else return x * 32 + grp * 8;
     };
 
-    KvSched sched;
+    KvSched<A> sched;
     sched.init(a, cut, sums, lds);
-    if (threadIdx.x == 0) joins[blockIdx.x].parts = 0;
+    if (!kShared<A> && threadIdx.x == 0) joins[blockIdx.x].parts = 0;
     uint64_t unit = blockIdx.x * sched.run;
     const uint64_t end = min(unit + sched.run, sched.all);
     if (pad && (gridDim.x - 1) * sched.run < sched.all) {
@@ -75,15 +75,15 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         const int h = it.head, r = it.r;
         const int row0 = it.tile * kDecodeRows;
         const int rows = min(it.n * a.G - row0, kDecodeRows);
-        const int prefix = a.prefix ? a.prefix[r] : 0;
+        const int prefix = kv_prefix_of(a, r);
 
         // this lane's row
         const int row = row0 + min(n16, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
-        const KvRange see = kv_see(a, it.ctx, it.n, token, prefix, it.first_token + token);
+        const KvRange see = kv_see(a, r, it.ctx, it.n, token, prefix, it.first_token + token);
         // the tile's keys: those that some row sees, and those that every row sees
-        const KvRange top = kv_first(a, r, it.ctx, it.n, row0 / a.G, prefix);
-        const KvRange bot = kv_last(a, r, it.ctx, it.n, (row0 + rows - 1) / a.G, prefix);
+        const KvRange top = kv_first_range(a, r, it.ctx, it.n, row0 / a.G, prefix);
+        const KvRange bot = kv_last_range(a, r, it.ctx, it.n, (row0 + rows - 1) / a.G, prefix);
         const int all_lo = bot.lo, all_hi = top.hi;
         const int base = top.lo & ~(kStepKeys - 1);
         const int k0 = min(base + it.step * kStepKeys, bot.hi);
@@ -104,14 +104,14 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         // to_exp leads to the exponent of its tanh
         const float slope = a.slopes ? a.slopes[hq] * kLog2e : 0.0f;
         const float cap = a.cap * kLog2e, to_exp = a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
-        const int p_row = a.slopes ? kv_row_place(a, it.ctx, it.n, token, it.first_token + token) : 0;
+        const int p_row = kShared<A> && !a.slopes ? 0 : kv_row_place(a, r, it.ctx, it.n, token, it.first_token + token);
 
         const char *kp = (const char *)a.k + bytes_of<C>((int64_t)h * a.k_head);
         const char *vp = (const char *)a.v + bytes_of<C>((int64_t)h * a.v_head);
         const int in_block = (1 << a.shift) - 1;
         const uint32_t k_lane = bytes_of<C>((uint32_t)(n16 * (int)a.k_token + component(0)));
         const uint32_t v_lane = bytes_of<C>((uint32_t)(grp * 4 * (int)a.v_token + n16 * VW));
-        const int32_t *table = a.table + (int64_t)r * a.table_stride;
+        const int32_t *table = kv_table(a, r);
 
         float m = -INFINITY, l = 0.0f;
         f32x4 o[VW];
@@ -393,25 +393,11 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         if (n16 < rows) {
             const int64_t t = it.first_token + token;
             const int64_t at = (int64_t)kv_part(blockIdx.x, it.step == 0) * kDecodeRows + n16;
-            const int64_t row_at = t * a.Hq + hq;
-            if (whole && a.with_ml) {  // behind a shared prefix
-                float by;
-                const float f = join_scales(m, l, a.with_ml[row_at], by);
-                const float *z = a.with_o + row_at * DP;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int j = 0; j < VW; j += 4) {
-                        if (by == 0.0f) continue;  // (and what is there may be anything)
-                        const f32x4 y = *(const f32x4 *)(z + VW * (grp * 4 + c) + j);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[j + i][c] = o[j + i][c] * f + by * y[i];
-                    }
-            }
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
-            const bool raw = !whole || a.raw_ml;
-            float *to = whole ? a.raw_o + row_at * DP : part_o + at * DP;
+            const bool raw = kShared<A> || !whole;  // (behind prefixes rows are joined afterwards)
+            const int64_t row_at = t * a.Hq + hq, raw_at = kShared<A> && whole ? row_at : at;
+            const KvRaw<A> to = kShared<A> && whole ? kv_raw(a, r) : KvRaw<A>{part_o, part_ml};
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -419,18 +405,18 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
                     const int d = VW * (grp * 4 + c) + j;
                     const f32x4 x = {o[j][c], o[j + 1][c], o[j + 2][c], o[j + 3][c]};
                     if (raw)
-                        *(f32x4 *)&to[d] = x;
+                        *(f32x4 *)&to.o[raw_at * DP + d] = x;
                     else if (FULL || d < a.D)
                         *(uint2 *)(out + d) = l == 0.0f ? make_uint2(0, 0)
                                                         : make_uint2(pack2<T>(x[0] * inv, x[1] * inv),
                                                                      pack2<T>(x[2] * inv, x[3] * inv));
                 }
             if (grp == 0) {
-                if (raw) (whole ? a.raw_ml + row_at : part_ml + at)[0] = make_float2(m, l);
+                if (raw) to.ml[raw_at] = make_float2(m, l);
                 else if (a.lse) a.lse[row_at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }
         }
-        if (!whole && it.step == 0 && lane == 0) {
+        if (!kShared<A> && !whole && it.step == 0 && lane == 0) {
             // (the item's last step lies `it.steps - go` steps beyond this run's end)
             KvJoin &j = joins[blockIdx.x];
             j.parts = 1 + (int)((it.steps - go + sched.run - 1) / sched.run);
@@ -445,32 +431,23 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
     }
 }
 
-template <class T, class C>
-void run_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, int DP, bool pad, float *o,
-                   float2 *ml, KvJoin *joins, hipStream_t st)
-{
-    constexpr int kThreads = 64;
-    const bool full = a.D == DP;
-    if (DP == 64) {
-        if (full) kv_decode_kernel<T, C, 64, true><<<c.groups, kThreads, 0, st>>>(a, c, sums, pad, o, ml, joins);
-        else kv_decode_kernel<T, C, 64, false><<<c.groups, kThreads, 0, st>>>(a, c, sums, pad, o, ml, joins);
-    } else if (DP == 128) {
-        if (full) kv_decode_kernel<T, C, 128, true><<<c.groups, kThreads, 0, st>>>(a, c, sums, pad, o, ml, joins);
-        else kv_decode_kernel<T, C, 128, false><<<c.groups, kThreads, 0, st>>>(a, c, sums, pad, o, ml, joins);
-    } else {
-        if (full) kv_decode_kernel<T, C, 256, true><<<c.groups, kThreads, 0, st>>>(a, c, sums, pad, o, ml, joins);
-        else kv_decode_kernel<T, C, 256, false><<<c.groups, kThreads, 0, st>>>(a, c, sums, pad, o, ml, joins);
-    }
-}
-
-template <class T>
-void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, int cache_dtype, int DP,
+template <class T, class A>
+void launch_kv_decode(const A &a, const KvCut &c, const uint64_t *sums, int cache_dtype, int DP,
                       bool pad, float *o, float2 *ml, KvJoin *joins, hipStream_t st)
 {
-    if (cache_dtype == DRO_FP8_E4M3) run_kv_decode<T, fp8>(a, c, sums, DP, pad, o, ml, joins, st);
-    else if (cache_dtype == DRO_MXFP4) run_kv_decode<T, mx4>(a, c, sums, DP, pad, o, ml, joins, st);
-    else if (cache_dtype == DRO_MXFP8) run_kv_decode<T, mx8>(a, c, sums, DP, pad, o, ml, joins, st);
-    else run_kv_decode<T, T>(a, c, sums, DP, pad, o, ml, joins, st);
+    auto go = [&](auto kernel) { kernel<<<c.groups, 64, 0, st>>>(a, c, sums, pad, o, ml, joins); };
+    auto of = [&](auto cache) {
+        using C = decltype(cache);
+        using K = KvKernelArgs<A, C>;
+        const bool full = a.D == DP;
+        if (DP == 64) full ? go(kv_decode_kernel<T, C, 64, true, K>) : go(kv_decode_kernel<T, C, 64, false, K>);
+        else if (DP == 128) full ? go(kv_decode_kernel<T, C, 128, true, K>) : go(kv_decode_kernel<T, C, 128, false, K>);
+        else full ? go(kv_decode_kernel<T, C, 256, true, K>) : go(kv_decode_kernel<T, C, 256, false, K>);
+    };
+    if (cache_dtype == DRO_FP8_E4M3) of(fp8{});
+    else if (cache_dtype == DRO_MXFP4) of(mx4{});
+    else if (cache_dtype == DRO_MXFP8) of(mx8{});
+    else of(T{});
 }
 
 }  // namespace dro

@@ -2,7 +2,7 @@
 #include "kv_decode.h"
 
 namespace dro {
-template void launch_kv_decode<bf16>(const KvAttnArgs &, const KvCut &, const uint64_t *, int, int, bool, float *,
+template void launch_kv_decode<bf16>(const KvMxArgs &, const KvCut &, const uint64_t *, int, int, bool, float *,
                                    float2 *, KvJoin *, hipStream_t);
 int kv_decode_waves(int cache_dtype, int DP)
 {

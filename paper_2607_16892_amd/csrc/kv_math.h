@@ -131,19 +131,6 @@ template <int N> __device__ __forceinline__ Words<N> load_words(const char *base
     return x;
 }
 
-// A row's running sums (of weights up to 2^(m - ..), V components) joined with others' of the row.
-// Returns what its own are to be multiplied by, and gives what the others' are.
-__device__ __forceinline__ float join_scales(float &m, float &l, float2 x, float &by)
-{
-    by = 0.0f;
-    if (x.y == 0.0f) return 1.0f;  // no key that the row sees
-    const float to = fmaxf(m, x.x), own = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-    by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - to);
-    m = to;
-    l = l * own + by * x.y;
-    return own;
-}
-
 // The rows of no request, by workgroup `nth` of `of`: those without other work, where there are
 // any, since the others' way to their first keys is a chain of loads already.
 template <class T> __device__ __forceinline__ void zero_rows(const KvAttnArgs &a, uint32_t nth, uint32_t of)

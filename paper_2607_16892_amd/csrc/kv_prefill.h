@@ -98,9 +98,9 @@ typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
 typedef const __attribute__((address_space(1))) void *GlobalPtr;
 typedef __attribute__((address_space(3))) void *LdsPtr;
 
-template <class T, class C, int DP, bool MODS, bool FULL>
+template <class T, class C, int DP, bool MODS, bool FULL, class A>
 __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
-    const KvAttnArgs a, const KvCut cut, const KvTiles tiles, bool pad, float *part_o, float2 *part_ml,
+    const A a, const KvCut cut, const KvTiles tiles, bool pad, float *part_o, float2 *part_ml,
     KvJoin *joins)
 {
     constexpr bool F8 = __is_same(C, fp8), MX = kMx<C>;
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     const bool by_head = a.H % kDies == 0;
     if (pad && gridDim.x <= all) zero_rows<T>(a, blockIdx.x, gridDim.x);
     else if (pad && blockIdx.x >= all) zero_rows<T>(a, blockIdx.x - all, gridDim.x - all);
-    if (blockIdx.x == 0)  // places of no tile
+    if (!kShared<A> && blockIdx.x == 0)  // places of no tile
         for (int i = list.parts * a.H + threadIdx.x; i < 2 * cut.groups; i += 256) joins[i].parts = 0;
     for (uint32_t unit = blockIdx.x; unit < all; unit += gridDim.x) {
         const uint32_t nth = unit / kDies, per = by_head ? all1 : (uint32_t)a.H, quot = (by_head ? nth : unit) / per,
@@ -165,22 +165,22 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         const int first_token = rt.first_token;
         const int row0 = tile * Rows;
         const int rows = min(rt.n * a.G - row0, Rows);
-        const int prefix = a.prefix ? a.prefix[r] : 0;
-        const KvRange top = kv_first(a, r, rt.ctx, rt.n, row0 / a.G, prefix);
-        const KvRange bot = kv_last(a, r, rt.ctx, rt.n, (row0 + rows - 1) / a.G, prefix);
+        const int prefix = kv_prefix_of(a, r);
+        const KvRange top = kv_first_range(a, r, rt.ctx, rt.n, row0 / a.G, prefix);
+        const KvRange bot = kv_last_range(a, r, rt.ctx, rt.n, (row0 + rows - 1) / a.G, prefix);
         const int base = top.lo & ~31;
         const int k0 = min(base + step0 * KT, bot.hi), k1 = min(base + (step0 + go) * KT, bot.hi);
         const int steps = (k1 - k0 + KT - 1) / KT;
 
         // this wave's rows, and this lane's
         const int wrow = min(rw, rows - 1), wlast = min(rw + 31, rows - 1);
-        const KvRange wtop = kv_first(a, r, rt.ctx, rt.n, (row0 + wrow) / a.G, prefix);
-        const KvRange wbot = kv_last(a, r, rt.ctx, rt.n, (row0 + wlast) / a.G, prefix);
+        const KvRange wtop = kv_first_range(a, r, rt.ctx, rt.n, (row0 + wrow) / a.G, prefix);
+        const KvRange wbot = kv_last_range(a, r, rt.ctx, rt.n, (row0 + wlast) / a.G, prefix);
         const bool idle = rw >= rows;
         const int row = row0 + min(rw + n32, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
-        const KvRange see = kv_see(a, rt.ctx, rt.n, token, prefix, first_token + token);
-        const int p_row = MODS ? kv_row_place(a, rt.ctx, rt.n, token, first_token + token) : 0;
+        const KvRange see = kv_see(a, r, rt.ctx, rt.n, token, prefix, first_token + token);
+        const int p_row = kShared<A> && (!MODS || !a.slopes) ? 0 : kv_row_place(a, r, rt.ctx, rt.n, token, first_token + token);
 
         u32x4 q[S];
         {
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 
         // Staging: piece x = lane of load i of group j goes to place 1024 i + 16 lane of the
         // group's rows, so the lane picks the piece of its row that belongs there.
-        const ScalarInts table = (ScalarInts)(a.table + (int64_t)r * a.table_stride);
+        const ScalarInts table = (ScalarInts)kv_table(a, r);
         const int in_block = (1 << a.shift) - 1;
         int ids[UP];
         auto load_ids = [&](int u) {
@@ -228,11 +228,13 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const int in = (k0 + u * KT + group * 16) & in_block;
                 const char *base = (vals ? (const char *)a.v + bytes_of<C>(h * a.v_head) : (const char *)a.k + bytes_of<C>(h * a.k_head)) +
                                    bytes_of<C>(id * (vals ? a.v_block : a.k_block) + in * s_token);
-                const int64_t p_token = vals ? a.vp_token : a.kp_token;
+                int64_t p_token = 0;
                 const uint8_t *pw = nullptr;
-                if constexpr (MX)
+                if constexpr (MX) {
+                    p_token = vals ? a.vp_token : a.kp_token;
                     pw = vals ? a.v_power + h * a.vp_head + id * a.vp_block + in * p_token
                               : a.k_power + h * a.kp_head + id * a.kp_block + in * p_token;
+                }
 #pragma unroll
                 for (int i = 0; i < IP; ++i) {
                     const int rr = i * RP + lane / NC;
@@ -515,44 +517,29 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         if (rw + n32 < rows) {
             const int64_t t = first_token + token;
             const int64_t at = (int64_t)place * Rows + rw + n32;
-            const int64_t row_at = t * a.Hq + hq;
-            const bool first = half == 0 && dt0 == 0;
-            if (whole && a.with_ml) {  // behind a shared prefix
-                float by;
-                const float f = join_scales(m, l, a.with_ml[row_at], by);
-                const float *z = a.with_o + row_at * DP;
-#pragma unroll
-                for (int j = 0; j < ND; ++j)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        if (by == 0.0f) continue;  // (and what is there may be anything)
-                        const f32x4 y = *(const f32x4 *)(z + (dt0 + j) * 32 + (i >> 2) * 8 + half * 4);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[j][i + e] = o[j][i + e] * f + by * y[e];
-                    }
-            }
             const float inv = l == 0.0f ? 0.0f : (F8 ? a.v_scale[h] : 1.0f) / l;
             T *out = (T *)a.out + t * a.out_token + hq * a.out_head;
-            const bool raw = !whole || a.raw_ml;
-            float *to = whole ? a.raw_o + row_at * DP : part_o + at * DP;
+            const bool raw = kShared<A> || !whole;  // (behind prefixes rows are joined afterwards)
+            const int64_t row_at = t * a.Hq + hq, raw_at = kShared<A> && whole ? row_at : at;
+            const KvRaw<A> to = kShared<A> && whole ? kv_raw(a, r) : KvRaw<A>{part_o, part_ml};
 #pragma unroll
             for (int j = 0; j < ND; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const int d = (dt0 + j) * 32 + (i >> 2) * 8 + half * 4;
                     if (raw)
-                        *(f32x4 *)&to[d] = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
+                        *(f32x4 *)&to.o[raw_at * DP + d] = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
                     else if (FULL || d < a.D)
                         *(uint2 *)(out + d) = l == 0.0f ? make_uint2(0, 0)
                                                         : make_uint2(pack2<T>(o[j][i] * inv, o[j][i + 1] * inv),
                                                                      pack2<T>(o[j][i + 2] * inv, o[j][i + 3] * inv));
                 }
-            if (first) {
-                if (raw) (whole ? a.raw_ml + row_at : part_ml + at)[0] = make_float2(m, l);
+            if (half == 0 && dt0 == 0) {
+                if (raw) to.ml[raw_at] = make_float2(m, l);
                 else if (a.lse) a.lse[row_at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }
         }
-        if (!whole && threadIdx.x == 0) {
+        if (!kShared<A> && !whole && threadIdx.x == 0) {
             KvJoin &j = joins[place];
             j.parts = chunk ? 0 : rt.chunks;
             j.first_token = first_token;
@@ -566,33 +553,32 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
     }
 }
 
-template <class T, class C, int DP>
-void run_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, bool pad, float *o, float2 *ml,
-                    KvJoin *joins, hipStream_t st)
+template <class T, class A>
+void launch_kv_prefill(const A &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
+                       float *o, float2 *ml, KvJoin *joins, hipStream_t st)
 {
-    auto run = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
     // A head dimension between the padded ones takes the kernel of all score changes as well.  Its
     // instances beyond 64 components keep 76 to 97 registers in scratch memory, and so do those of 128
     // with score changes (14, with 8 bits 49) and of 256 in 8 bits with them (4): read back in the
     // steps, behind the next tile's loads.
-    if (a.D != DP) run(kv_prefill_kernel<T, C, DP, true, false>);
-    else if (a.cap > 0.0f || a.slopes || a.scale == 0.0f) run(kv_prefill_kernel<T, C, DP, true, true>);
-    else run(kv_prefill_kernel<T, C, DP, false, true>);
-}
-
-template <class T>
-void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
-                       float *o, float2 *ml, KvJoin *joins, hipStream_t st)
-{
-    auto run = [&](auto c0) {
-        using C = decltype(c0);
-        (DP == 64 ? run_kv_prefill<T, C, 64> : DP == 128 ? run_kv_prefill<T, C, 128> : run_kv_prefill<T, C, 256>)(
-            a, c, t, grid, pad, o, ml, joins, st);
+    auto of = [&](auto cache, auto dim) {
+        using C = decltype(cache);
+        using K = KvKernelArgs<A, C>;
+        constexpr int P = decltype(dim)::value;
+        if (a.D != P) go(kv_prefill_kernel<T, C, P, true, false, K>);
+        else if (a.cap > 0.0f || a.slopes || a.scale == 0.0f) go(kv_prefill_kernel<T, C, P, true, true, K>);
+        else go(kv_prefill_kernel<T, C, P, false, true, K>);
     };
-    if (cache_dtype == DRO_FP8_E4M3) run(fp8{});
-    else if (cache_dtype == DRO_MXFP4) run(mx4{});
-    else if (cache_dtype == DRO_MXFP8) run(mx8{});
-    else run(T{});
+    auto with = [&](auto cache) {
+        if (DP == 64) of(cache, std::integral_constant<int, 64>{});
+        else if (DP == 128) of(cache, std::integral_constant<int, 128>{});
+        else of(cache, std::integral_constant<int, 256>{});
+    };
+    if (cache_dtype == DRO_FP8_E4M3) with(fp8{});
+    else if (cache_dtype == DRO_MXFP4) with(mx4{});
+    else if (cache_dtype == DRO_MXFP8) with(mx8{});
+    else with(T{});
 }
 
 }  // namespace dro

@@ -2,7 +2,7 @@
 #include "kv_prefill.h"
 
 namespace dro {
-template void launch_kv_prefill<bf16>(const KvAttnArgs &, const KvCut &, const KvTiles &, unsigned, int, int, bool, float *,
+template void launch_kv_prefill<bf16>(const KvMxArgs &, const KvCut &, const KvTiles &, unsigned, int, int, bool, float *,
                                     float2 *, KvJoin *, hipStream_t);
 int kv_prefill_groups(int DP) { return prefill_groups(DP); }
 int kv_prefill_rows(int DP) { return prefill_rows(DP); }

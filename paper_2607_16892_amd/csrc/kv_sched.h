@@ -9,7 +9,10 @@
 // an item leaves a partial result, at most two a workgroup, for the join.
 #pragma once
 
+#include <type_traits>
+
 #include "kv.h"
+#include "kv_types.h"
 #include "wave.h"
 
 namespace dro {
@@ -48,21 +51,70 @@ struct KvCut {
 
 constexpr int kStepKeys = 32;
 
-__device__ __forceinline__ KvShare kv_share(const KvAttnArgs &a, const KvCut &c, int r)
+template <class A> constexpr bool kShared = __is_same(A, KvSharedArgs);
+
+// The requests, or the sources of keys: the groups' prefixes, then the requests' own tokens.
+template <class A> __device__ __forceinline__ int kv_requests(const A &a)
+{
+    if constexpr (kShared<A>) return a.groups + a.R;
+    else return a.R;
+}
+template <class A> __device__ __forceinline__ bool kv_is_prefix(const A &a, int r)
+{
+    if constexpr (kShared<A>) return r < a.groups;
+    else return false;
+}
+template <class A> __device__ __forceinline__ int kv_own(const A &a, int r)  // the request's number
+{
+    if constexpr (kShared<A>) return r - a.groups;
+    else return r;
+}
+template <class A> __device__ __forceinline__ int kv_first_token(const A &a, int r)
+{
+    if constexpr (kShared<A>)
+        if (r < a.groups) return a.p_start[r];
+    return min(max(a.start[kv_own(a, r)], 0), a.T);
+}
+template <class A> __device__ __forceinline__ int kv_end_token(const A &a, int r)
+{
+    if constexpr (kShared<A>)
+        if (r < a.groups) return a.p_start[r + 1];
+    return min(max(a.start[kv_own(a, r) + 1], 0), a.T);
+}
+template <class A> __device__ __forceinline__ int kv_context(const A &a, int r)
+{
+    if constexpr (kShared<A>)
+        if (r < a.groups) return (int)min((long long)max(a.p_context[r], 0), (long long)a.p_W << a.shift);
+    return (int)min((long long)max(a.context[kv_own(a, r)], 0), (long long)a.W << a.shift);
+}
+template <class A> __device__ __forceinline__ const int32_t *kv_table(const A &a, int r)
+{
+    if constexpr (kShared<A>)
+        if (r < a.groups) return a.p_table + (int64_t)r * a.p_stride;
+    return a.table + (int64_t)kv_own(a, r) * a.table_stride;
+}
+template <class A> __device__ __forceinline__ int kv_prefix_of(const A &a, int r)  // keys that all rows see
+{
+    return a.prefix && !kv_is_prefix(a, r) ? a.prefix[kv_own(a, r)] : 0;
+}
+
+template <class A> __device__ __forceinline__ KvShare kv_share(const A &a, const KvCut &c, int r)
 {
     KvShare s{0, 0, 0, 0};
-    if (r >= a.R) return s;
-    const int t0 = min(max(a.start[r], 0), a.T), t1 = min(max(a.start[r + 1], 0), a.T);
-    const int n = max(t1 - t0, 0);
+    if (r >= kv_requests(a)) return s;
+    const int n = max(kv_end_token(a, r) - kv_first_token(a, r), 0);
     if (n == 0 || (n <= c.few) != c.below) return s;
     s.n = n;
-    s.ctx = (int)min((long long)max(a.context[r], 0), (long long)a.W << a.shift);
+    s.ctx = kv_context(a, r);
     s.tiles = (int)(((long long)n * a.G + c.rows - 1) / c.rows);
     s.span = s.ctx;
-    if (a.window && !a.prefix)  // a tile's rows lie within rows / G + 2 tokens
+    if (kv_is_prefix(a, r)) {
+        if constexpr (kShared<A>)
+            if (a.ends) s.span = s.ctx - (a.ends[r].x & ~(kStepKeys - 1));
+    } else if (a.window && !a.prefix) {  // a tile's rows lie within rows / G + 2 tokens
         s.span = (int)min((long long)s.ctx,
                           (long long)a.window + min(c.rows / a.G + 2, n) + kStepKeys);
-    if (a.ends) s.span = s.ctx - (a.ends[r].x & ~(kStepKeys - 1));
+    }
     return s;
 }
 
@@ -79,11 +131,14 @@ __device__ __forceinline__ uint64_t kv_units(const KvAttnArgs &a, const KvShare 
 // item of many steps alone would be cut so fine that the join takes longer than the steps (one
 // request of 131,000 keys, 8 heads on one: 81 us with runs of one step, 34 with eight; of
 // 16,000: 27 with one, 19 with two).
-__device__ __forceinline__ uint64_t kv_run(const KvCut &c, uint64_t all, uint32_t longest)
+__device__ __forceinline__ uint64_t kv_run_of(const KvCut &c, uint64_t all, uint64_t least)
 {
-    const uint64_t least = __any(longest >= 2048) ? 8 : __any(longest >= 512) ? 4 : __any(longest >= 128) ? 2 : 1;
     if (all < 0xffff0000u) return max((uint64_t)(((uint32_t)all + (uint32_t)c.groups - 1) / (uint32_t)c.groups), least);
     return (all + c.groups - 1) / (uint32_t)c.groups;
+}
+__device__ __forceinline__ uint64_t kv_run(const KvCut &c, uint64_t all, uint32_t longest)
+{
+    return kv_run_of(c, all, __any(longest >= 2048) ? 8 : __any(longest >= 512) ? 4 : __any(longest >= 128) ? 2 : 1);
 }
 
 // First index of the ascending x[0 .. n) whose next entry exceeds v (the n-th counts as
@@ -109,14 +164,17 @@ struct KvLds {
 };
 
 // The items by their steps: from the workgroup's own scan in LDS, or, beyond
-// kInlineRequests, from the exclusive sums [R + 1] of kv_plan_kernel.
-struct KvSched {
+// kInlineRequests and behind shared prefixes, from the exclusive sums [n + 2] of a launch before
+// (the last: steps a workgroup).
+template <class A> struct KvSched {
     uint64_t all, run;  // all steps, and those of a workgroup
 
+    static __device__ __forceinline__ bool scanned(const A &a) { return !kShared<A> && a.R <= kInlineRequests; }
+
     // (all waves; the results are in LDS after it)
-    __device__ __forceinline__ void init(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, KvLds &lds)
+    __device__ __forceinline__ void init(const A &a, const KvCut &c, const uint64_t *sums, KvLds &lds)
     {
-        if (a.R <= kInlineRequests) {
+        if (scanned(a)) {
             const int lane = threadIdx.x & 63;
             const KvShare s = kv_share(a, c, lane);
             const uint64_t upto = scan_wave(kv_units(a, s));
@@ -128,24 +186,24 @@ struct KvSched {
             __syncthreads();
             run = kv_run(c, all, kv_steps(s));
         } else {
-            all = sums[a.R];
-            run = kv_run(c, all, 1);
+            all = sums[kv_requests(a)];
+            run = kShared<A> ? sums[kv_requests(a) + 1] : kv_run(c, all, 1);
         }
     }
 
     // The item that step u (< all, uniform) belongs to.
-    __device__ __forceinline__ KvItem item(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums,
+    __device__ __forceinline__ KvItem item(const A &a, const KvCut &c, const uint64_t *sums,
                                            const KvLds &lds, uint64_t u) const
     {
         KvItem w;
         KvShare s;
         uint64_t first;
-        if (a.R <= kInlineRequests) {
+        if (scanned(a)) {
             w.r = __builtin_ctzll(__ballot(lds.upto[threadIdx.x & 63] > u));
             first = w.r ? lds.upto[w.r - 1] : 0;
             s = lds.share[w.r];
         } else {
-            w.r = __builtin_amdgcn_readfirstlane(kv_find(sums, a.R, u));
+            w.r = __builtin_amdgcn_readfirstlane(kv_find(sums, kv_requests(a), u));
             first = sums[w.r];
             s = kv_share(a, c, w.r);
         }
@@ -153,7 +211,7 @@ struct KvSched {
         w.n = uniform(s.n);
         w.ctx = uniform(s.ctx);
         w.steps = uniform((int)kv_steps(s));
-        w.first_token = uniform(min(max(a.start[w.r], 0), a.T));
+        w.first_token = uniform(kv_first_token(a, w.r));
         const uint64_t local = u - first;
         uint32_t item;
         if (local < 0xffffffffu) item = (uint32_t)local / (uint32_t)w.steps;
@@ -183,38 +241,59 @@ struct KvRange {
 };
 __device__ __forceinline__ KvRange kv_row_range(const KvAttnArgs &a, int ctx, int n, int token, int prefix)
 {
-    KvRange v{0, ctx};
-    if (a.raw_ml) return v;
     const int p = ctx - n + token;  // negative where the cache holds fewer tokens than there are rows
+    KvRange v;
     v.hi = min(max(p + 1, prefix), ctx);
     v.lo = a.window ? max(p - a.window + 1, 0) : 0;
     return v;
 }
-// The same of the row itself, t of the call's (a prefix's keys have a window by the row's place), and
-// of the first and the last of some rows: up to where no row of them sees keys, and from where on
-// all do.
-__device__ __forceinline__ KvRange kv_see(const KvAttnArgs &a, int ctx, int n, int token, int prefix, int t)
+// The same of a row of request or group r; it is row t of the call's.  A shared prefix is seen by
+// all rows of its group, but for a window by their places.
+template <class A>
+__device__ __forceinline__ KvRange kv_see(const A &a, int r, int ctx, int n, int token, int prefix, int t)
 {
-    KvRange v = kv_row_range(a, ctx, n, token, prefix);
-    if (a.ends) v.lo = (int)min(max((long long)ctx + a.row_pos[t] - a.prefix_window + 1, 0LL), (long long)ctx);
+    if (!kv_is_prefix(a, r)) return kv_row_range(a, ctx, n, token, prefix);
+    KvRange v{0, ctx};
+    if constexpr (kShared<A>)
+        if (a.ends) v.lo = (int)min(max((long long)ctx + a.row_pos[t] - a.p_window + 1, 0LL), (long long)ctx);
     return v;
 }
-__device__ __forceinline__ KvRange kv_first(const KvAttnArgs &a, int r, int ctx, int n, int token, int prefix)
+// The same of the first and of the last of some rows: up to where none of them sees keys, and from
+// where on all do.
+template <class A>
+__device__ __forceinline__ KvRange kv_first_range(const A &a, int r, int ctx, int n, int token, int prefix)
 {
-    KvRange v = kv_row_range(a, ctx, n, token, prefix);
-    if (a.ends) v.lo = a.ends[r].x;
+    if (!kv_is_prefix(a, r)) return kv_row_range(a, ctx, n, token, prefix);
+    KvRange v{0, ctx};
+    if constexpr (kShared<A>)
+        if (a.ends) v.lo = a.ends[r].x;
     return v;
 }
-__device__ __forceinline__ KvRange kv_last(const KvAttnArgs &a, int r, int ctx, int n, int token, int prefix)
+template <class A>
+__device__ __forceinline__ KvRange kv_last_range(const A &a, int r, int ctx, int n, int token, int prefix)
 {
-    KvRange v = kv_row_range(a, ctx, n, token, prefix);
-    if (a.ends) v.lo = a.ends[r].y;
+    if (!kv_is_prefix(a, r)) return kv_row_range(a, ctx, n, token, prefix);
+    KvRange v{0, ctx};
+    if constexpr (kShared<A>)
+        if (a.ends) v.lo = a.ends[r].y;
     return v;
 }
-// The row's place, for a bias by distance.
-__device__ __forceinline__ int kv_row_place(const KvAttnArgs &a, int ctx, int n, int token, int t)
+// A row's place, counted from its source's first key, for a bias by distance.
+template <class A> __device__ __forceinline__ int kv_row_place(const A &a, int r, int ctx, int n, int token, int t)
 {
-    return a.raw_ml ? ctx + a.row_pos[t] : ctx - n + token;
+    if constexpr (kShared<A>)
+        if (r < a.groups) return ctx + a.row_pos[t];
+    return ctx - n + token;
+}
+// Where a finished row of sums goes that is joined with its other source's.
+template <class A> struct KvRaw {
+    float *o;
+    float2 *ml;
+};
+template <class A> __device__ __forceinline__ KvRaw<A> kv_raw(const A &a, int r)
+{
+    if constexpr (kShared<A>) return {a.raw_o[r >= a.groups], a.raw_ml[r >= a.groups]};
+    else return {nullptr, nullptr};
 }
 
 // ---- many rows a request ------------------------------------------------------------
@@ -241,13 +320,13 @@ struct KvTiles {
 };
 
 // Steps of `keys` keys of a tile.
-__device__ __forceinline__ uint32_t kv_tile_steps(const KvAttnArgs &a, const KvShare &s, int r, int tile, int rows,
-                                                  int keys)
+template <class A>
+__device__ __forceinline__ uint32_t kv_tile_steps(const A &a, const KvShare &s, int r, int tile, int rows, int keys)
 {
-    const int prefix = a.prefix ? a.prefix[r] : 0, row0 = tile * rows;
+    const int prefix = kv_prefix_of(a, r), row0 = tile * rows;
     const int last = min(s.n - 1, (row0 + rows - 1) / a.G);
-    const int lo = kv_first(a, r, s.ctx, s.n, row0 / a.G, prefix).lo & ~31;
-    const int hi = kv_row_range(a, s.ctx, s.n, last, prefix).hi;
+    const int lo = kv_first_range(a, r, s.ctx, s.n, row0 / a.G, prefix).lo & ~31;
+    const int hi = kv_last_range(a, r, s.ctx, s.n, last, prefix).hi;
     return (uint32_t)max((hi - lo + keys - 1) / keys, 1);
 }
 
@@ -259,16 +338,19 @@ __device__ __forceinline__ uint64_t kv_tile_share(const KvCut &c, uint64_t all)
     return max((all + (uint32_t)c.groups - 1) / (uint32_t)c.groups, (uint64_t)4);
 }
 
+// What a kernel over a cache of type C takes, of arguments A (KvMxArgs or KvSharedArgs).
+template <class A, class C> using KvKernelArgs = std::conditional_t<kShared<A> || kMx<C>, A, KvAttnArgs>;
+
 // The kernels of few and of many rows a request; they zero the rows of no request as well
 // if `pad`.
-template <class T>
-void launch_kv_decode(const KvAttnArgs &a, const KvCut &c, const uint64_t *sums, int cache_dtype, int DP,
+template <class T, class A>
+void launch_kv_decode(const A &a, const KvCut &c, const uint64_t *sums, int cache_dtype, int DP,
                       bool pad, float *o, float2 *ml, KvJoin *joins, hipStream_t st);
 // its waves a SIMD
 int kv_decode_waves(int cache_dtype, int DP);
 
-template <class T>
-void launch_kv_prefill(const KvAttnArgs &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
+template <class T, class A>
+void launch_kv_prefill(const A &a, const KvCut &c, const KvTiles &t, unsigned grid, int cache_dtype, int DP, bool pad,
                        float *o, float2 *ml, KvJoin *joins, hipStream_t st);
 // its workgroups a compute unit, rows of a tile, and keys a step
 int kv_prefill_groups(int DP);
