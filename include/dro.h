@@ -487,8 +487,8 @@ int kv_block_tables(dro_ctx *ctx, const dro_kv_pool *pool, const int32_t *len, c
  * DRO_MXFP4 and DRO_MXFP8 (dim a multiple of 32, strides multiples of 32 elements, k and
  * v aligned to 16 bytes) need no scales beforehand: components 32 g .. 32 g + 31 of a row
  * share the power of two 2^(y - 127), y the byte
- *   k_power[b k_power_block + i k_power_token + h k_power_head + g]
- * (255: the group is NaN), and are codes of 4 bits (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign,
+ *   k_power[b k_power_block + h k_power_head + i dim / 32 + g]
+ * (255: the group is NaN; a head's powers of a block lie together, aligned to 16 bytes), and are codes of 4 bits (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign,
  * e2m1; component d in byte d / 2 of the row, the even one in its low half) or 8 (e4m3).
  * kv_store takes for a group of largest magnitude top (an infinity counts as the largest
  * finite number of its type, NaN aside) the least power with top <= 7 2^e (MXFP4) or
@@ -506,8 +506,7 @@ typedef struct {
     int64_t v_block, v_token, v_head;
     const float *k_scale, *v_scale;
     uint8_t *k_power, *v_power;
-    int64_t k_power_block, k_power_token, k_power_head;
-    int64_t v_power_block, v_power_token, v_power_head;
+    int64_t k_power_block, k_power_head, v_power_block, v_power_head;
 } dro_kv_cache;
 
 /* The keys and values of T tokens into their slots: token t, head h, component d

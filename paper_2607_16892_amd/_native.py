@@ -49,8 +49,7 @@ class KvCacheStruct(ct.Structure):
                 ("k", P), ("v", P), ("k_block", i64), ("k_token", i64), ("k_head", i64),
                 ("v_block", i64), ("v_token", i64), ("v_head", i64), ("k_scale", P),
                 ("v_scale", P), ("k_power", P), ("v_power", P), ("k_power_block", i64),
-                ("k_power_token", i64), ("k_power_head", i64), ("v_power_block", i64),
-                ("v_power_token", i64), ("v_power_head", i64)]
+                ("k_power_head", i64), ("v_power_block", i64), ("v_power_head", i64)]
 
 
 class KvRowsStruct(ct.Structure):

@@ -36,8 +36,8 @@ struct KvStoreArgs {
     void *c[2];                   // the cache's
     int64_t c_block[2], c_token[2], c_head[2];
     const float *scale[2];        // fp8 caches
-    uint8_t *power[2];            // caches in shared scales
-    int64_t p_block[2], p_token[2], p_head[2];
+    uint8_t *power[2];            // caches in shared scales; D / 32 from token to token
+    int64_t p_block[2], p_head[2];
     const int64_t *slot;
 };
 hipError_t launch_kv_store(const KvStoreArgs &a, int dtype, int cache_dtype, hipStream_t st);
@@ -69,7 +69,7 @@ struct KvAttnArgs {
 // otherwise, 105.7 us for 103.4 on 64 requests of 50 to 8192 keys.)
 struct KvMxArgs : KvAttnArgs {
     const uint8_t *k_power, *v_power;
-    int64_t kp_block, kp_token, kp_head, vp_block, vp_token, vp_head;
+    int64_t kp_block, kp_head, vp_block, vp_head;  // (D / 32 from token to token)
 };
 // bytes of scratch that a call needs
 size_t kv_attention_bytes(const KvAttnArgs &a, int cache_dtype);

@@ -112,13 +112,14 @@ int check_cache(dro_ctx *ctx, const dro_kv_cache *c)
         return fail(ctx, DRO_EINVAL, "k_scale and v_scale go with DRO_FP8_E4M3 and no other type");
     if (!mx) return DRO_OK;  // (the fields behind are not read)
     if (!c->k_power || !c->v_power) return fail(ctx, DRO_EINVAL, "the cache's k_power or v_power is NULL");
-    const int64_t t[6] = {c->k_power_block, c->k_power_token, c->k_power_head,
-                          c->v_power_block, c->v_power_token, c->v_power_head};
-    for (int64_t x : t)
+    const int64_t t[4] = {c->k_power_block, c->k_power_head, c->v_power_block, c->v_power_head};
+    for (int64_t x : t) {
+        if (x % 16) return fail(ctx, DRO_EINVAL, "a stride %lld of the powers is not a multiple of 16", (long long)x);
         if (x < 0 || x > (1LL << 38))
             return fail(ctx, DRO_ELIMIT, "a stride %lld of the powers is outside [0, 2^38]", (long long)x);
-    if (std::max(c->k_power_token, c->v_power_token) * c->block > 0x7fffffffLL)
-        return fail(ctx, DRO_ELIMIT, "the powers of a block lie 2^31 bytes or more apart");
+    }
+    if (!aligned(c->k_power, 16) || !aligned(c->v_power, 16))
+        return fail(ctx, DRO_EINVAL, "the cache's k_power or v_power is not aligned to 16 bytes");
     return DRO_OK;
 }
 
@@ -172,8 +173,6 @@ int move_rows(dro_ctx *ctx, const dro_kv_cache *c, int32_t dtype, int64_t T, voi
         a.power[1] = c->v_power;
         a.p_block[0] = c->k_power_block;
         a.p_block[1] = c->v_power_block;
-        a.p_token[0] = c->k_power_token;
-        a.p_token[1] = c->v_power_token;
         a.p_head[0] = c->k_power_head;
         a.p_head[1] = c->v_power_head;
     }
@@ -248,10 +247,8 @@ int attention(dro_ctx *ctx, const dro_kv_cache *c, const dro_kv_rows *q, const d
         a.k_power = c->k_power;
         a.v_power = c->v_power;
         a.kp_block = c->k_power_block;
-        a.kp_token = c->k_power_token;
         a.kp_head = c->k_power_head;
         a.vp_block = c->v_power_block;
-        a.vp_token = c->v_power_token;
         a.vp_head = c->v_power_head;
     }
     a.scale = q->scale;

@@ -346,14 +346,6 @@ __global__ __launch_bounds__(kStoreThreads) void kv_store_kernel(const KvStoreAr
 // division: 2^-e is a power of two, and rounding to the codes is the hardware's, to nearest even.
 // Bound by memory: 8001 tokens of 8 heads of 128 components into 8 bits and read back, 99 MB, 22.4 us
 // together, 4.4 TB/s.
-template <class C> struct MxFormat {
-    static constexpr bool kFour = __is_same(C, mx4);
-    static constexpr int kTop = kFour ? 2 : 8;                        // exponent of the largest code
-    static constexpr uint32_t kAbove = kFour ? 0x600000 : 0x680000;   // fraction beyond which e grows
-    static constexpr int kLeast = kFour ? -125 : -117;                // smallest code normal in bf16
-    template <class T> static constexpr int kMost = (__is_same(T, f16) ? 15 : 127) - kTop;  // largest finite in T
-};
-
 template <class T, class C>
 __global__ __launch_bounds__(kStoreThreads) void kv_store_mx_kernel(const KvStoreArgs a)
 {
@@ -418,7 +410,7 @@ __global__ __launch_bounds__(kStoreThreads) void kv_store_mx_kernel(const KvStor
                 *(uint2 *)to = make_uint2(pack_fp8(f), pack_fp8(f + 4));
             }
             if ((threadIdx.x & 3) == 0)
-                p[block * a.p_block[which] + token * a.p_token[which]] = F::kFour && n ? 255 : e + 127;
+                p[block * a.p_block[which] + token * (a.D / kGroup)] = F::kFour && n ? 255 : e + 127;
         }
     }
 }
@@ -462,8 +454,7 @@ __global__ __launch_bounds__(kStoreThreads) void kv_load_kernel(const KvStoreArg
             else
                 for (int j = 0; j < kWords; ++j) w[i][j] = z[j];
             if constexpr (kMx<C>)
-                power[i] = a.power[which][block * a.p_block[which] + token * a.p_token[which] + h * a.p_head[which] +
-                                          d / kGroup];
+                power[i] = a.power[which][block * a.p_block[which] + h * a.p_head[which] + token * (a.D / kGroup) + d / kGroup];
         }
         float s = 1.0f;
         if constexpr (__is_same(C, fp8)) s = a.scale[which][h];

@@ -15,6 +15,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "kv_math.h"
 #include "kv_sched.h"
@@ -30,12 +31,33 @@ constexpr int kDecodeRows = 16;
 constexpr int decode_waves(int DP, int E) { return DP == 256 ? 1 : DP * E >= 256 ? 2 : DP * E >= 128 ? 3 : 4; }
 
 // Caches in shared scales.  A lane reads 16 bytes of a key row at a time, so its codes of 4 bits are
-// one whole group (with 64 components half of one), of 8 bits half a group: one power a read.  They
-// are widened by one instruction a pair that takes the power as well, to exactly what they stand
-// for (in f16 rounded), and from there on are values of T like any other.
+// one whole group (with 64 components half of one), of 8 bits half a group: one power a read.  Of the
+// values it reads the powers of its four rows at once, which lie next to one another.  Codes are
+// widened by one instruction a pair that takes the power as well, to exactly what they stand for (in
+// f16 rounded), and from there on are values of T like any other.
+//
+// 128 components of 4 bits: an instruction issues in 70 % of a SIMD's cycles (435 vector ones for 64 keys: 128 that
+// widen, 64 that pair rows), so with two waves 199 us for 128 requests of 1000 to 16,384 keys, 64 heads
+// on 8, with three 189 (4.5 TB/s in the kernel), with four 205, as registers run short; 64 keys a step
+// instead of 32 take 187 with two waves, but 64 requests of 50 to 8192 keys 50 us for 45.  In 8 bits with
+// two waves 320 us, with three 345, where again there are too few registers; of 256 components 97 us
+// with one and 120 with two for 64 requests of 500 to 8192 keys, 16 heads on 4.
+template <class C> constexpr int decode_waves_of(int DP)
+{
+    if (__is_same(C, mx4)) return DP == 256 ? 2 : DP == 128 ? 3 : 4;
+    if (__is_same(C, mx8)) return DP == 256 ? 1 : DP == 128 ? 2 : 4;
+    return decode_waves(DP, (int)sizeof(C));
+}
+
+// f(0), .., f(N - 1), each with its number as a constant
+template <class F, int... I> __device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
 template <class T, class C, int DP, bool FULL, class A>
-__global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decode_kernel(
+__global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
     const A a, const KvCut cut, const uint64_t *sums, bool pad, float *part_o, float2 *part_ml,
     KvJoin *joins)
 {
@@ -43,10 +65,9 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
     constexpr int VW = DP / 16;            // components a lane reads of a value row
     constexpr bool F8 = __is_same(C, fp8), MX = kMx<C>, FOUR = __is_same(C, mx4);
     constexpr int KWords = FOUR ? S : sizeof(C) == 1 ? S * 2 : S * 4;  // dwords a lane reads of a key row
-    constexpr int VWords = F8 ? VW / 4 : VW / 2;  // and of a value row (shared scales: widened to T)
+    constexpr int VWords = F8 ? VW / 4 : VW / 2;  // and of a value row
     constexpr int KReads = FOUR ? (S + 3) / 4 : S / 2;  // shared scales: reads of a key row, a power each
-    constexpr int VRaw = FOUR ? (VW + 7) / 8 : VW / 4;  // and dwords of a value row before they are widened
-    using VC = std::conditional_t<MX, T, C>;            // what the values' dwords hold
+    constexpr int VRaw = FOUR ? (VW + 7) / 8 : VW / 4;  // and dwords of a value row
     __shared__ KvLds lds;
 
     const int lane = threadIdx.x, n16 = lane & 15, grp = lane >> 4;
@@ -104,6 +125,13 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         // to_exp leads to the exponent of its tanh
         const float slope = a.slopes ? a.slopes[hq] * kLog2e : 0.0f;
         const float cap = a.cap * kLog2e, to_exp = a.cap > 0.0f ? ks * (2.0f * kLog2e) / a.cap : ks * kLog2e;
+        // shared scales, scores changed by nothing else: the factor is applied with the maximum's
+        // subtraction, so it has to be positive
+        const bool late = MX && a.cap == 0.0f && !a.slopes && ks != 0.0f;
+        const float by = late ? fmaxf(fabsf(to_exp), 0x1p-126f) : 1.0f;
+        if (MX && late && ks < 0.0f)
+#pragma unroll
+            for (int s = 0; s < S; ++s) q[s] ^= 0x80008000u;
         const int p_row = kShared<A> && !a.slopes ? 0 : kv_row_place(a, r, it.ctx, it.n, token, it.first_token + token);
 
         const char *kp = (const char *)a.k + bytes_of<C>((int64_t)h * a.k_head);
@@ -121,11 +149,24 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         // Steps: keys k0 + 32 u.  A lane holds the block of one group of 16 keys, 32 steps ahead.
         const int steps = (k1 - k0 + kStepKeys - 1) / kStepKeys;
         int ids = 0;
+        uint64_t at_k = 0, at_v = 0, at_kp = 0, at_vp = 0;  // shared scales: and where its 16 keys lie
         bool found = false;  // infinities or NaN among values that only some rows see
         auto fetch_ids = [&](int u) {
             const int key = k0 + (u + (lane >> 1)) * kStepKeys + (lane & 1) * 16;
             ids = min(max(table[min(key, k1 - 1) >> a.shift], 0), a.num_blocks - 1);
+            if constexpr (MX) {
+                const int64_t id = ids, in = key & in_block;
+                at_k = (uint64_t)kp + bytes_of<C>(id * a.k_block + in * a.k_token);
+                at_v = (uint64_t)vp + bytes_of<C>(id * a.v_block + in * a.v_token);
+                at_kp = (uint64_t)(a.k_power + h * a.kp_head + id * a.kp_block) + in * (a.D / kGroup);
+                at_vp = (uint64_t)(a.v_power + h * a.vp_head + id * a.vp_block) + in * (a.D / kGroup);
+            }
         };
+        auto buffer_of = [&](uint64_t at, int u, int t) {
+            const int from = 2 * (u & 31) + t;
+            return Buffer(lane_value((uint32_t)at, from), lane_value((uint32_t)(at >> 32), from));
+        };
+        const uint32_t v_row = bytes_of<C>((uint32_t)a.v_token);
         auto place_of = [&](int64_t block_stride, int64_t token_stride, int u, int t) {
             const int id = __builtin_amdgcn_readlane(ids, 2 * (u & 31) + t);
             const int key = k0 + u * kStepKeys + t * 16;
@@ -139,18 +180,18 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         auto load_k = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const char *p = base_of(kp, a.k_block, a.k_token, u, t);
+                const char *p = MX ? nullptr : base_of(kp, a.k_block, a.k_token, u, t);
                 if constexpr (MX) {
                     constexpr int N = KWords / KReads;
-                    const uint8_t *pw = a.k_power + h * a.kp_head + place_of(a.kp_block, a.kp_token, u, t);
+                    const Buffer kb = buffer_of(at_k, u, t), pb = buffer_of(at_kp, u, t);
 #pragma unroll
                     for (int x = 0; x < KReads; ++x) {
                         const int d = component(x * (S / KReads));
                         Words<N> y{};
                         k_pow[t][x] = 127;
                         if (FULL || d < a.D) {
-                            y = load_words<N>(p + x * 64, k_lane);
-                            k_pow[t][x] = pw[(uint32_t)(n16 * (int)a.kp_token + d / kGroup)];
+                            y = kb.words<N>(k_lane, x * 64);
+                            k_pow[t][x] = pb.byte(n16 * (a.D / kGroup) + component(0) / kGroup, x * (FOUR ? 4 : 2));
                         }
 #pragma unroll
                         for (int j = 0; j < N; ++j) k[t].w[N * x + j] = y.w[j];
@@ -184,28 +225,43 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
         for (int u = 0; u < steps; ++u) {
             const int key0 = k0 + u * kStepKeys;
             const bool edge = key0 < all_lo || key0 + kStepKeys > min(all_hi, k1);
-            Words<VWords> v[8];
+            Words<VWords> v[MX ? 1 : 8];
             Words<MX ? VRaw : 1> raw[MX ? 8 : 1];
-            uint32_t v_pow[MX ? 8 : 1];
+            uint32_t v_pow[MX ? 2 : 1];  // the power of row n16 % 4 of a tile's four (see `power`)
             auto load_v = [&]() {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
+                    if constexpr (MX) {
+                        const Buffer vb = buffer_of(at_v, u, t), pb = buffer_of(at_vp, u, t);
+                        const uint32_t row = (grp * 4 + (n16 & 3)) * (a.D / kGroup);
+                        if constexpr (DP < 256) {
+                            const int g = n16 * VW / kGroup;
+                            v_pow[t] = 127;
+                            if (FULL || g < a.D / kGroup) v_pow[t] = pb.byte(row + g, 0);
+                        } else if constexpr (FULL) {  // of two groups
+                            v_pow[t] = pb.half(row + (n16 >> 2) * 2, 0);
+                        } else {
+                            const int g = (n16 >> 2) * 2;
+                            v_pow[t] = 127;
+                            if (g < a.D / kGroup) v_pow[t] = pb.byte(row + g, 0);
+                            if (g + 1 < a.D / kGroup) v_pow[t] |= pb.byte(row + g + 1, 0) << 8;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            Words<VRaw> &y = raw[t * 4 + i];
+                            y = Words<VRaw>{};
+                            if (FULL || n16 * VW < a.D) {
+                                if constexpr (FOUR && VW == 4) y.w[0] = vb.half(v_lane, i * v_row);
+                                else y = vb.words<VRaw>(v_lane, i * v_row);
+                            }
+                        }
+                        continue;
+                    }
                     const char *p = base_of(vp, a.v_block, a.v_token, u, t);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const char *at = p + bytes_of<C>((int64_t)i * a.v_token);
-                        if constexpr (MX) {
-                            const uint8_t *pw = a.v_power + h * a.vp_head + place_of(a.vp_block, a.vp_token, u, t) +
-                                                i * a.vp_token;
-                            Words<VRaw> &y = raw[t * 4 + i];
-                            y = Words<VRaw>{};
-                            v_pow[t * 4 + i] = 127;
-                            if (FULL || n16 * VW < a.D) {
-                                if constexpr (FOUR && VW == 4) y.w[0] = *(const uint16_t *)(at + v_lane);
-                                else y = load_words<VRaw>(at, v_lane);
-                                v_pow[t * 4 + i] = pw[(uint32_t)(grp * 4 * (int)a.vp_token + n16 * VW / kGroup)];
-                            }
-                        } else if constexpr (FULL) {
+                        if constexpr (FULL) {
                             v[t * 4 + i] = load_words<VWords>(at, v_lane);
                         } else {
                             constexpr int N = F8 ? 2 : 4, P = VWords < N ? VWords : N;
@@ -240,6 +296,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
                     }
                     s[t] = mfma16<T>(kf, q[x], s[t]);
                 }
+                if constexpr (MX) __builtin_amdgcn_sched_barrier(0);  // (few registers)
             }
             // the next step's keys are on their way while this one's values are used; the blocks
             // of the next 32 steps only after this step's values have been asked for
@@ -251,7 +308,10 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             // scores to exponents of two
             float e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = s[i >> 2][i & 3] * to_exp;
+            for (int i = 0; i < 8; ++i) e[i] = s[i >> 2][i & 3];
+            if (!late)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] *= to_exp;
             if (a.cap > 0.0f || a.slopes) {
                 const float b0 = slope * (float)(key0 + grp * 4 - p_row);
 #pragma unroll
@@ -263,11 +323,17 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             if (edge) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int key = key0 + (i >> 2) * 16 + grp * 4 + (i & 3);
-                    e[i] = key >= see.lo && key < see.hi ? e[i] : -INFINITY;
+                    if constexpr (MX) {  // (compared with constants: few registers)
+                        const int from = see.lo - key0 - grp * 4;
+                        e[i] = (uint32_t)((i >> 2) * 16 + (i & 3) - from) < (uint32_t)max(see.hi - see.lo, 0) ? e[i] : -INFINITY;
+                    } else {
+                        const int key = key0 + (i >> 2) * 16 + grp * 4 + (i & 3);
+                        e[i] = key >= see.lo && key < see.hi ? e[i] : -INFINITY;
+                    }
                 }
             }
             float mt = fmaxf(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])), fmaxf(fmaxf(e[4], e[5]), fmaxf(e[6], e[7])));
+            if constexpr (MX) mt *= by;
             mt = max_groups(mt);
             if (__any(has_to_raise<T>(mt, m))) {
                 const float to = fmaxf(m, mt - kUnit<T>);
@@ -280,78 +346,130 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
             const float mu = m == -INFINITY ? 0.0f : m;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                e[i] = __builtin_amdgcn_exp2f(e[i] - mu);
+                e[i] = __builtin_amdgcn_exp2f(MX ? __builtin_fmaf(e[i], by, -mu) : e[i] - mu);
                 l += e[i];
             }
             const u32x4 w = {pack2<T>(e[0], e[1]), pack2<T>(e[2], e[3]), pack2<T>(e[4], e[5]), pack2<T>(e[6], e[7])};
 
             if constexpr (MX) {
+                // Four neighbouring lanes hold components of one group (of 256 components, of two), so
+                // each has asked for the power of one of the four rows, and takes the others' from them.
+                float ps[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float ps = group_scale(v_pow[i]);
-                    if constexpr (VW == 4) {
-                        v[i].w[0] = unpack_mx<T, C, 0>(raw[i].w[0], ps);
-                        v[i].w[1] = unpack_mx<T, C, 1>(raw[i].w[0], ps);
-                    } else {
+                for (int t = 0; t < 2; ++t) {
+                    const int x = (int)(DP < 256 ? v_pow[t] << 23 : v_pow[t]);
+                    const int y[4] = {quad_lane<0>(x), quad_lane<1>(x), quad_lane<2>(x), quad_lane<3>(x)};
 #pragma unroll
-                        for (int j = 0; j < VW / 8; ++j) {
-                            const u32x4 y = unpack_mx8of<T, C>(&raw[i].w[j * VRaw * 8 / VW], ps);
+                    for (int i = 0; i < 4; ++i)
+                        ps[4 * t + i] = DP < 256 ? __builtin_bit_cast(float, y[i])
+                                                 : group_scale((uint32_t)y[i] >> (n16 & 2) * 4 & 0xff);
+                }
+                if (edge) {  // (see below)
+                    const int from = top.lo - key0 - grp * 4;
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) v[i].w[4 * j + c] = y[c];
-                        }
+                    for (int i = 0; i < 8; ++i) {
+                        const bool keep = (uint32_t)((i >> 2) * 16 + (i & 3) - from) < (uint32_t)max(bot.hi - top.lo, 0);
+                        ps[i] = keep ? ps[i] : 1.0f;
+#pragma unroll
+                        for (int j = 0; j < VRaw; ++j) raw[i].w[j] = keep ? raw[i].w[j] : 0;
                     }
                 }
-            }
-            if (edge) {
-                // a weight of zero does not silence an infinity or a NaN: values that no row of
-                // the tile sees become zero, and those that some see are added after the last
-                // step, to these rows alone
-                uint32_t odd = 0;
+                if (edge) {
+                    // what is not finite: a power from which on codes can be so, or a code of NaN
+                    uint32_t odd = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int key = key0 + (i >> 2) * 16 + grp * 4 + (i & 3);
-                    const bool keep = key >= top.lo && key < bot.hi;
+                    for (int i = 0; i < 8; ++i) {
+                        odd |= __builtin_bit_cast(uint32_t, ps[i]) > (uint32_t)(MxFormat<C>::template kMost<T> + 127) << 23;
+                        if constexpr (!FOUR)
 #pragma unroll
-                    for (int j = 0; j < VWords; ++j) {
-                        v[i].w[j] = keep ? v[i].w[j] : 0;
-                        odd |= nonfinite_mask<VC>(v[i].w[j]);
+                            for (int j = 0; j < VRaw; ++j) odd |= nonfinite_mask<C>(raw[i].w[j]);
+                    }
+                    if (__any(odd)) {
+                        found = true;
+                        each<8>([&](auto row) {
+                            constexpr int i = decltype(row)::value;
+                            each<VW / 2>([&](auto pair) {
+                                constexpr int p = decltype(pair)::value, of = FOUR ? 4 : 2, n = 32 / of;
+                                uint32_t &y = raw[i].w[p / of];
+                                const uint32_t bad = nonfinite_mask<T>(unpack_mx<T, C, p % of>(y, ps[i]));
+                                y &= ~(((bad & ((1u << n / 2) - 1)) | (bad >> 16 & ((1u << n / 2) - 1)) << n / 2) << p % of * n);
+                                __builtin_amdgcn_sched_barrier(0);  // rare: few registers, not speed
+                            });
+                            ps[i] = __builtin_isfinite(ps[i]) ? ps[i] : 1.0f;
+                        });
                     }
                 }
-                if (__any(odd)) {
-                    found = true;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-#pragma unroll
-                        for (int j = 0; j < VWords; ++j) v[i].w[j] &= ~nonfinite_mask<VC>(v[i].w[j]);
-                }
-            }
-            // V^T: dword y of column j holds rows 2y and 2y + 1
-#pragma unroll
-            for (int j = 0; j < VWords; ++j) {
-                if constexpr (F8) {
-                    u32x4 x[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const uint32_t lo = v[2 * y].w[j], hi = v[2 * y + 1].w[j];
-                        const uint32_t x0 = __builtin_amdgcn_perm(hi, lo, 0x05010400u);
-                        const uint32_t x1 = __builtin_amdgcn_perm(hi, lo, 0x07030602u);
-                        x[0][y] = unpack_fp8<T, false>(x0);
-                        x[1][y] = unpack_fp8<T, true>(x0);
-                        x[2][y] = unpack_fp8<T, false>(x1);
-                        x[3][y] = unpack_fp8<T, true>(x1);
-                    }
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) o[4 * j + c] = mfma16<T>(x[c], w, o[4 * j + c]);
-                } else {
+                // V^T by pairs of columns: row i's dword, of rows 2y and 2y + 1 the halves of one column
+                each<VW / 2>([&](auto pc) {
+                    constexpr int p = decltype(pc)::value;
+                    auto widen = [&](int i) {
+                        if constexpr (FOUR) return unpack_mx<T, C, p & 3>(raw[i].w[p >> 2], ps[i]);
+                        else return unpack_mx<T, C, p & 1>(raw[i].w[p >> 1], ps[i]);
+                    };
                     u32x4 x[2];
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
-                        const uint32_t lo = v[2 * y].w[j], hi = v[2 * y + 1].w[j];
+                        const uint32_t lo = widen(2 * y), hi = widen(2 * y + 1);
                         x[0][y] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
                         x[1][y] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
                     }
+                    o[2 * p] = mfma16<T>(x[0], w, o[2 * p]);
+                    o[2 * p + 1] = mfma16<T>(x[1], w, o[2 * p + 1]);
+                    __builtin_amdgcn_sched_barrier(0);  // (few registers)
+                });
+            }
+            if constexpr (!MX) {
+                if (edge) {
+                    // a weight of zero does not silence an infinity or a NaN: values that no row of
+                    // the tile sees become zero, and those that some see are added after the last
+                    // step, to these rows alone
+                    uint32_t odd = 0;
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) o[2 * j + c] = mfma16<T>(x[c], w, o[2 * j + c]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int key = key0 + (i >> 2) * 16 + grp * 4 + (i & 3);
+                        const bool keep = key >= top.lo && key < bot.hi;
+#pragma unroll
+                        for (int j = 0; j < VWords; ++j) {
+                            v[i].w[j] = keep ? v[i].w[j] : 0;
+                            odd |= nonfinite_mask<C>(v[i].w[j]);
+                        }
+                    }
+                    if (__any(odd)) {
+                        found = true;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+#pragma unroll
+                            for (int j = 0; j < VWords; ++j) v[i].w[j] &= ~nonfinite_mask<C>(v[i].w[j]);
+                    }
+                }
+                // V^T: dword y of column j holds rows 2y and 2y + 1
+#pragma unroll
+                for (int j = 0; j < VWords; ++j) {
+                    if constexpr (F8) {
+                        u32x4 x[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const uint32_t lo = v[2 * y].w[j], hi = v[2 * y + 1].w[j];
+                            const uint32_t x0 = __builtin_amdgcn_perm(hi, lo, 0x05010400u);
+                            const uint32_t x1 = __builtin_amdgcn_perm(hi, lo, 0x07030602u);
+                            x[0][y] = unpack_fp8<T, false>(x0);
+                            x[1][y] = unpack_fp8<T, true>(x0);
+                            x[2][y] = unpack_fp8<T, false>(x1);
+                            x[3][y] = unpack_fp8<T, true>(x1);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) o[4 * j + c] = mfma16<T>(x[c], w, o[4 * j + c]);
+                    } else {
+                        u32x4 x[2];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const uint32_t lo = v[2 * y].w[j], hi = v[2 * y + 1].w[j];
+                            x[0][y] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+                            x[1][y] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) o[2 * j + c] = mfma16<T>(x[c], w, o[2 * j + c]);
+                    }
                 }
             }
         }
@@ -368,7 +486,7 @@ __global__ __launch_bounds__(64, decode_waves(DP, (int)sizeof(C))) void kv_decod
                 const char *at = vp + bytes_of<C>(id * a.v_block + (int64_t)(key & in_block) * a.v_token);
                 const uint8_t *pw = nullptr;
                 if constexpr (MX) {
-                    pw = a.v_power + id * a.vp_block + (int64_t)(key & in_block) * a.vp_token + h * a.vp_head;
+                    pw = a.v_power + id * a.vp_block + (key & in_block) * (a.D / kGroup) + h * a.vp_head;
                     if (!mx_row_nonfinite<T, C>(at, pw, a.D)) continue;
                 } else {
                     if (!row_nonfinite<C>(at, bytes_of<C>(a.D))) continue;

@@ -80,7 +80,7 @@ __device__ __forceinline__ float tanh_scaled(float x, float cap, float add)
 // exponent of ones (fp8: NaN alone) carries into the sign's place
 template <class C> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w)
 {
-    if constexpr (sizeof(C) == 1)
+    if constexpr (__is_same(C, fp8) || __is_same(C, mx8))
         return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
     else if constexpr (__is_same(C, bf16))
         return ((((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
@@ -130,6 +130,46 @@ template <int N> __device__ __forceinline__ Words<N> load_words(const char *base
     }
     return x;
 }
+
+// The same of memory whose place is uniform but for a lane's offset and known in two parts: the
+// address of a buffer (uniform, less than 2^31 bytes from its base on) stays in scalar registers, so
+// that it takes one vector register whatever the row.  (Pointers: the compiler adds up a 64-bit
+// vector address a load, and the loads on their way spill registers.)
+struct Buffer {
+    __amdgpu_buffer_rsrc_t r;
+    // (the base: two words of an address)
+    __device__ __forceinline__ Buffer(uint32_t low, uint32_t high)
+        : r(__builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)high << 32 | low), 0, 0x7fffffff, 0x00020000))
+    {
+    }
+    template <int N> __device__ __forceinline__ Words<N> words(uint32_t lane, uint32_t uniform) const
+    {
+        Words<N> x;
+        if constexpr (N == 1) {
+            x.w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane, uniform, 0);
+        } else if constexpr (N == 2) {
+            const auto y = __builtin_amdgcn_raw_buffer_load_b64(r, lane, uniform, 0);
+            x.w[0] = y[0];
+            x.w[1] = y[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) {
+                const auto y = __builtin_amdgcn_raw_buffer_load_b128(r, lane, uniform + 16 * i, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x.w[4 * i + j] = y[j];
+            }
+        }
+        return x;
+    }
+    __device__ __forceinline__ uint32_t half(uint32_t lane, uint32_t uniform) const
+    {
+        return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, lane, uniform, 0);
+    }
+    __device__ __forceinline__ uint32_t byte(uint32_t lane, uint32_t uniform) const
+    {
+        return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, lane, uniform, 0);
+    }
+};
 
 // The rows of no request, by workgroup `nth` of `of`: those without other work, where there are
 // any, since the others' way to their first keys is a chain of loads already.

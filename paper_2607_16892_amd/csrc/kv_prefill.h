@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 {
     constexpr bool F8 = __is_same(C, fp8), MX = kMx<C>;
     constexpr bool REG = F8 || MX;  // widened on the way to LDS, through registers
-    constexpr int PW = __is_same(C, mx4) ? 1 : 2;  // dwords of a piece then
+    constexpr int GW = __is_same(C, mx4) ? 4 : 8;  // dwords of a group's codes
     constexpr bool LEAN = MODS || REG || DP == 256;  // places in LDS and memory are not kept over the steps
     constexpr int KT = prefill_keys(DP);
     constexpr int S = DP / 16;           // steps of 16 components of a score
@@ -214,8 +214,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             for (int j = 0; j < UP; ++j)
                 ids[j] = table[min(k0 + u * KT + (wave + 4 * j) % NG * 16, k1 - 1) >> a.shift];
         };
-        Words<PW> reg[REG ? UP * IP : 1];
-        uint32_t power[MX ? UP * IP : 1];
+        Words<2> reg[F8 ? UP * IP : 1];
         auto load = [&](auto odd_tile, int u) {
             int lane = threadIdx.x & 63;
             if constexpr (LEAN) asm volatile("" : "+v"(lane));  // (see `fresh`)
@@ -228,13 +227,6 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 const int in = (k0 + u * KT + group * 16) & in_block;
                 const char *base = (vals ? (const char *)a.v + bytes_of<C>(h * a.v_head) : (const char *)a.k + bytes_of<C>(h * a.k_head)) +
                                    bytes_of<C>(id * (vals ? a.v_block : a.k_block) + in * s_token);
-                int64_t p_token = 0;
-                const uint8_t *pw = nullptr;
-                if constexpr (MX) {
-                    p_token = vals ? a.vp_token : a.kp_token;
-                    pw = vals ? a.v_power + h * a.vp_head + id * a.vp_block + in * p_token
-                              : a.k_power + h * a.kp_head + id * a.kp_block + in * p_token;
-                }
 #pragma unroll
                 for (int i = 0; i < IP; ++i) {
                     const int rr = i * RP + lane / NC;
@@ -242,10 +234,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                     const uint32_t off = bytes_of<C>((uint32_t)(lane / NC * (int)s_token + c * 8));
                     const char *p = base + bytes_of<C>(i * RP * s_token);
                     if (FULL || c * 8 < a.D) {
-                        if constexpr (REG) reg[j * IP + i] = load_words<PW>(p, off);
-                        if constexpr (MX) power[j * IP + i] = pw[i * RP * p_token + (uint32_t)(lane / NC * (int)p_token + c / 4)];
-                        if constexpr (REG) continue;
-                        if (vals)
+                        if constexpr (F8)
+                            reg[j * IP + i] = load_words<2>(p, off);
+                        else if (vals)
                             __builtin_amdgcn_global_load_lds(
                                 (GlobalPtr)(p + off),
                                 (LdsPtr)((decltype(odd_tile)::value ? v_odd : v_even) + group * 16 * Row + i * 1024), 16, 0, 0);
@@ -257,28 +248,90 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 }
             }
         };
-        auto store = [&](auto odd_tile) {  // fewer bits: widened on the way
-            if constexpr (REG) {
+        auto store = [&](auto odd_tile) {  // fp8: widened on the way
+            if constexpr (F8) {
 #pragma unroll
                 for (int j = 0; j < UP; ++j) {
                     const bool vals = (wave + 4 * j) / NG;
                     const int group = (wave + 4 * j) % NG;
 #pragma unroll
                     for (int i = 0; i < IP; ++i) {
-                        const Words<PW> &x = reg[j * IP + i];
+                        const Words<2> &x = reg[j * IP + i];
                         const int rr = i * RP + lane / NC;
                         const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
-                        if (FULL || c * 8 < a.D) {
-                            u32x4 y;
-                            if constexpr (MX) y = unpack_mx8of<T, C>(x.w, group_scale(power[j * IP + i]));
-                            else
-                                y = u32x4{unpack_fp8<T, false>(x.w[0]), unpack_fp8<T, true>(x.w[0]),
-                                          unpack_fp8<T, false>(x.w[1]), unpack_fp8<T, true>(x.w[1])};
+                        if (FULL || c * 8 < a.D)
                             *(u32x4 *)((vals ? (decltype(odd_tile)::value ? v_odd : v_even)
                                               : (decltype(odd_tile)::value ? k_odd : k_even)) +
-                                        group * 16 * Row + i * 1024 + lane * 16) = y;
-                        }
+                                        group * 16 * Row + i * 1024 + lane * 16) =
+                                u32x4{unpack_fp8<T, false>(x.w[0]), unpack_fp8<T, true>(x.w[0]),
+                                      unpack_fp8<T, false>(x.w[1]), unpack_fp8<T, true>(x.w[1])};
                     }
+                }
+            }
+        };
+        // Shared scales: a tile's keys have 256 groups, so a lane stages one, of the keys and of the
+        // values, 16 bytes of 4-bit codes (32 of 8-bit ones) and a power each; lanes next to one another
+        // take rows next to one another, so that their pieces go to different banks.  The values' rows
+        // are turned by fours, so there a lane writes its four pieces in an order by its row.  Four
+        // chunks of 512 tokens over 4000 to 8192 keys, 32 heads on 8: 303 us in 4 bits, 307 in 8, fp8
+        // 297, 16 bits 267 (which no register passes on the way to LDS).
+        const int n16 = lane & 15, mx_g = DP == 64 ? lane >> 4 & 1 : DP == 128 ? lane >> 4 : (lane >> 4) + 4 * (wave & 1);
+        auto mx_group = [&](int j) { return DP == 64 ? wave * 2 + j : DP == 128 ? wave : wave >> 1; };  // of 16 keys
+        Words<MX ? GW : 1> mx_reg[2];
+        uint32_t mx_power[2];
+        constexpr int MG = MX && DP == 64 ? 2 : 1;  // groups of keys of a wave
+        auto mx_ids = [&](int u) {
+#pragma unroll
+            for (int j = 0; j < MG; ++j) ids[j] = table[min(k0 + u * KT + mx_group(j) * 16, k1 - 1) >> a.shift];
+        };
+        auto mx_load = [&](int u) {
+            if constexpr (MX) {
+                const char *base[MG][2];
+                const uint8_t *pw[MG][2];
+#pragma unroll
+                for (int j = 0; j < MG; ++j) {
+                    const int64_t id = min(max(ids[j], 0), a.num_blocks - 1);
+                    const int in = (k0 + u * KT + mx_group(j) * 16) & in_block;
+                    base[j][0] = (const char *)a.k + bytes_of<C>(h * a.k_head + id * a.k_block + in * a.k_token);
+                    base[j][1] = (const char *)a.v + bytes_of<C>(h * a.v_head + id * a.v_block + in * a.v_token);
+                    pw[j][0] = a.k_power + h * a.kp_head + id * a.kp_block + in * (a.D / kGroup);
+                    pw[j][1] = a.v_power + h * a.vp_head + id * a.vp_block + in * (a.D / kGroup);
+                }
+                const bool second = MG == 2 && lane >= 32;
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+                    if (FULL || mx_g * kGroup < a.D) {
+                        const uint32_t off = bytes_of<C>((uint32_t)(n16 * (int)(v ? a.v_token : a.k_token) + mx_g * kGroup));
+                        mx_reg[v] = load_words<GW>(second ? base[MG - 1][v] : base[0][v], off);
+                        mx_power[v] = (second ? pw[MG - 1][v] : pw[0][v])[(uint32_t)(n16 * (a.D / kGroup) + mx_g)];
+                    }
+            }
+        };
+        auto mx_store = [&](auto odd_tile) {
+            if constexpr (MX) {
+                if (!FULL && mx_g * kGroup >= a.D) return;
+                const int row = mx_group(MG == 2 ? lane >> 5 : 0) * 16 + n16, rot = n16 >> 2;
+                const float ks = group_scale(mx_power[0]), vs = group_scale(mx_power[1]);
+                char *kt = (decltype(odd_tile)::value ? k_odd : k_even) + row * Row;
+                char *vt = (decltype(odd_tile)::value ? v_odd : v_even) + row * Row;
+                constexpr int N = GW / 4;
+                auto &y = mx_reg[1].w;
+#pragma unroll
+                for (int x = 0; x < 2 * N; ++x) {  // piece i becomes piece i ^ rot
+                    const int i = x / N * 2 * N + x % N, lo = y[i], hi = y[i + N];
+                    y[i] = rot & 1 ? hi : lo;
+                    y[i + N] = rot & 1 ? lo : hi;
+                }
+#pragma unroll
+                for (int i = 0; i < 2 * N; ++i) {
+                    const int lo = y[i], hi = y[i + 2 * N];
+                    y[i] = rot & 2 ? hi : lo;
+                    y[i + 2 * N] = rot & 2 ? lo : hi;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    *(u32x4 *)(kt + ((4 * mx_g + i) ^ key_turn<DP>(row)) * 16) = unpack_mx8of<T, C>(&mx_reg[0].w[i * N], ks);
+                    *(u32x4 *)(vt + ((4 * mx_g + (i ^ rot)) ^ value_turn<DP>(row)) * 16) = unpack_mx8of<T, C>(&y[i * N], vs);
                 }
             }
         };
@@ -319,10 +372,17 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         __syncthreads();  // the last item's tiles are read
         if (threadIdx.x == 0) found = 0;
         if (steps) {
-            load_ids(0);
-            load(even, 0);
-            load_ids(1);
-            store(even);
+            if constexpr (MX) {
+                mx_ids(0);
+                mx_load(0);
+                mx_ids(1);
+                mx_store(even);
+            } else {
+                load_ids(0);
+                load(even, 0);
+                load_ids(1);
+                store(even);
+            }
         }
         auto step = [&](auto odd_tile, int u) {
             constexpr std::integral_constant<bool, !decltype(odd_tile)::value> next{};
@@ -331,8 +391,13 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile u has landed
             __syncthreads();                     // everybody's has, and tile u - 1 is read
             if (u + 1 < steps) {
-                load(next, u + 1);
-                load_ids(u + 2);
+                if constexpr (MX) {
+                    mx_load(u + 1);
+                    mx_ids(u + 2);
+                } else {
+                    load(next, u + 1);
+                    load_ids(u + 2);
+                }
             }
             // A weight of zero does not silence an infinity or a NaN.  Where some row of the
             // workgroup does not see some key of the tile, such values become zero in LDS and are
@@ -473,7 +538,10 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 __builtin_amdgcn_sched_group_barrier(kMfma, kAheadOf, 0);
                 __builtin_amdgcn_s_setprio(0);
             }
-            if (u + 1 < steps) store(next);
+            if (u + 1 < steps) {
+                if constexpr (MX) mx_store(next);
+                else store(next);
+            }
         };
         for (int u = 0; u < steps; u += 2) {
             step(even, u);
@@ -493,7 +561,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                                                                  (int64_t)h * a.v_head);
                 const uint8_t *pw = nullptr;
                 if constexpr (MX) {
-                    pw = a.v_power + id * a.vp_block + (int64_t)(key & in_block) * a.vp_token + h * a.vp_head;
+                    pw = a.v_power + id * a.vp_block + (key & in_block) * (a.D / kGroup) + h * a.vp_head;
                     if (!mx_row_nonfinite<T, C>(at, pw, a.D)) continue;
                 } else {
                     if (!row_nonfinite<C>(at, bytes_of<C>(a.D))) continue;

@@ -54,6 +54,14 @@ template <class T, bool kHigh> __device__ __forceinline__ uint32_t unpack_fp8(ui
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHigh));
 }
 
+template <class C> struct MxFormat {
+    static constexpr bool kFour = __is_same(C, mx4);
+    static constexpr int kTop = kFour ? 2 : 8;                        // exponent of the largest code
+    static constexpr uint32_t kAbove = kFour ? 0x600000 : 0x680000;   // fraction beyond which the power grows
+    static constexpr int kLeast = kFour ? -125 : -117;                // smallest code normal in bf16
+    template <class T> static constexpr int kMost = (__is_same(T, f16) ? 15 : 127) - kTop;  // largest finite in T
+};
+
 // Pair kPair of the components in a dword of codes of scale `s`, as packed T: exact in bf16 (in f16
 // rounded, infinite beyond its range), NaN where the group's byte is 255.
 __device__ __forceinline__ float group_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }

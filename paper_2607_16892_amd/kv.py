@@ -140,9 +140,9 @@ class KvCache:
     [num_blocks, block, heads, dim] tensors, strided as they like except for the
     contiguous components, in torch.bfloat16, torch.float16 or, with scales,
     torch.float8_e4m3fn.  With k_power and v_power, uint8 [num_blocks, block, heads,
-    dim / 32] whose groups lie next to one another, the cache is in shared scales: MXFP8 if
-    k and v are torch.float8_e4m3fn, MXFP4 if they are torch.uint8 [.., dim / 2], two
-    components a byte.  The tensors are checked once, here, and stay the cache's."""
+    dim / 32] whose groups and tokens of a head lie next to one another, the cache is in
+    shared scales: MXFP8 if k and v are torch.float8_e4m3fn, MXFP4 if they are torch.uint8
+    [.., dim / 2], two components a byte.  The tensors are checked once, here, and stay the cache's."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: Optional[torch.Tensor] = None   # float32 [heads]
@@ -223,12 +223,16 @@ class KvCache:
                 t = getattr(self, name)
                 if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or t.device != self.k.device:
                     raise TypeError(f"{name} must be a uint8 tensor on {self.k.device}")
-                if tuple(t.shape) != shape or (shape[3] > 1 and t.stride(3) != 1):
-                    raise ValueError(f"{name} must have shape {shape} with the groups of a row next to "
-                                     f"one another, got {tuple(t.shape)}")
+                if (tuple(t.shape) != shape or (shape[3] > 1 and t.stride(3) != 1)
+                        or (shape[1] > 1 and t.stride(1) != shape[3])):
+                    raise ValueError(f"{name} must have shape {shape} with a head's tokens of a block next "
+                                     f"to one another, got {tuple(t.shape)} strided {t.stride()}")
             s.k_power, s.v_power = self.k_power.data_ptr(), self.v_power.data_ptr()
-            s.k_power_block, s.k_power_token, s.k_power_head = self.k_power.stride()[:3]
-            s.v_power_block, s.v_power_token, s.v_power_head = self.v_power.stride()[:3]
+            # (the stride of a dimension of one entry may be anything)
+            for name in ("k_power", "v_power"):
+                blocks, _, heads, _ = getattr(self, name).stride()
+                setattr(s, name + "_block", blocks if shape[0] > 1 else 0)
+                setattr(s, name + "_head", heads if shape[2] > 1 else 0)
         for name in ("k_scale", "v_scale"):
             t = getattr(self, name)
             if t is not None:

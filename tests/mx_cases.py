@@ -50,9 +50,10 @@ def cache(dev, kind, nb, block, heads, D, layout="heads", seed=0, fill=0x5a):
     out = []
     for width in (D // 2 if kind == "mxfp4" else D, D // 32):
         for _ in range(2):
-            shape = (nb, heads, block, width) if layout == "heads" else (nb, block, heads, width)
+            heads_first = layout == "heads" or width == D // 32
+            shape = (nb, heads, block, width) if heads_first else (nb, block, heads, width)
             x = torch.full(shape, fill, dtype=torch.uint8, device=dev)
-            out.append(x.permute(0, 2, 1, 3) if layout == "heads" else x)
+            out.append(x.permute(0, 2, 1, 3) if heads_first else x)
     k, v, kp, vp = out
     if kind == "mxfp8":
         k, v = k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn)
@@ -98,11 +99,15 @@ def mx_case(dev, kind, ctx, new, Hq, H, D, dtype="bf16", layout="heads", **kw):
         held = torch.from_numpy(okv.mx_decode(code, byte, kind)).float()
         t = [torch.from_numpy(z).to(dev) for z in (code, byte)]
         if layout == "heads":            # laid out as blocks of one head's tokens
-            t = [z.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for z in t]
-        else:                            # the powers with a byte between the rows'
-            wide = torch.full((*t[1].shape[:3], D // 32 + 1), 200, dtype=torch.uint8, device=dev)
-            wide[..., : D // 32] = t[1]
-            t[1] = wide[..., : D // 32]
+            t[0] = t[0].permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+            t[1] = t[1].permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+        else:                            # the powers by heads, with some bytes between the blocks'
+            nb, blk = t[1].shape[:2]
+            size = H * blk * (D // 32)
+            wide = torch.full((nb, size + 16), 200, dtype=torch.uint8, device=dev)
+            mine = wide[:, :size].unflatten(1, (H, blk, D // 32)).permute(0, 2, 1, 3)
+            mine.copy_(t[1])
+            t[1] = mine
         if kind == "mxfp8":
             t[0] = t[0].view(torch.float8_e4m3fn)
         out.append((held, *t))

@@ -198,6 +198,9 @@ def test_refusals(ctx, dev):
             dro.KvCache(c.k, c.v, **bad)
     with pytest.raises(ValueError):
         dro.KvCache(c.k, c.v, k_power=c.k_power[:1], v_power=c.v_power)
+    apart = torch.zeros((2, 16, 2, 2), dtype=torch.uint8, device=dev)   # tokens of a head apart
+    with pytest.raises(ValueError):
+        dro.KvCache(c.k, c.v, k_power=apart, v_power=c.v_power)
     with pytest.raises(TypeError):
         dro.KvCache(c.k, c.v)                                      # bytes without powers
     with pytest.raises(TypeError):
@@ -233,8 +236,10 @@ def test_refusals(ctx, dev):
         return lib.kv_load(ctx.handle, ct.byref(cache), dtype, T, x.data_ptr(), 128, 64, x.data_ptr(), 128, 64,
                            slot.data_ptr(), None)
 
-    for change, code in ((dict(dtype=5), -1), (dict(k_power=None), -1), (dict(v_power_block=-1), -5),
-                         (dict(k_power_token=1 << 39), -5), (dict(k_power_token=1 << 30), -5), (dict(dim=48), -5),
+    for change, code in ((dict(dtype=5), -1), (dict(k_power=None), -1),
+                         (dict(v_power_block=-16), -5), (dict(v_power_block=-1), -1),
+                         (dict(k_power_head=1 << 39), -5), (dict(k_power_head=8), -1), (dict(v_power=s.v_power + 4), -1),
+                         (dict(dim=48), -5),
                          (dict(k_head=16), -1), (dict(k=s.k + 8), -1), (dict(dim=288), -5)):
         bad = _native.KvCacheStruct.from_buffer_copy(s)
         for name, value in change.items():
