@@ -79,6 +79,7 @@ hipError_t launch_kv_attention(const KvMxArgs &a, int dtype, int cache_dtype, vo
 // tokens, and are attended like requests of their own, the groups before the requests.
 struct KvSharedArgs : KvMxArgs {
     int groups, p_W, p_window, p_max_new;  // p_W = columns of the prefixes' table
+    int p_few;               // groups of up to this many tokens belong to the kernel of few rows
     const int32_t *first, *p_context, *p_table;
     int64_t p_stride;
     // scratch
@@ -87,6 +88,7 @@ struct KvSharedArgs : KvMxArgs {
                              // sees, and the first from which on all do
     int32_t *row_pos;        // [T], null: no window and no slopes.  The rows' places among their
                              // requests' own tokens
+    int2 *row_of;            // [T] each row's request and group, or -1
     float *raw_o[2];         // [T][Hq] rows of DP sums of a source's items (0: prefixes) that
     float2 *raw_ml[2];       // one workgroup has finished, and their maxima and weights' sums
 };

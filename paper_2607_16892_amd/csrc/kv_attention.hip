@@ -121,7 +121,10 @@ static __device__ __forceinline__ void plan_tiles(const A &a, const KvCut &cut, 
         plan_scan(steps, part, total);
         steps_all += total;
     }
-    const uint64_t share = kv_tile_share(cut, steps_all * a.H);
+    uint64_t share = kv_tile_share(cut, steps_all * a.H);
+    // Prefixes' tiles have many rows to write and join for few steps: eight steps where every compute
+    // unit gets a part all the same (64 requests behind 8192 tokens, 32 heads on 8: 83 us, so 80).
+    if constexpr (kShared<A>) share = max(share, min((uint64_t)8, steps_all * a.H / (uint32_t)(cut.groups / 2)));
     // Where not all tiles run at once and one pass holds them, they go by quarters of a share, the
     // longest first, so that none of them is waited for alone (128 requests of 500 to 4000 keys, three
     // tokens of 8 heads to each of 8: 206 us as they come, so 180; six prompts of 300 to 2000 tokens, 12
@@ -459,22 +462,48 @@ hipError_t launch_kv_attention(const KvMxArgs &a, int dtype, int cache_dtype, vo
 // and then the requests), the kernels of few and of many rows leave sums, and one launch joins
 // each row's, up to the order of the sources and of their keys.
 
-// Each row's place among its request's own tokens.
-constexpr int kPlaceThreads = 256;
-__global__ __launch_bounds__(kPlaceThreads) void kv_places_kernel(const KvSharedArgs a)
+static __device__ __forceinline__ int group_request(const KvSharedArgs &a, int g) { return min(max(a.first[g], 0), a.R); }
+
+// The last index of the ascending x[0 .. n) whose entry is at most v (0: or none is).
+template <class U> static __device__ __forceinline__ int last_upto(const U *x, int n, int v)
 {
-    for (uint32_t t = blockIdx.x * kPlaceThreads + threadIdx.x; t < (uint32_t)a.T; t += gridDim.x * kPlaceThreads) {
-        int lo = 0, hi = a.R;  // the last request that begins at t or before
-        while (hi - lo > 1) {
-            const int m = (lo + hi) >> 1;
-            if (a.start[m] <= (int)t) lo = m;
-            else hi = m;
-        }
-        a.row_pos[t] = kv_context(a, a.groups + lo) - kv_end_token(a, a.groups + lo) + (int)t;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (x[m] <= v) lo = m;
+        else hi = m;
     }
+    return lo;
 }
 
-static __device__ __forceinline__ int group_request(const KvSharedArgs &a, int g) { return min(max(a.first[g], 0), a.R); }
+// The plan, by parts: workgroup 0 sums the steps of the sources of few rows, workgroup 1 lists the
+// tiles of the others (both find the groups' rows, and below a window where a group's rows begin to
+// see its prefix), and the others give each row its request and group, 1024 rows at a time.  (One
+// workgroup for all, and searches by whoever joins a row: 12 us and 16 where this takes x and y, of
+// 64 requests behind one prefix of 8192 tokens, 32 heads on 8.)
+constexpr int kSearched = 2048;
+
+static __device__ __forceinline__ void plan_rows(const KvSharedArgs &a, int32_t *start_lds, int32_t *first_lds)
+{
+    const bool near = a.R < kSearched && a.groups < kSearched;
+    if (near) {
+        for (int i = threadIdx.x; i <= a.R; i += kPlanThreads) start_lds[i] = a.start[i];
+        for (int i = threadIdx.x; i <= a.groups; i += kPlanThreads) first_lds[i] = a.first[i];
+        __syncthreads();
+    }
+    auto start = [&](int r) { return min(max(near ? start_lds[r] : a.start[r], 0), a.T); };
+    auto first = [&](int g) { return min(max(near ? first_lds[g] : a.first[g], 0), a.R); };
+    for (int64_t t0 = (int64_t)(blockIdx.x - 2) * kPlanThreads; t0 < a.T; t0 += (int64_t)(gridDim.x - 2) * kPlanThreads) {
+        const int t = (int)t0 + threadIdx.x;
+        if (t >= a.T) continue;
+        const int r = near ? last_upto(start_lds, a.R, t) : last_upto(a.start, a.R, t);
+        const bool own = start(r) <= t && t < start(r + 1);
+        const int g = near ? last_upto(first_lds, a.groups, r) : last_upto(a.first, a.groups, r);
+        const bool behind = own && first(g) <= r && r < first(g + 1) && start(first(g)) <= t && t < start(first(g + 1));
+        a.row_of[t] = make_int2(own ? r : -1, behind ? g : -1);
+        if (a.row_pos) a.row_pos[t] = kv_context(a, a.groups + r) - start(r + 1) + t;
+    }
+}
 
 __global__ __launch_bounds__(kPlanThreads) void kv_shared_plan_kernel(const KvSharedArgs a, const KvCut few, const KvCut many,
                                                                       int keys, int most, uint64_t *sums, uint64_t *before,
@@ -482,7 +511,13 @@ __global__ __launch_bounds__(kPlanThreads) void kv_shared_plan_kernel(const KvSh
                                                                       int2 *where)
 {
     __shared__ KvTileLds lds;
-    for (int g = threadIdx.x; g <= a.groups; g += kPlanThreads)
+    if (blockIdx.x >= 2) {
+        static_assert(sizeof(KvTileLds) >= 8 * kSearched, "starts and first requests");
+        plan_rows(a, (int32_t *)&lds, (int32_t *)&lds + kSearched);
+        return;
+    }
+    if (!(blockIdx.x ? many.groups : few.groups)) return;
+    for (int g = threadIdx.x; g <= a.groups; g += kPlanThreads)  // (both workgroups write the same)
         a.p_start[g] = min(max(a.start[group_request(a, g)], 0), a.T);
     if (a.ends) {
         const int lane = threadIdx.x & 63;
@@ -504,9 +539,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_shared_plan_kernel(const KvSh
         }
     }
     __syncthreads();  // (both are there for the workgroup)
-    if (few.groups) plan_sums(a, few, sums, lds.part);
-    __syncthreads();
-    if (many.groups) plan_tiles(a, many, keys, most, before, tile_sums, tiles, list, where, lds);
+    if (blockIdx.x == 0) plan_sums(a, few, sums, lds.part);
+    else plan_tiles(a, many, keys, most, before, tile_sums, tiles, list, where, lds);
 }
 
 struct KvSharedWork {
@@ -520,7 +554,19 @@ struct KvSharedWork {
     size_t bytes;
 };
 
-// A wave to the rows of a token that share a key head, as many as its lanes reach with 16 bytes each.
+// Where the sums of a row over one of its sources are: `parts` rows, of which part 0 is row `first`
+// and part c row next + (c - 1) stride.
+struct KvSums32 {
+    const float *o;
+    const float2 *ml;
+    int parts;
+    int64_t first, next;
+    int stride;
+};
+
+// A wave to as many of a token's rows as its lanes reach with 16 bytes each: first a row's prefix, then
+// its own keys, each in the order of the keys.  Bound by latency, so what says where both are is asked
+// for at once (whichever kernel's it is), and then several parts of both.
 constexpr int kRowsWaves = 4;
 template <class T, int DP>
 __global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const KvSharedArgs a, const KvCut few, const KvCut many,
@@ -530,72 +576,90 @@ __global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const K
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = lane % Lanes * 4;
     KvTileList list{0, 0, 0};
     if (many.groups) list = *w.list;
+    const uint64_t run = few.groups ? w.sums[a.groups + a.R + 1] : 1;
     for (uint32_t unit = blockIdx.x * kRowsWaves + wave; unit < units; unit += gridDim.x * kRowsWaves) {
-        const uint32_t part = unit % per, th = unit / per;
-        const int t = th / (uint32_t)a.H, h = th - (uint32_t)t * a.H;
-        const int j = part * Rows + lane / Lanes;  // query head of the key head
-        const int r = __builtin_amdgcn_readfirstlane(kv_find(a.start, a.R, t));
-        const bool own = a.start[r] <= t && t < a.start[r + 1];
-        const int g = __builtin_amdgcn_readfirstlane(kv_find(a.first, a.groups, r));
-        const bool behind = own && a.first[g] <= r && r < a.first[g + 1] && a.p_start[g] <= t && t < a.p_start[g + 1];
-        if (j >= a.G) continue;
-        const int hq = h * a.G + j;
+        const int t = unit / per, hq = (int)(unit - (uint32_t)t * per) * Rows + lane / Lanes;
+        const int2 of = a.row_of[t];
+        if (hq >= a.Hq) continue;
+        const int h = hq / a.G, j = hq - h * a.G;
         const int64_t row_at = (int64_t)t * a.Hq + hq;
-        RowSum<4> s;
-        s.clear();
-        auto add = [&](int i, int source) {
+        auto find = [&](int i, int source, bool is) {
+            KvSums32 x{a.raw_o[source], a.raw_ml[source], 1, row_at, 0, 0};
             const int first = kv_first_token(a, i), n = kv_end_token(a, i) - first, row = (t - first) * a.G + j;
-            KvJoin it{};
-            int kind = 0, y;
-            if (few.groups && n <= few.few) {
-                const KvShare x = kv_share(a, few, i);
-                const int tile = row / few.rows;
-                y = row - tile * few.rows;
-                const uint64_t run = w.sums[a.groups + a.R + 1];
-                const uint64_t u0 = w.sums[i] + ((uint64_t)h * x.tiles + tile) * kv_steps(x), u1 = u0 + kv_steps(x) - 1;
+            const KvShare s = kv_share(a, few, i);
+            const uint64_t sum = few.groups ? w.sums[i] : 0, listed = many.groups ? w.before[i] : 0;
+            if (few.groups && n <= kv_few(a, few, i)) {
+                const int tile = row / few.rows, y = row - tile * few.rows;
+                const uint64_t u0 = sum + ((uint64_t)h * s.tiles + tile) * kv_steps(s), u1 = u0 + kv_steps(s) - 1;
                 const bool small = u1 < 0xffffffffu;  // (then the run is)
                 const uint32_t b0 = small ? (uint32_t)u0 / (uint32_t)run : (uint32_t)(u0 / run);
                 const uint32_t b1 = small ? (uint32_t)u1 / (uint32_t)run : (uint32_t)(u1 / run);
-                it.parts = (int)(b1 - b0) + 1;
-                it.first = kv_part(b0, true);
-                it.next = kv_part(b0 + 1, false);
-                it.stride = 2;
+                if (b0 < b1)
+                    x = KvSums32{w.o[0], w.ml[0], (int)(b1 - b0) + 1, (int64_t)kv_part(b0, true) * few.rows + y,
+                                 (int64_t)kv_part(b0 + 1, false) * few.rows + y, 2 * few.rows};
             } else {
-                kind = 1;
-                const int tile = row / many.rows;
-                y = row - tile * many.rows;
+                const int tile = row / many.rows, y = row - tile * many.rows;
                 const int tiles = (int)(((long long)n * a.G + many.rows - 1) / many.rows);
-                const uint64_t nth = w.before[i] + (tiles - 1 - tile);  // (listed last tile first)
-                if (nth >= (uint64_t)list.count) return;  // (starts that are not ascending)
-                const int2 x = w.where[nth];
-                it.parts = x.y;
-                it.first = x.x + list.parts * h;
-                it.next = it.first + 1;
-                it.stride = 1;
+                const uint64_t nth = listed + (tiles - 1 - tile);  // (listed last tile first)
+                is &= nth < (uint64_t)list.count;                  // (starts that are not ascending)
+                const int2 at = is ? w.where[nth] : make_int2(0, 1);
+                const int64_t place = at.x + list.parts * h;
+                if (at.y > 1)
+                    x = KvSums32{w.o[1], w.ml[1], at.y, place * many.rows + y, (place + 1) * many.rows + y, many.rows};
             }
-            if (it.parts == 1) {
-                const Vec<float, 4> z = *(const Vec<float, 4> *)(a.raw_o[source] + row_at * DP + d);
-                const float x[4] = {z[0], z[1], z[2], z[3]};
-                s.add(a.raw_ml[source][row_at], x);
-            } else if (it.parts == 2) {
-                s.template sum<DP, 2>(it, kind ? many.rows : few.rows, w.o[kind], w.ml[kind], y, d, 0, 1);
-            } else {
-                s.template sum<DP, 8>(it, kind ? many.rows : few.rows, w.o[kind], w.ml[kind], y, d, 0, 1);
+            if (!is) x.parts = 0;
+            return x;
+        };
+        const KvSums32 prefix = find(max(of.y, 0), 0, of.y >= 0), own = find(a.groups + max(of.x, 0), 1, of.x >= 0);
+        const int all = prefix.parts + own.parts;
+        RowSum<4> s;
+        s.clear();
+        auto sum = [&](auto ahead) {
+            constexpr int N = decltype(ahead)::value;
+            for (int c = 0; c < all; c += N) {
+                float2 x[N];
+                Vec<float, 4> z[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int n = min(c + i, all - 1), k = n < prefix.parts ? n : n - prefix.parts;
+                    const KvSums32 &from = n < prefix.parts ? prefix : own;
+                    const int64_t at = k == 0 ? from.first : from.next + (int64_t)(k - 1) * from.stride;
+                    x[i] = from.ml[at];
+                    z[i] = *(const Vec<float, 4> *)(from.o + at * DP + d);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (c + i < all) {
+                        const float y[4] = {z[i][0], z[i][1], z[i][2], z[i][3]};
+                        s.add(x[i], y);
+                    }
             }
         };
-        if (behind) add(g, 0);
-        if (own) add(a.groups + r, 1);
+        if (all <= 4) sum(std::integral_constant<int, 4>{});
+        else if (all <= 8) sum(std::integral_constant<int, 8>{});
+        else sum(std::integral_constant<int, 16>{});
         s.template write_row<T>(a, t, h, hq, d);
     }
+}
+
+// Tokens up to which a group's prefix is the kernel's for few rows: one of its tiles, and four where
+// the prefixes are small (by their table), since the other kernel takes 10 us to begin.  (Eight
+// requests behind 1000 tokens, 8 heads on one: 28 us by four tiles, 36 by the other; behind 300, 32 on
+// 8, 25 and 36; 16 requests behind 4000, 32 on 8, 46 and 42; 64 behind 16 prefixes of 1000 to 4000, 64
+// on 8, two tiles a group: 84 and 67.)
+static int shared_few(const KvSharedArgs &a)
+{
+    const int64_t keys = (int64_t)a.groups * a.H * a.p_W << a.shift;
+    return std::max((keys <= 8192 ? 64 : 16) / a.G, 1);
 }
 
 static KvPlans shared_plans(const KvSharedArgs &a, int cache_dtype)
 {
     const int DP = padded_dim(a.D), requests = a.groups + a.R;
-    const int few = std::max(((int64_t)requests * a.H < 16 ? 32 : 16) / a.G, 1);
+    const int few = std::max(((int64_t)requests * a.H < 16 ? 32 : 16) / a.G, 1), p_few = shared_few(a);
     // As without prefixes, but single tokens keep their kernel beside groups of many rows, whose
     // tiles are few and long.
-    const bool all_few = a.max_new <= few && a.p_max_new <= few;
+    const bool all_few = a.max_new <= few && a.p_max_new <= p_few;
     const bool all_many = a.max_new > few && (a.R <= kFewRequests || a.T > (int64_t)(a.R - 1) * a.max_new + few);
     KvPlans p{};
     if (!all_many) {
@@ -609,8 +673,9 @@ static KvPlans shared_plans(const KvSharedArgs &a, int cache_dtype)
         p.many.groups = a.num_cu * kv_prefill_groups(DP) / kDies * kDies;
         p.many.few = all_many ? 0 : few;
         p.many.below = false;
-        const int64_t longer = all_many ? a.T : a.T / (few + 1) + 1;  // sources that have tiles
-        p.most_tiles = (int)(2 * ((int64_t)a.T * a.G / p.many.rows) + std::min<int64_t>(a.groups, longer) +
+        // sources that have tiles
+        const int64_t longer = all_many ? a.T : a.T / (few + 1) + 1, wider = all_many ? a.T : a.T / (p_few + 1) + 1;
+        p.most_tiles = (int)(2 * ((int64_t)a.T * a.G / p.many.rows) + std::min<int64_t>(a.groups, wider) +
                              std::min<int64_t>(a.R, longer));
         const int64_t items = (int64_t)p.most_tiles * a.H;
         p.grid = (unsigned)std::min<int64_t>((items + 2 * p.many.groups + kDies) / kDies * kDies, 1 << 23);
@@ -635,6 +700,7 @@ static KvSharedWork shared_work(KvSharedArgs &a, const KvPlans &p, void *ws)
     take(a.p_start, (size_t)a.groups + 1);
     take(a.ends, a.groups);
     take(a.row_pos, a.T);
+    take(a.row_of, a.T);
     take(w.sums, requests + 2);
     take(w.before, requests);
     take(w.tile_sums, (size_t)p.most_tiles + 1);
@@ -643,6 +709,7 @@ static KvSharedWork shared_work(KvSharedArgs &a, const KvPlans &p, void *ws)
     take(w.list, 1);
     if (!a.p_window) a.ends = nullptr;
     if (!a.p_window && !a.slopes) a.row_pos = nullptr;
+    a.p_few = !p.many.groups ? 0x7fffffff : !p.few.groups ? 0 : shared_few(a);
     w.bytes = take.at - (char *)ws;
     return w;
 }
@@ -656,17 +723,16 @@ size_t kv_shared_bytes(const KvSharedArgs &a, int cache_dtype)
 template <class T> static void run_shared(const KvSharedArgs &a, const KvPlans &p, const KvSharedWork &w, int cache_dtype, hipStream_t st)
 {
     const int DP = padded_dim(a.D);
-    if (a.row_pos)
-        kv_places_kernel<<<std::min((a.T + kPlaceThreads - 1) / kPlaceThreads, 4 * a.num_cu), kPlaceThreads, 0, st>>>(a);
-    kv_shared_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, p.few, p.many, kv_prefill_keys(DP), p.most_tiles, w.sums, w.before,
-                                                      w.tile_sums, w.tiles, w.list, w.where);
+    const unsigned row_groups = (unsigned)std::min((a.T + kPlanThreads - 1) / kPlanThreads, a.num_cu);
+    kv_shared_plan_kernel<<<2 + row_groups, kPlanThreads, 0, st>>>(a, p.few, p.many, kv_prefill_keys(DP), p.most_tiles, w.sums,
+                                                                  w.before, w.tile_sums, w.tiles, w.list, w.where);
     if (p.many.groups) {
         const KvTiles t{w.tile_sums, w.tiles, w.list};
         launch_kv_prefill<T>(a, p.many, t, p.grid, cache_dtype, DP, false, w.o[1], w.ml[1], nullptr, st);
     }
     if (p.few.groups) launch_kv_decode<T>(a, p.few, w.sums, cache_dtype, DP, false, w.o[0], w.ml[0], nullptr, st);
     const int rows = 64 / (DP / 4);  // of a wave
-    const uint32_t per = (uint32_t)(a.G + rows - 1) / rows, units = (uint32_t)a.T * a.H * per;
+    const uint32_t per = (uint32_t)(a.Hq + rows - 1) / rows, units = (uint32_t)a.T * per;
     const unsigned blocks = std::min((units + kRowsWaves - 1) / kRowsWaves, 1u << 20);
     auto kernel = DP == 64 ? kv_shared_join_kernel<T, 64> : DP == 128 ? kv_shared_join_kernel<T, 128> : kv_shared_join_kernel<T, 256>;
     kernel<<<blocks, kRowsWaves * 64, 0, st>>>(a, p.few, p.many, w, units, per);

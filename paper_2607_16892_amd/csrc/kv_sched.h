@@ -98,12 +98,19 @@ template <class A> __device__ __forceinline__ int kv_prefix_of(const A &a, int r
     return a.prefix && !kv_is_prefix(a, r) ? a.prefix[kv_own(a, r)] : 0;
 }
 
+template <class A> __device__ __forceinline__ int kv_few(const A &a, const KvCut &c, int r)
+{
+    if constexpr (kShared<A>)
+        if (r < a.groups) return a.p_few;
+    return c.few;
+}
+
 template <class A> __device__ __forceinline__ KvShare kv_share(const A &a, const KvCut &c, int r)
 {
     KvShare s{0, 0, 0, 0};
     if (r >= kv_requests(a)) return s;
     const int n = max(kv_end_token(a, r) - kv_first_token(a, r), 0);
-    if (n == 0 || (n <= c.few) != c.below) return s;
+    if (n == 0 || (n <= kv_few(a, c, r)) != c.below) return s;
     s.n = n;
     s.ctx = kv_context(a, r);
     s.tiles = (int)(((long long)n * a.G + c.rows - 1) / c.rows);

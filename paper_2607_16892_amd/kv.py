@@ -328,10 +328,13 @@ def kv_load(ctx: Context, cache: KvCache, slot: torch.Tensor, dtype=None, k=None
         out = []
         for name, t in (("k", k), ("v", v)):
             if t is None:
-                t = torch.empty((T, cs.heads, cs.dim), dtype=dtype, device=dev)
-            elif t.dtype is not dtype or t.shape[:1] != (T,):
+                out.append((torch.empty((T, cs.heads, cs.dim), dtype=dtype, device=dev),
+                            (cs.heads * cs.dim, cs.dim)))
+                continue
+            rows, stride = _need_rows(t, name, dev, cs.heads, cs.dim)
+            if t.dtype is not dtype or rows != T:
                 raise ValueError(f"{name} must hold {T} rows of {dtype}")
-            out.append((t, _need_rows(t, name, dev, cs.heads, cs.dim)[1]))
+            out.append((t, stride))
     (k, ks), (v, vs) = out
     if k.requires_grad or v.requires_grad or cache._grad:
         _no_gradient("kv_load")
