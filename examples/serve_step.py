@@ -8,7 +8,11 @@ around them is two random layers of projections, so the tokens mean nothing; wha
 shows is how the calls fit together, and how often a policy's requests have to wait for
 blocks.
 
-    python examples/serve_step.py [--steps 200] [--policy dro|mean] [--cache bf16|fp8]
+With --share the L_pre shared tokens of each class are held once: a row of the table of their
+own brings them like a request, and the class's requests, which lie next to one another in the
+batch, follow them by kv_shared_attention.
+
+    python examples/serve_step.py [--steps 200] [--policy dro|mean] [--cache bf16|fp8|mxfp8|mxfp4] [--share]
 """
 from __future__ import annotations
 
@@ -41,12 +45,13 @@ class Layers:
         self.back = [weight(width, width) for _ in range(LAYERS)]
         self.embed = weight(4096, width) * width ** 0.5
 
-    def step(self, ctx, caches, x, pool, plan, max_new):
+    def step(self, ctx, caches, x, pool, plan, max_new, shared=None):
         for cache, qkv, back in zip(caches, self.qkv, self.back):
             y = (x @ qkv).view(-1, HEADS + 2 * KV_HEADS, DIM)
             dro.kv_store(ctx, cache, y[:, HEADS:HEADS + KV_HEADS], y[:, HEADS + KV_HEADS:], plan["slot"])
-            o = dro.kv_attention(ctx, cache, y[:, :HEADS], pool.table, plan["start"], plan["context"],
-                                 max_new, want_lse=False)["out"]
+            rows = (ctx, cache, y[:, :HEADS], pool.table, plan["start"], plan["context"], max_new)
+            o = (dro.kv_attention(*rows, want_lse=False) if shared is None else
+                 dro.kv_shared_attention(*rows, shared, want_lse=False))["out"]
             x = x + o.reshape(len(x), -1) @ back
         return x
 
@@ -63,7 +68,7 @@ def reservations(ctx, w, dev, policy):
 
 
 def serve(dev="cuda:0", steps=200, policy="dro", cache="bf16", slots=48, blocks=3600, block=16, seed=0,
-          collect=None):
+          collect=None, share=False):
     """Runs the loop; returns counts.  collect(step, x): called with the rows' outputs."""
     r = np.random.default_rng(seed)
     dev = torch.device(dev)
@@ -74,20 +79,34 @@ def serve(dev="cuda:0", steps=200, policy="dro", cache="bf16", slots=48, blocks=
     with dro.Context(dev.index or 0) as ctx:
         eta = reservations(ctx, w, dev, policy)
         layers = Layers(dev, dtype, seed)
-        kind = torch.float8_e4m3fn if cache == "fp8" else dtype
+        kind = {"fp8": torch.float8_e4m3fn, "bf16": dtype}.get(cache, cache)
         scale = torch.full((KV_HEADS,), 0.05, device=dev)
         caches = [dro.KvCache.empty(blocks, block, KV_HEADS, DIM, kind, dev,
                                     *((scale, scale) if cache == "fp8" else ()))
                   for _ in range(LAYERS)]
-        pool = dro.BlockPool.empty(slots, most, blocks, block, dev)
-        held, target, prompt, want = (np.zeros(slots, np.int64) for _ in range(4))
-        live = np.zeros(slots, bool)
+        # a row of the table for each slot, and behind them one for each prefix that is shared
+        groups = w.C if share else 0
+        rows = slots + groups
+        pool = dro.BlockPool.empty(rows, most, blocks, block, dev)
+        held, target, prompt, want = (np.zeros(rows, np.int64) for _ in range(4))
+        live = np.zeros(rows, bool)
+        edges = np.arange(groups + 1) * slots // max(groups, 1)  # the slots of each group
+        first = torch.from_numpy(edges.astype(np.int32)).to(dev)
+        if share:
+            live[slots:], target[slots:] = True, 1 << 40
+            prompt[slots:] = want[slots:] = svc.Lpre
         for step in range(steps):
             for i in np.flatnonzero(~live)[: 1 + step % 3]:      # arrivals
                 c = int(r.integers(w.C))
-                live[i], held[i], prompt[i] = True, 0, svc.Lin[c]
-                target[i] = svc.Lin[c] + r.choice(w.samples_of(c))
-                want[i] = svc.Lin[c] + eta[c]
+                own = svc.Lin[c]
+                if share:                                        # a slot of its class, behind its prefix
+                    free_slots = np.flatnonzero(~live[edges[c]:edges[c + 1]])
+                    if held[slots + c] < prompt[slots + c] or not len(free_slots):
+                        continue
+                    i, own = edges[c] + free_slots[0], svc.Lin[c] - svc.Lpre[c]
+                live[i], held[i], prompt[i] = True, 0, own
+                target[i] = own + r.choice(w.samples_of(c))
+                want[i] = own + eta[c]
             over = live & (held >= target)                       # ended: their blocks go back
             add = np.where(live, np.where(held < prompt, np.minimum(prompt - held, CHUNK), 1), 0)
             add[over] = -1
@@ -95,11 +114,13 @@ def serve(dev="cuda:0", steps=200, policy="dro", cache="bf16", slots=48, blocks=
             i32 = [torch.from_numpy(x.astype(np.int32)).to(dev) for x in (held, add, want)]
             plan = pool.take(dro.kv_block_tables(ctx, pool, i32[0], i32[1], T, reserve=i32[2]))
             x = layers.embed[torch.from_numpy(r.integers(0, 4096, T)).to(dev)]
-            x = layers.step(ctx, caches, x, pool, plan, int(add.max(initial=0)))
+            new = np.maximum(add, 0)
+            shared = dro.SharedPrefixes(first, plan["context"][slots:], pool.table[slots:],
+                                        int(max(new[a:b].sum() for a, b in zip(edges, edges[1:])))) if share else None
+            x = layers.step(ctx, caches, x, pool, plan, int(add.max(initial=0)), shared)
             if collect:
                 collect(step, x)
             granted = plan["granted"].cpu().numpy().astype(bool)
-            new = np.maximum(add, 0)
             waits += int((live & ~over & ~granted).sum())
             tokens += int(new[granted].sum())
             done += int(over.sum())
@@ -115,8 +136,9 @@ if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--policy", choices=("dro", "mean"), default="dro")
-    ap.add_argument("--cache", choices=("bf16", "fp8"), default="bf16")
+    ap.add_argument("--cache", choices=("bf16", "fp8", "mxfp8", "mxfp4"), default="bf16")
+    ap.add_argument("--share", action="store_true", help="hold each class's shared prefix once")
     a = ap.parse_args()
-    out = serve(steps=a.steps, policy=a.policy, cache=a.cache)
+    out = serve(steps=a.steps, policy=a.policy, cache=a.cache, share=a.share)
     print("{policy}: {tokens} tokens in {steps} steps, {ended} requests ended, {waits} waits for blocks, "
           "{in_use} of {blocks} blocks in use".format(**out))
