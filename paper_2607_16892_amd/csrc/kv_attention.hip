@@ -479,8 +479,8 @@ template <class U> static __device__ __forceinline__ int last_upto(const U *x, i
 // The plan, by parts: workgroup 0 sums the steps of the sources of few rows, workgroup 1 lists the
 // tiles of the others (both find the groups' rows, and below a window where a group's rows begin to
 // see its prefix), and the others give each row its request and group, 1024 rows at a time.  (One
-// workgroup for all, and searches by whoever joins a row: 12 us and 16 where this takes x and y, of
-// 64 requests behind one prefix of 8192 tokens, 32 heads on 8.)
+// workgroup for all, 12 us, and searches by whoever joins a row, 16 us; now 8.6 and 14, of 64 requests
+// behind one prefix of 8192 tokens, 32 heads on 8.)
 constexpr int kSearched = 2048;
 
 static __device__ __forceinline__ void plan_rows(const KvSharedArgs &a, int32_t *start_lds, int32_t *first_lds)
@@ -566,7 +566,8 @@ struct KvSums32 {
 
 // A wave to as many of a token's rows as its lanes reach with 16 bytes each: first a row's prefix, then
 // its own keys, each in the order of the keys.  Bound by latency, so what says where both are is asked
-// for at once (whichever kernel's it is), and then several parts of both.
+// for at once (whichever kernel's it is), and then several parts of both, up to eight (16: more registers,
+// 112 us for 109 of the call, 128 requests behind 12 prefixes in 4 bits).
 constexpr int kRowsWaves = 4;
 template <class T, int DP>
 __global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const KvSharedArgs a, const KvCut few, const KvCut many,
@@ -636,8 +637,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const K
             }
         };
         if (all <= 4) sum(std::integral_constant<int, 4>{});
-        else if (all <= 8) sum(std::integral_constant<int, 8>{});
-        else sum(std::integral_constant<int, 16>{});
+        else sum(std::integral_constant<int, 8>{});
         s.template write_row<T>(a, t, h, hq, d);
     }
 }
