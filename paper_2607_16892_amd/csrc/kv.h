@@ -92,6 +92,13 @@ struct KvSharedArgs : KvMxArgs {
     float *raw_o[2];         // [T][Hq] rows of DP sums of a source's items (0: prefixes) that
     float2 *raw_ml[2];       // one workgroup has finished, and their maxima and weights' sums
 };
+// The same where every request reads its group's prefix itself, before its own tokens: few requests
+// and groups, no window.
+struct KvJoinedArgs : KvMxArgs {
+    int groups, p_W;
+    const int32_t *first, *p_context, *p_table;
+    int64_t p_stride;
+};
 size_t kv_shared_bytes(const KvSharedArgs &a, int cache_dtype);
 hipError_t launch_kv_shared(KvSharedArgs a, int dtype, int cache_dtype, void *ws, hipStream_t st);
 

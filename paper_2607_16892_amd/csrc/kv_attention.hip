@@ -714,8 +714,30 @@ static KvSharedWork shared_work(KvSharedArgs &a, const KvPlans &p, void *ws)
     return w;
 }
 
+// Whether each request reads its prefix itself, the same bytes from the caches mostly, which takes two
+// launches instead of three or four: where single tokens read at most 300 MB of the prefixes in all (by
+// their table).  (32 heads on 8 of 128 components, 16 bits, one prefix unless said: 16 requests
+// behind 256 tokens 28 us and by groups 49; 16 behind four of 2000, 131 MB, 35 and 53; 64 behind 992, 260
+// MB, 44 and 60; 32 behind two of 4000, 524 MB, 81 and 48; 64 behind 8192, 287 and 79.)
+constexpr double kReadItself = 300e6;
+static bool reads_itself(const KvSharedArgs &a, int cache_dtype)
+{
+    if (a.p_window || a.R > kInlineRequests || a.groups > kInlineRequests || a.max_new > std::max(few_rows(a) / a.G, 1))
+        return false;
+    const int bits = cache_dtype == DRO_MXFP4 ? 4 : cache_dtype == DRO_MXFP8 || cache_dtype == DRO_FP8_E4M3 ? 8 : 16;
+    return (double)a.R * a.H * a.D * bits / 4 * ((int64_t)a.p_W << a.shift) <= kReadItself;
+}
+
+static KvJoinedArgs joined_args(const KvSharedArgs &a)
+{
+    KvJoinedArgs j{a, a.groups, a.p_W, a.first, a.p_context, a.p_table, a.p_stride};
+    j.window = 0;
+    return j;
+}
+
 size_t kv_shared_bytes(const KvSharedArgs &a, int cache_dtype)
 {
+    if (reads_itself(a, cache_dtype)) return kv_attention_bytes(joined_args(a), cache_dtype);
     KvSharedArgs b = a;
     return shared_work(b, shared_plans(a, cache_dtype), nullptr).bytes;
 }
@@ -738,8 +760,23 @@ template <class T> static void run_shared(const KvSharedArgs &a, const KvPlans &
     kernel<<<blocks, kRowsWaves * 64, 0, st>>>(a, p.few, p.many, w, units, per);
 }
 
+template <class T> static void run_joined(const KvJoinedArgs &a, const KvPlans &p, const KvWork &w, int cache_dtype, hipStream_t st)
+{
+    const int DP = padded_dim(a.D);
+    launch_kv_decode<T>(a, p.few, nullptr, cache_dtype, DP, true, w.o, w.ml, w.joins, st);
+    launch_join<T>(a, p.few, p.few.groups, 0, w, DP, st);
+}
+
 hipError_t launch_kv_shared(KvSharedArgs a, int dtype, int cache_dtype, void *ws, hipStream_t st)
 {
+    if (reads_itself(a, cache_dtype)) {
+        const KvJoinedArgs j = joined_args(a);
+        const KvPlans p = plans(j, cache_dtype);
+        const KvWork w = work_of(j, p, ws);
+        if (dtype == DRO_BF16) run_joined<bf16>(j, p, w, cache_dtype, st);
+        else run_joined<f16>(j, p, w, cache_dtype, st);
+        return hipGetLastError();
+    }
     const KvPlans p = shared_plans(a, cache_dtype);
     const KvSharedWork w = shared_work(a, p, ws);
     if (dtype == DRO_BF16) run_shared<bf16>(a, p, w, cache_dtype, st);

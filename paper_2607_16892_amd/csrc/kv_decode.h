@@ -68,7 +68,7 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
     constexpr int VWords = F8 ? VW / 4 : VW / 2;  // and of a value row
     constexpr int KReads = FOUR ? (S + 3) / 4 : S / 2;  // shared scales: reads of a key row, a power each
     constexpr int VRaw = FOUR ? (VW + 7) / 8 : VW / 4;  // and dwords of a value row
-    __shared__ KvLds lds;
+    __shared__ KvLdsOf<A> lds;
 
     const int lane = threadIdx.x, n16 = lane & 15, grp = lane >> 4;
     // the first of the 8 components that this lane multiplies in step x of a score
@@ -101,10 +101,22 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
         // this lane's row
         const int row = row0 + min(n16, rows - 1);
         const int token = row / a.G, hq = h * a.G + row - token * a.G;
-        const KvRange see = kv_see(a, r, it.ctx, it.n, token, prefix, it.first_token + token);
+        KvRange see = kv_see(a, r, it.ctx, it.n, token, prefix, it.first_token + token);
         // the tile's keys: those that some row sees, and those that every row sees
-        const KvRange top = kv_first_range(a, r, it.ctx, it.n, row0 / a.G, prefix);
-        const KvRange bot = kv_last_range(a, r, it.ctx, it.n, (row0 + rows - 1) / a.G, prefix);
+        KvRange top = kv_first_range(a, r, it.ctx, it.n, row0 / a.G, prefix);
+        KvRange bot = kv_last_range(a, r, it.ctx, it.n, (row0 + rows - 1) / a.G, prefix);
+        // keys of a shared prefix before its own: all rows see them, and nobody what is between
+        KvPrefix pre{0, 0, 0};
+        const int32_t *p_table = nullptr;
+        if constexpr (kJoined<A>) {
+            pre.group = __builtin_amdgcn_readfirstlane(lds.prefix[r].group);
+            pre.keys = __builtin_amdgcn_readfirstlane(lds.prefix[r].keys);
+            pre.own = __builtin_amdgcn_readfirstlane(lds.prefix[r].own);
+            p_table = a.p_table + (int64_t)pre.group * a.p_stride;
+            see.hi = pre.own + max(see.hi, 0);
+            top.hi = pre.own + max(top.hi, 0);
+            bot.hi = pre.own + max(bot.hi, 0);
+        }
         const int all_lo = bot.lo, all_hi = top.hi;
         const int base = top.lo & ~(kStepKeys - 1);
         const int k0 = min(base + it.step * kStepKeys, bot.hi);
@@ -132,7 +144,7 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
         if (MX && late && ks < 0.0f)
 #pragma unroll
             for (int s = 0; s < S; ++s) q[s] ^= 0x80008000u;
-        const int p_row = kShared<A> && !a.slopes ? 0 : kv_row_place(a, r, it.ctx, it.n, token, it.first_token + token);
+        const int p_row = kShared<A> && !a.slopes ? 0 : kv_row_place(a, r, it.ctx, it.n, token, it.first_token + token) + pre.own;
 
         const char *kp = (const char *)a.k + bytes_of<C>((int64_t)h * a.k_head);
         const char *vp = (const char *)a.v + bytes_of<C>((int64_t)h * a.v_head);
@@ -151,11 +163,17 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
         int ids = 0;
         uint64_t at_k = 0, at_v = 0, at_kp = 0, at_vp = 0;  // shared scales: and where its 16 keys lie
         bool found = false;  // infinities or NaN among values that only some rows see
+        auto in_of = [&](int key) { return kJoined<A> && key >= pre.own ? key - pre.own : key; };  // its own place
         auto fetch_ids = [&](int u) {
             const int key = k0 + (u + (lane >> 1)) * kStepKeys + (lane & 1) * 16;
-            ids = min(max(table[min(key, k1 - 1) >> a.shift], 0), a.num_blocks - 1);
+            if constexpr (kJoined<A>)
+                ids = key < pre.own ? p_table[min(key, pre.keys - 1) >> a.shift]
+                                    : table[max(min(key, k1 - 1) - pre.own, 0) >> a.shift];
+            else
+                ids = table[min(key, k1 - 1) >> a.shift];
+            ids = min(max(ids, 0), a.num_blocks - 1);
             if constexpr (MX) {
-                const int64_t id = ids, in = key & in_block;
+                const int64_t id = ids, in = in_of(key) & in_block;
                 at_k = (uint64_t)kp + bytes_of<C>(id * a.k_block + in * a.k_token);
                 at_v = (uint64_t)vp + bytes_of<C>(id * a.v_block + in * a.v_token);
                 at_kp = (uint64_t)(a.k_power + h * a.kp_head + id * a.kp_block) + in * (a.D / kGroup);
@@ -170,7 +188,7 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
         auto place_of = [&](int64_t block_stride, int64_t token_stride, int u, int t) {
             const int id = __builtin_amdgcn_readlane(ids, 2 * (u & 31) + t);
             const int key = k0 + u * kStepKeys + t * 16;
-            return (int64_t)id * block_stride + (int64_t)(key & in_block) * token_stride;
+            return (int64_t)id * block_stride + (int64_t)(in_of(key) & in_block) * token_stride;
         };
         auto base_of = [&](const char *p, int64_t block_stride, int64_t token_stride, int u, int t) {
             return p + bytes_of<C>(place_of(block_stride, token_stride, u, t));
@@ -224,7 +242,9 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
         }
         for (int u = 0; u < steps; ++u) {
             const int key0 = k0 + u * kStepKeys;
-            const bool edge = key0 < all_lo || key0 + kStepKeys > min(all_hi, k1);
+            // where a prefix ends within its last step
+            const bool gap = kJoined<A> && key0 < pre.own && key0 + kStepKeys > pre.keys;
+            const bool edge = gap || key0 < all_lo || key0 + kStepKeys > min(all_hi, k1);
             Words<VWords> v[MX ? 1 : 8];
             Words<MX ? VRaw : 1> raw[MX ? 8 : 1];
             uint32_t v_pow[MX ? 2 : 1];  // the power of row n16 % 4 of a tile's four (see `power`)
@@ -313,13 +333,17 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
 #pragma unroll
                 for (int i = 0; i < 8; ++i) e[i] *= to_exp;
             if (a.cap > 0.0f || a.slopes) {
-                const float b0 = slope * (float)(key0 + grp * 4 - p_row);
+                const float b0 = slope * (float)(key0 + grp * 4 - p_row + (key0 < pre.own ? pre.own - pre.keys : 0));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float add = __builtin_fmaf((float)((i >> 2) * 16 + (i & 3)), slope, b0);
                     e[i] = a.cap > 0.0f ? tanh_scaled(e[i], cap, add) : e[i] + add;
                 }
             }
+            if (gap)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    e[i] = (i >> 2) * 16 + (i & 3) < pre.keys - key0 - grp * 4 ? e[i] : -INFINITY;
             if (edge) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -368,7 +392,8 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
                     const int from = top.lo - key0 - grp * 4;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const bool keep = (uint32_t)((i >> 2) * 16 + (i & 3) - from) < (uint32_t)max(bot.hi - top.lo, 0);
+                        const bool keep = (uint32_t)((i >> 2) * 16 + (i & 3) - from) < (uint32_t)max(bot.hi - top.lo, 0) &&
+                                          !(gap && (i >> 2) * 16 + (i & 3) >= pre.keys - key0 - grp * 4);
                         ps[i] = keep ? ps[i] : 1.0f;
 #pragma unroll
                         for (int j = 0; j < VRaw; ++j) raw[i].w[j] = keep ? raw[i].w[j] : 0;
@@ -427,7 +452,7 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int key = key0 + (i >> 2) * 16 + grp * 4 + (i & 3);
-                        const bool keep = key >= top.lo && key < bot.hi;
+                        const bool keep = key >= top.lo && key < bot.hi && !(gap && key >= pre.keys);
 #pragma unroll
                         for (int j = 0; j < VWords; ++j) {
                             v[i].w[j] = keep ? v[i].w[j] : 0;
@@ -480,13 +505,16 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
             // looking at every value of every step would cost more than it is worth.)
             for (int key = k0; key < k1; ++key) {
                 const int step = k0 + ((key - k0) & ~(kStepKeys - 1));
-                if (step >= all_lo && step + kStepKeys <= min(all_hi, k1)) continue;  // not zeroed
+                const bool gap = kJoined<A> && step < pre.own && step + kStepKeys > pre.keys;
+                if (!gap && step >= all_lo && step + kStepKeys <= min(all_hi, k1)) continue;  // not zeroed
+                if (gap && key >= pre.keys) continue;
                 const bool seen = key >= see.lo && key < see.hi;
-                const int id = min(max(table[key >> a.shift], 0), a.num_blocks - 1);
-                const char *at = vp + bytes_of<C>(id * a.v_block + (int64_t)(key & in_block) * a.v_token);
+                const int place = in_of(key);
+                const int id = min(max((kJoined<A> && key < pre.own ? p_table : table)[place >> a.shift], 0), a.num_blocks - 1);
+                const char *at = vp + bytes_of<C>(id * a.v_block + (int64_t)(place & in_block) * a.v_token);
                 const uint8_t *pw = nullptr;
                 if constexpr (MX) {
-                    pw = a.v_power + id * a.vp_block + (key & in_block) * (a.D / kGroup) + h * a.vp_head;
+                    pw = a.v_power + id * a.vp_block + (place & in_block) * (a.D / kGroup) + h * a.vp_head;
                     if (!mx_row_nonfinite<T, C>(at, pw, a.D)) continue;
                 } else {
                     if (!row_nonfinite<C>(at, bytes_of<C>(a.D))) continue;

@@ -52,6 +52,7 @@ struct KvCut {
 constexpr int kStepKeys = 32;
 
 template <class A> constexpr bool kShared = __is_same(A, KvSharedArgs);
+template <class A> constexpr bool kJoined = __is_same(A, KvJoinedArgs);
 
 // The requests, or the sources of keys: the groups' prefixes, then the requests' own tokens.
 template <class A> __device__ __forceinline__ int kv_requests(const A &a)
@@ -169,6 +170,16 @@ struct KvLds {
     uint64_t upto[kInlineRequests];  // inclusive
     KvShare share[kInlineRequests];
 };
+// Requests that read their prefixes themselves: a request's keys are on one axis, its prefix's `keys`
+// from 0 on and its own from `own` on, the next multiple of a step.
+struct KvPrefix {
+    int group, keys, own;
+};
+struct KvJoinedLds : KvLds {
+    KvPrefix prefix[kInlineRequests];
+    int32_t first[kInlineRequests + 1];
+};
+template <class A> using KvLdsOf = std::conditional_t<kJoined<A>, KvJoinedLds, KvLds>;
 
 // The items by their steps: from the workgroup's own scan in LDS, or, beyond
 // kInlineRequests and behind shared prefixes, from the exclusive sums [n + 2] of a launch before
@@ -179,11 +190,27 @@ template <class A> struct KvSched {
     static __device__ __forceinline__ bool scanned(const A &a) { return !kShared<A> && a.R <= kInlineRequests; }
 
     // (all waves; the results are in LDS after it)
-    __device__ __forceinline__ void init(const A &a, const KvCut &c, const uint64_t *sums, KvLds &lds)
+    __device__ __forceinline__ void init(const A &a, const KvCut &c, const uint64_t *sums, KvLdsOf<A> &lds)
     {
         if (scanned(a)) {
             const int lane = threadIdx.x & 63;
-            const KvShare s = kv_share(a, c, lane);
+            KvShare s = kv_share(a, c, lane);
+            if constexpr (kJoined<A>) {  // (a wave; up to 64 groups)
+                for (int g = lane; g <= a.groups; g += 64) lds.first[g] = a.first[g];
+                __syncthreads();
+                int g = 0;
+                for (int hi = a.groups; hi - g > 1;) {
+                    const int m = (g + hi) >> 1;
+                    if (lds.first[m] <= lane) g = m;
+                    else hi = m;
+                }
+                KvPrefix p{g, 0, 0};
+                if (lds.first[g] <= lane && lane < lds.first[g + 1])
+                    p.keys = (int)min((long long)max(a.p_context[g], 0), (long long)a.p_W << a.shift);
+                p.own = (p.keys + kStepKeys - 1) & ~(kStepKeys - 1);
+                lds.prefix[lane] = p;
+                s.span += p.own;
+            }
             const uint64_t upto = scan_wave(kv_units(a, s));
             all = lane_value(upto, 63);
             if (threadIdx.x < 64) {
@@ -200,7 +227,7 @@ template <class A> struct KvSched {
 
     // The item that step u (< all, uniform) belongs to.
     __device__ __forceinline__ KvItem item(const A &a, const KvCut &c, const uint64_t *sums,
-                                           const KvLds &lds, uint64_t u) const
+                                           const KvLdsOf<A> &lds, uint64_t u) const
     {
         KvItem w;
         KvShare s;
@@ -345,8 +372,8 @@ __device__ __forceinline__ uint64_t kv_tile_share(const KvCut &c, uint64_t all)
     return max((all + (uint32_t)c.groups - 1) / (uint32_t)c.groups, (uint64_t)4);
 }
 
-// What a kernel over a cache of type C takes, of arguments A (KvMxArgs or KvSharedArgs).
-template <class A, class C> using KvKernelArgs = std::conditional_t<kShared<A> || kMx<C>, A, KvAttnArgs>;
+// What a kernel over a cache of type C takes, of arguments A (KvMxArgs, KvSharedArgs or KvJoinedArgs).
+template <class A, class C> using KvKernelArgs = std::conditional_t<kShared<A> || kJoined<A> || kMx<C>, A, KvAttnArgs>;
 
 // The kernels of few and of many rows a request; they zero the rows of no request as well
 // if `pad`.

@@ -4,4 +4,6 @@
 namespace dro {
 template void launch_kv_decode<f16>(const KvSharedArgs &, const KvCut &, const uint64_t *, int, int, bool, float *,
                                    float2 *, KvJoin *, hipStream_t);
+template void launch_kv_decode<f16>(const KvJoinedArgs &, const KvCut &, const uint64_t *, int, int, bool, float *,
+                                   float2 *, KvJoin *, hipStream_t);
 }  // namespace dro

@@ -8,7 +8,10 @@ import numpy as np
 
 class Shared:
     """sizes[g] requests of group g behind pre[g] shared tokens, after `before` requests without a
-    group and before the rest."""
+    group and before the rest.  `wide`: the prefixes' table has columns for a million tokens, so that
+    small calls of single tokens are planned like large ones too."""
+
+    wide = False
 
     def __init__(self, dev, ctx, new, sizes, pre, Hq, H, D, dtype="bf16", cache=None, before=0, **kw):
         import torch
@@ -30,7 +33,11 @@ class Shared:
                 self.of[r] = g
         first = torch.tensor(self.first_h, dtype=torch.int32, device=dev)
         most = max([sum(self.new[self.first_h[g]:self.first_h[g + 1]]) for g in range(len(pre))] + [0])
-        self.shared = dro.SharedPrefixes(first, c.context[R:], c.table[R:], most)
+        table = c.table[R:]
+        if self.wide:
+            table = torch.full((len(pre), (1 << 20) // c.block), -1, dtype=torch.int32, device=dev)
+            table[:, : c.table.shape[1]] = c.table[R:]
+        self.shared = dro.SharedPrefixes(first, c.context[R:], table, most)
 
     def run(self, ctx, **kw):
         import paper_2607_16892_amd as dro

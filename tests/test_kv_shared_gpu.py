@@ -18,6 +18,12 @@ def ctx(dev):
     c.close()
 
 
+@pytest.fixture(params=[False, True], ids=["narrow", "wide"], autouse=True)
+def wide(request, monkeypatch):
+    """Both ways of a call of single tokens: requests that read their prefixes themselves, and groups."""
+    monkeypatch.setattr(Shared, "wide", request.param)
+
+
 def same(a, b):
     import torch
     return torch.equal(a["out"], b["out"]) and torch.equal(a["lse"], b["lse"])
@@ -173,6 +179,8 @@ def test_bad_data_stays_inside(ctx, dev):
     full = c.run(ctx)
     c.shared.context = torch.tensor([k.table.shape[1] * 16], dtype=torch.int32, device=dev)
     assert same(c.run(ctx), full)
+    if Shared.wide:
+        c.shared.table = table
     for first in ([-5, 2 ** 31 - 1], [-2 ** 31, 0], [7, 9], [2, 1], [2 ** 31 - 1, -2 ** 31]):
         c.shared.first = torch.tensor(first, dtype=torch.int32, device=dev)
         c.run(ctx, window=30)
