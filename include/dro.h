@@ -513,7 +513,8 @@ typedef struct {
  * at k[t k_token + h k_head + d] (strides of this call, multiples of 8, k and v
  * aligned to 16 bytes) of type `dtype`, DRO_BF16 or DRO_F16, which the cache's
  * type is unless that is one of 8 or 4 bits.  Slots outside [0, num_blocks * block)
- * (-1: no slot) are skipped; of two tokens with one slot either may remain. */
+ * (-1: no slot) are skipped; of two tokens with one slot either may remain (in shared
+ * scales a part of each: codes of the one under powers of the other). */
 int kv_store(dro_ctx *ctx, const dro_kv_cache *cache, int32_t dtype, int64_t T, const void *k,
              int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
              const int64_t *slot, dro_stream_t stream);
@@ -589,7 +590,9 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *cache, const dro_kv_rows *row
  * softmax over all keys seen.  A prefix is a request of the pool that brings tokens but has no
  * rows here: kv_block_tables and kv_store fill it like any other, and it ends after the last of
  * its group.  Two calls with the same arguments give the same bits; the rows differ in rounding
- * from kv_attention's over tables that name the prefix's blocks for each request. */
+ * from kv_attention's over tables that name the prefix's blocks for each request.  Where it is
+ * worth it (the sizes alone decide) the rows of a group share their reading, and the workspace
+ * then holds 8 T Hq bytes a padded component (of 64, 128 or 256). */
 typedef struct {
     int32_t groups;
     const int32_t *first;       /* [groups+1] ascending                                   */

@@ -319,7 +319,7 @@ def kv_load(ctx: Context, cache: KvCache, slot: torch.Tensor, dtype=None, k=None
     T = slot.numel()
     if dtype is None:
         given = k if k is not None else v
-        dtype = (given.dtype if given is not None else
+        dtype = (getattr(given, "dtype", None) if given is not None else
                  torch.bfloat16 if cs.dtype not in (0, 1) else cache.k.dtype)
     if dtype is not torch.bfloat16 and dtype is not torch.float16:
         raise TypeError(f"dtype must be torch.bfloat16 or torch.float16, got {dtype}")

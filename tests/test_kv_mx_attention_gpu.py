@@ -212,3 +212,52 @@ def test_a_captured_step(dev):
             graph.replay()
             torch.cuda.synchronize()
             assert torch_equal(dict(out=out, lse=lse), step())
+
+
+@pytest.mark.parametrize("new", [2, 60])
+@pytest.mark.parametrize("kind,dtype,D,byte", [("mxfp4", "bf16", 128, 253), ("mxfp4", "f16", 64, 141), ("mxfp8", "bf16", 96, 250),
+                                               ("mxfp8", "f16", 128, 139)])
+def test_values_beyond_the_range(ctx, dev, new, kind, dtype, D, byte):
+    """Codes whose values are infinite in q's type, as no store leaves them: the row that sees them has
+    them, infinite or NaN, in their components, and the others are as they were."""
+    import torch
+    lens = [new + 5, new + 40]
+    c = mx_case(dev, kind, lens, [new] * 2, 4, 2, D, dtype, seed=new + D)
+    ref = c.run(ctx)
+    p = lens[1] - 1
+    b, i = int(c.table_h[1, p // 16]), p % 16
+    c.cache.v_power[b, i, 0, 1] = byte
+    c.v.view(torch.uint8)[b, i, 0, 16 if kind == "mxfp4" else 32] = 0x07 if kind == "mxfp4" else 0x7e   # component 32
+    got = c.run(ctx)
+    hit = torch.zeros_like(ref["out"], dtype=torch.bool)
+    hit[2 * new - 1, :2, 32:64] = True
+    assert not torch.isfinite(got["out"][2 * new - 1, :2, 32]).any()
+    assert torch.equal(got["out"][~hit], ref["out"][~hit]) and torch.equal(got["lse"], ref["lse"])
+
+
+@pytest.mark.parametrize("kind", ["mxfp4", "mxfp8"])
+def test_places_beyond_32_bits(ctx, dev, kind):
+    """Requests, and a shared prefix, at the end of a cache of more than 2^32 bytes: as in a small one."""
+    import torch
+    import paper_2607_16892_amd as dro
+    H, D, block = 8, 128, 1024
+    nb = 9000 if kind == "mxfp4" else 5000                             # 4.7 and 5.2 GB of codes each
+    g = torch.Generator().manual_seed(1)
+    i32 = dict(dtype=torch.int32, device=dev)
+    k, v = (torch.randn((3 * block, H, D), generator=g).bfloat16().to(dev) for _ in range(2))
+    q = torch.randn((61, 32, D), generator=g).bfloat16().to(dev)
+    start, context = torch.tensor([0, 1, 61], **i32), torch.tensor([1500, 900], **i32)
+    out = []
+    for blocks in (nb, 3):
+        c = dro.KvCache.empty(blocks, block, H, D, kind, dev)
+        dro.kv_store(ctx, c, k, v, torch.arange((blocks - 3) * block, blocks * block, device=dev))
+        table = torch.tensor([[blocks - 1, blocks - 3], [blocks - 2, 0]], **i32)
+        both = dro.kv_attention(ctx, c, q, table, start, context, 60)
+        one = dro.kv_attention(ctx, c, q[:1], table[:1], start[:2], context[:1], 1)
+        shared = dro.SharedPrefixes(torch.tensor([0, 2], **i32), torch.tensor([700], **i32),
+                                    torch.tensor([[blocks - 3]], **i32), 61)
+        out.append((both, one, dro.kv_shared_attention(ctx, c, q, table, start, context, 60, shared),
+                    dro.kv_shared_attention(ctx, c, q[:1], table, start[:2].repeat_interleave(torch.tensor([1, 2], device=dev)),
+                                            context, 1, shared)))
+        del c
+    assert all(torch_equal(a, b) for a, b in zip(*out))

@@ -219,6 +219,8 @@ def test_refusals(ctx, dev):
         dro.kv_load(ctx, c, slot, dtype=torch.float16, k=x)
     with pytest.raises(TypeError):
         dro.kv_load(ctx, c, slot.int())
+    with pytest.raises(TypeError):
+        dro.kv_load(ctx, c, slot, k=[1, 2, 3])
     with pytest.raises(dro.DroError):                              # a 16-bit cache gives its own type
         dro.kv_load(ctx, dro.KvCache.empty(2, 16, 2, 64, torch.float16, dev), slot, dtype=torch.bfloat16)
     with pytest.raises(dro.DroError):                              # rows of 68 elements: not aligned
