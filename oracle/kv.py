@@ -108,8 +108,9 @@ def mx_encode(x, kind, dtype):
     bad = np.isnan(g)
     size = np.minimum(np.abs(np.where(bad, 0.0, g)), FINITE[dtype])
     top = size.max(1)
-    e = np.full(len(g), lowest)
-    while True:                          # up until the largest is not above half a step too much
+    # from below up until the largest is not above half a step too much
+    e = np.clip(np.floor(np.log2(np.maximum(top, 2.0 ** -200))) - 12, lowest, highest).astype(np.int64)
+    while True:
         small = (top > (values[-1] + half) * 2.0 ** e) & (e < highest)
         if not small.any():
             break

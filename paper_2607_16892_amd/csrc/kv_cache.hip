@@ -344,8 +344,8 @@ __global__ __launch_bounds__(kStoreThreads) void kv_store_kernel(const KvStoreAr
 // the format's largest or below it, i.e. top / 2^e <= 7 (of 6) or 464 (of 448): with
 // top = m 2^x, 1 <= m < 2, e = x - 2 (x - 8), and one more where m is above 1.75 (1.8125).  No
 // division: 2^-e is a power of two, and rounding to the codes is the hardware's, to nearest even.
-// Bound by memory: 8001 tokens of 8 heads of 128 components into 8 bits and read back, 99 MB, 22.4 us
-// together, 4.4 TB/s.
+// Bound by memory: 8001 tokens of 8 heads of 128 components into 8 bits and read back, 99 MB, 22.4 to
+// 23.2 us together, 4.3 to 4.4 TB/s.
 template <class T, class C>
 __global__ __launch_bounds__(kStoreThreads) void kv_store_mx_kernel(const KvStoreArgs a)
 {
