@@ -21,7 +21,7 @@ def ctx(dev):
 EDGES = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257, 513, 0, 1023]
 KINDS = [(k, t) for k in ("mxfp4", "mxfp8") for t in ("bf16", "f16")]
 SHAPES = [(8, 1, 128, 16), (14, 2, 128, 32), (3, 3, 64, 16), (32, 2, 96, 16), (4, 2, 256, 64), (40, 1, 32, 128),
-          (2, 1, 192, 16), (5, 5, 160, 256)]
+          (2, 1, 192, 16), (5, 5, 160, 1024)]
 
 
 @pytest.mark.parametrize("kind,dtype", KINDS)
