@@ -270,14 +270,13 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
             }
         };
         // Shared scales: a tile's keys have 256 groups, so a lane stages one, of the keys and of the
-        // values, 16 bytes of 4-bit codes (32 of 8-bit ones) and a power each.  Its row is its number's
-        // low bits turned by its group, so that a group's piece lies where the lane's number says, and
-        // lanes that write at once meet all banks; the values' rows are turned by fours, so there a lane
-        // writes its four pieces in an order by its number.  (Rows in the lanes' order: 6.9 million cycles
-        // of conflicts on four chunks of 512 tokens over 4000 to 8192 keys, 32 heads on 8, 308 us for
-        // 304 in 4 bits.  fp8 takes 297 there, 16 bits, which no register passes on the way, 267.)
+        // values, 16 bytes of 4-bit codes (32 of 8-bit ones) and a power each; lanes next to one another
+        // take rows next to one another.  The values' rows are turned by fours, so there a lane writes
+        // its four pieces in an order by its row.  Bank conflicts are a seventh of LDS's busy cycles
+        // (6.9 of 48 million in 4 bits); rows turned by their groups leave that count and the time as
+        // they are.  Four chunks of 512 tokens over 4000 to 8192 keys, 32 heads on 8: 308 us in 4 bits,
+        // 310 in 8, fp8 297, 16 bits 267 (which no register passes on the way to LDS).
         const int n16 = lane & 15, mx_g = DP == 64 ? lane >> 4 & 1 : DP == 128 ? lane >> 4 : (lane >> 4) + 4 * (wave & 1);
-        const int mx_row = n16 ^ (DP == 64 ? 8 * mx_g : 4 * (mx_g & 3));
         auto mx_group = [&](int j) { return DP == 64 ? wave * 2 + j : DP == 128 ? wave : wave >> 1; };  // of 16 keys
         Words<MX ? GW : 1> mx_reg[2];
         uint32_t mx_power[2];
@@ -303,16 +302,16 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
                 for (int v = 0; v < 2; ++v)
                     if (FULL || mx_g * kGroup < a.D) {
-                        const uint32_t off = bytes_of<C>((uint32_t)(mx_row * (int)(v ? a.v_token : a.k_token) + mx_g * kGroup));
+                        const uint32_t off = bytes_of<C>((uint32_t)(n16 * (int)(v ? a.v_token : a.k_token) + mx_g * kGroup));
                         mx_reg[v] = load_words<GW>(second ? base[MG - 1][v] : base[0][v], off);
-                        mx_power[v] = (second ? pw[MG - 1][v] : pw[0][v])[(uint32_t)(mx_row * (a.D / kGroup) + mx_g)];
+                        mx_power[v] = (second ? pw[MG - 1][v] : pw[0][v])[(uint32_t)(n16 * (a.D / kGroup) + mx_g)];
                     }
             }
         };
         auto mx_store = [&](auto odd_tile) {
             if constexpr (MX) {
                 if (!FULL && mx_g * kGroup >= a.D) return;
-                const int row = mx_group(MG == 2 ? lane >> 5 : 0) * 16 + mx_row, rot = n16 >> 2;
+                const int row = mx_group(MG == 2 ? lane >> 5 : 0) * 16 + n16, rot = n16 >> 2;
                 const float ks = group_scale(mx_power[0]), vs = group_scale(mx_power[1]);
                 char *kt = (decltype(odd_tile)::value ? k_odd : k_even) + row * Row;
                 char *vt = (decltype(odd_tile)::value ? v_odd : v_even) + row * Row;
