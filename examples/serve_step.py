@@ -52,7 +52,7 @@ class Layers:
             rows = (ctx, cache, y[:, :HEADS], pool.table, plan["start"], plan["context"], max_new)
             o = (dro.kv_attention(*rows, want_lse=False) if shared is None else
                  dro.kv_shared_attention(*rows, shared, want_lse=False))["out"]
-            x = x + o.reshape(len(x), -1) @ back
+            x = x + o.flatten(1) @ back
         return x
 
 
@@ -109,6 +109,7 @@ def serve(dev="cuda:0", steps=200, policy="dro", cache="bf16", slots=48, blocks=
                 want[i] = own + eta[c]
             over = live & (held >= target)                       # ended: their blocks go back
             add = np.where(live, np.where(held < prompt, np.minimum(prompt - held, CHUNK), 1), 0)
+            add[slots:][held[slots:] >= prompt[slots:]] = 0      # a prefix that is whole brings nothing more
             add[over] = -1
             T = int(np.maximum(add, 0).sum())
             i32 = [torch.from_numpy(x.astype(np.int32)).to(dev) for x in (held, add, want)]
