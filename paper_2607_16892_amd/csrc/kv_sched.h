@@ -43,7 +43,7 @@ struct KvItem {
 
 // Requests of up to `few` tokens belong to the one kernel, others to the other.
 struct KvCut {
-    int rows;      // of a tile
+    int rows = 1;  // of a tile (where the kernel is not launched, any)
     int groups;    // workgroups
     int few;       // tokens
     bool below;    // the kernel of the requests of up to `few` tokens
