@@ -149,8 +149,8 @@ __global__ __launch_bounds__(64, decode_waves_of<C>(DP)) void kv_decode_kernel(
         const char *kp = (const char *)a.k + bytes_of<C>((int64_t)h * a.k_head);
         const char *vp = (const char *)a.v + bytes_of<C>((int64_t)h * a.v_head);
         const int in_block = (1 << a.shift) - 1;
-        const uint32_t k_lane = bytes_of<C>((uint32_t)(n16 * (int)a.k_token + component(0)));
-        const uint32_t v_lane = bytes_of<C>((uint32_t)(grp * 4 * (int)a.v_token + n16 * VW));
+        const uint32_t k_lane = row_bytes<C>(n16, a.k_token, component(0));
+        const uint32_t v_lane = row_bytes<C>(grp * 4, a.v_token, n16 * VW);
         const int32_t *table = kv_table(a, r);
 
         float m = -INFINITY, l = 0.0f;

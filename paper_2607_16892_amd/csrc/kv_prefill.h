@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
                 for (int i = 0; i < IP; ++i) {
                     const int rr = i * RP + lane / NC;
                     const int c = (lane % NC) ^ (vals ? value_turn<DP>(rr) : key_turn<DP>(rr));
-                    const uint32_t off = bytes_of<C>((uint32_t)(lane / NC * (int)s_token + c * 8));
+                    const uint32_t off = row_bytes<C>(lane / NC, s_token, c * 8);
                     const char *p = base + bytes_of<C>(i * RP * s_token);
                     if (FULL || c * 8 < a.D) {
                         if constexpr (F8)
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
 #pragma unroll
                 for (int v = 0; v < 2; ++v)
                     if (FULL || mx_g * kGroup < a.D) {
-                        const uint32_t off = bytes_of<C>((uint32_t)(n16 * (int)(v ? a.v_token : a.k_token) + mx_g * kGroup));
+                        const uint32_t off = row_bytes<C>(n16, v ? a.v_token : a.k_token, mx_g * kGroup);
                         mx_reg[v] = load_words<GW>(second ? base[MG - 1][v] : base[0][v], off);
                         mx_power[v] = (second ? pw[MG - 1][v] : pw[0][v])[(uint32_t)(n16 * (a.D / kGroup) + mx_g)];
                     }

@@ -30,6 +30,13 @@ template <class C, class N> __host__ __device__ constexpr N bytes_of(N n)
     return __is_same(C, mx4) ? n / 2 : n * (N)sizeof(C);
 }
 
+// Bytes from a row of a block to component d of the row n further (n < 16): unsigned, as rows of 4-bit
+// codes lie up to 2^28 components apart, whose bytes alone stay below 2^31.
+template <class C> __host__ __device__ constexpr uint32_t row_bytes(int n, int64_t stride, int d)
+{
+    return bytes_of<C>((uint32_t)n * (uint32_t)stride + (uint32_t)d);
+}
+
 template <class T, int N> using Vec = T __attribute__((ext_vector_type(N)));
 
 __device__ __forceinline__ float to_float(bf16 x) { return (float)x; }

@@ -27,3 +27,18 @@ def test_shares_of_a_kernel_that_is_not_launched(tmp_path):
         }
 ''')
     assert out.split() == "5 40 5 40 5 40 2 5 40 2".split()
+
+
+def test_rows_of_codes_far_apart(tmp_path):
+    """The last row of 16 in the widest strides that the entry points take: blocks of 16 tokens end
+    below 2^31 bytes."""
+    out = host_code.run(tmp_path, "kv_types.h", r'''
+    const int64_t four = (1ll << 28) - 32, eight = (1ll << 27) - 32, sixteen = (1ll << 26) - 8;
+    std::printf("%u %u ", row_bytes<mx4>(15, four, 255), row_bytes<mx4>(12, four, 0));
+    std::printf("%u %u %u ", row_bytes<mx8>(15, eight, 255), row_bytes<fp8>(15, eight, 7), row_bytes<bf16>(15, sixteen, 9));
+    std::printf("%u ", row_bytes<mx4>(15, 0, 31));
+''')
+    four, eight, sixteen = (1 << 28) - 32, (1 << 27) - 32, (1 << 26) - 8
+    assert [int(x) for x in out.split()] == [(15 * four + 255) // 2, 6 * four, 15 * eight + 255, 15 * eight + 7,
+                                             2 * (15 * sixteen + 9), 15]
+    assert 16 * four // 2 < 2 ** 31
