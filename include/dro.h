@@ -589,8 +589,8 @@ int kv_attention(dro_ctx *ctx, const dro_kv_cache *cache, const dro_kv_rows *row
  * these positions (rows.prefix counts a request's own tokens).  out and lse are those of one
  * softmax over all keys seen.  A prefix is a request of the pool that brings tokens but has no
  * rows here: kv_block_tables and kv_store fill it like any other, from then on it brings none
- * (add 0, which needs no block, so that its context is S in every step), and it ends after the
- * last of its group.  Two calls with the same arguments give the same bits; the rows differ in rounding
+ * (add 0 and no reservation beyond its blocks: never refused, so that its context is S in every
+ * step), and it ends after the last of its group.  Two calls with the same arguments give the same bits; the rows differ in rounding
  * from kv_attention's over tables that name the prefix's blocks for each request.  Where it is
  * worth it (the sizes alone decide) the rows of a group share their reading, and the workspace
  * then holds 8 T Hq bytes a padded component (of 64, 128 or 256). */

@@ -123,7 +123,7 @@ static __device__ __forceinline__ void plan_tiles(const A &a, const KvCut &cut, 
     }
     uint64_t share = kv_tile_share(cut, steps_all * a.H);
     // Prefixes' tiles have many rows to write and join for few steps: eight steps where every compute
-    // unit gets a part all the same (64 requests behind 8192 tokens, 32 heads on 8: 83 us, so 80).
+    // unit gets a part all the same (64 requests behind 8192 tokens, 32 heads on 8: 92 us, so 83).
     if constexpr (kShared<A>) share = max(share, min((uint64_t)8, steps_all * a.H / (uint32_t)(cut.groups / 2)));
     // Where not all tiles run at once and one pass holds them, they go by quarters of a share, the
     // longest first, so that none of them is waited for alone (128 requests of 500 to 4000 keys, three
@@ -479,8 +479,8 @@ template <class U> static __device__ __forceinline__ int last_upto(const U *x, i
 // The plan, by parts: workgroup 0 sums the steps of the sources of few rows, workgroup 1 lists the
 // tiles of the others (both find the groups' rows, and below a window where a group's rows begin to
 // see its prefix), and the others give each row its request and group, 1024 rows at a time.  (One
-// workgroup for all, 12 us, and searches by whoever joins a row, 16 us; now 8.6 and 14, of 64 requests
-// behind one prefix of 8192 tokens, 32 heads on 8.)
+// workgroup for all took 12 us, and a join whose rows search for themselves 2 us more; now plan and join
+// take 8.4 and 11.1, of 64 requests behind one prefix of 8192 tokens, 32 heads on 8.)
 constexpr int kSearched = 2048;
 
 static __device__ __forceinline__ void plan_rows(const KvSharedArgs &a, int32_t *start_lds, int32_t *first_lds)
@@ -567,7 +567,7 @@ struct KvSums32 {
 // A wave to as many of a token's rows as its lanes reach with 16 bytes each: first a row's prefix, then
 // its own keys, each in the order of the keys.  Bound by latency, so what says where both are is asked
 // for at once (whichever kernel's it is), and then several parts of both, up to eight (16: more registers,
-// 112 us for 109 of the call, 128 requests behind 12 prefixes in 4 bits).
+// and 3 % more of the call, 128 requests behind 12 prefixes in 4 bits).
 constexpr int kRowsWaves = 4;
 template <class T, int DP>
 __global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const KvSharedArgs a, const KvCut few, const KvCut many,
@@ -643,10 +643,12 @@ __global__ __launch_bounds__(kRowsWaves * 64) void kv_shared_join_kernel(const K
 }
 
 // Tokens up to which a group's prefix is the kernel's for few rows: one of its tiles, and four where
-// the prefixes are small (by their table), since the other kernel takes 10 us to begin.  (Eight
-// requests behind 1000 tokens, 8 heads on one: 28 us by four tiles, 36 by the other; behind 300, 32 on
-// 8, 25 and 36; 16 requests behind 4000, 32 on 8, 46 and 42; 64 behind 16 prefixes of 1000 to 4000, 64
-// on 8, two tiles a group: 84 and 67.)
+// the prefixes are small (by their table), since the other kernel takes 10 us to begin.  (Calls of single
+// tokens whose requests do not read their prefixes themselves.  Eight requests behind 1000 tokens, 8 heads
+// on one, below a window of 900: 24 us by four tiles, 38 by the other; 16 behind 500, 8 on two, below 400:
+// 22 and 38; eight behind 900 beside 64 without a prefix, 8 on one: 23 and 33.  16 behind 4000, 32 on 8, below
+// a window of 4000: 43 either way; 64 behind 16 prefixes of 1000 to 4000, 64 on 8, two tiles a group: 95 and
+// 68.)
 static int shared_few(const KvSharedArgs &a)
 {
     const int64_t keys = (int64_t)a.groups * a.H * a.p_W << a.shift;
@@ -658,7 +660,12 @@ static KvPlans shared_plans(const KvSharedArgs &a, int cache_dtype)
     const int DP = padded_dim(a.D), requests = a.groups + a.R;
     const int few = std::max(((int64_t)requests * a.H < 16 ? 32 : 16) / a.G, 1), p_few = shared_few(a);
     // As without prefixes, but single tokens keep their kernel beside groups of many rows, whose
-    // tiles are few and long.
+    // tiles are few and long.  One kernel takes all sources of up to kFewRequests requests with chunks here
+    // as well: both have their rows planned and joined by the same launches, but run one after the other.
+    // (7 chunks of 33 to 300 beside 13 single tokens, 12 heads of 64 components, behind two prefixes of 1801
+    // to 3500: 51 us by one, 64 by both, below a window and a cap 74 and 77; 8 of 33 to 256 beside 16, 32
+    // heads on 8, MXFP4: 131 and 141; 4 of 512 beside 56 over 600 to 4000: 324 and 370; one of 500 beside 7
+    // over 600 to 30,000: 382 and 390.)
     const bool all_few = a.max_new <= few && a.p_max_new <= p_few;
     const bool all_many = a.max_new > few && (a.R <= kFewRequests || a.T > (int64_t)(a.R - 1) * a.max_new + few);
     KvPlans p{};
@@ -717,8 +724,10 @@ static KvSharedWork shared_work(KvSharedArgs &a, const KvPlans &p, void *ws)
 // Whether each request reads its prefix itself, the same bytes from the caches mostly, which takes two
 // launches instead of three or four: where single tokens read at most 300 MB of the prefixes in all (by
 // their table).  (32 heads on 8 of 128 components, 16 bits, one prefix unless said: 16 requests
-// behind 256 tokens 28 us and by groups 49; 16 behind four of 2000, 131 MB, 35 and 53; 64 behind 992, 260
-// MB, 44 and 60; 32 behind two of 4000, 524 MB, 81 and 48; 64 behind 8192, 287 and 79.)
+// behind 256 tokens 17 us and by groups 22; 16 behind four of 2000, 131 MB, 30 and 47; 64 behind 992, 260
+// MB, 35 and 42; 32 behind two of 4000, 524 MB, 77 and 40; 64 behind 8192, 287 and 83.  The lengths
+// are on the device, so a table wider than its prefixes counts as it is: 48 behind six of 300 in a table
+// for 2512 tokens, 39 us by groups where their own reading takes 22.)
 constexpr double kReadItself = 300e6;
 static bool reads_itself(const KvSharedArgs &a, int cache_dtype)
 {

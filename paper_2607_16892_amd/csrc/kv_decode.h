@@ -36,12 +36,12 @@ constexpr int decode_waves(int DP, int E) { return DP == 256 ? 1 : DP * E >= 256
 // widened by one instruction a pair that takes the power as well, to exactly what they stand for (in
 // f16 rounded), and from there on are values of T like any other.
 //
-// 128 components of 4 bits: an instruction issues in 70 % of a SIMD's cycles (435 vector ones for 64 keys: 128 that
-// widen, 64 that pair rows), so with two waves 199 us for 128 requests of 1000 to 16,384 keys, 64 heads
-// on 8, with three 189 (4.5 TB/s in the kernel), with four 205, as registers run short; 64 keys a step
-// instead of 32 take 187 with two waves, but 64 requests of 50 to 8192 keys 50 us for 45.  In 8 bits with
-// two waves 320 us, with three 345, where again there are too few registers; of 256 components 97 us
-// with one and 120 with two for 64 requests of 500 to 8192 keys, 16 heads on 4.
+// 128 components of 4 bits: an instruction issues in 73 % of a SIMD's cycles (435 vector ones for 64 keys: 128 that
+// widen, 64 that pair rows), so with two waves 184 us for 128 requests of 1000 to 16,384 keys, 64 heads
+// on 8, with three 177 (4.9 TB/s in the kernel), with four 193, as registers run short; 64 keys a step
+// instead of 32 were 1 % faster there with two waves, but 11 % slower for 64 requests of 50 to 8192 keys.
+// In 8 bits with two waves 298 us, with three 325, where again there are too few registers; of 256
+// components 89 us with one and 123 with two for 64 requests of 500 to 8192 keys, 16 heads on 4.
 template <class C> constexpr int decode_waves_of(int DP)
 {
     if (__is_same(C, mx4)) return DP == 256 ? 2 : DP == 128 ? 3 : 4;

@@ -15,7 +15,8 @@
 //
 // A prompt of 8192 tokens, 64 heads on 8 of 128 components: 1.06 to 1.15 ms from card to card, 0.96 to
 // 1.04 PFLOP/s, the matrix units busy 52 % of the cycles; four chunks of 512 over 4000 to 8192, 32 heads
-// on 8: 234 to 251 us, 880 to 940 TFLOP/s.
+// on 8: 234 to 251 us, 880 to 940 TFLOP/s; with lengths that fill the compute units less evenly 270 us,
+// 830 TFLOP/s.
 #pragma once
 
 #include <type_traits>
@@ -274,8 +275,9 @@ __global__ __launch_bounds__(256, prefill_groups(DP)) void kv_prefill_kernel(
         // take rows next to one another.  The values' rows are turned by fours, so there a lane writes
         // its four pieces in an order by its row.  Bank conflicts are a seventh of LDS's busy cycles
         // (6.9 of 48 million in 4 bits); rows turned by their groups leave that count and the time as
-        // they are.  Four chunks of 512 tokens over 4000 to 8192 keys, 32 heads on 8: 308 us in 4 bits,
-        // 310 in 8, fp8 297, 16 bits 267 (which no register passes on the way to LDS).
+        // they are.  Four chunks of 512 tokens over 4000 to 8192 keys, 32 heads on 8, of the less even
+        // lengths above, one after the other on one card: 284 us in 4 bits, 303 in 8, fp8 291, 16 bits
+        // 270 (which no register passes on the way to LDS).
         const int n16 = lane & 15, mx_g = DP == 64 ? lane >> 4 & 1 : DP == 128 ? lane >> 4 : (lane >> 4) + 4 * (wave & 1);
         auto mx_group = [&](int j) { return DP == 64 ? wave * 2 + j : DP == 128 ? wave : wave >> 1; };  // of 16 keys
         Words<MX ? GW : 1> mx_reg[2];
@@ -627,10 +629,12 @@ void launch_kv_prefill(const A &a, const KvCut &c, const KvTiles &t, unsigned gr
                        float *o, float2 *ml, KvJoin *joins, hipStream_t st)
 {
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, c, t, pad, o, ml, joins); };
-    // A head dimension between the padded ones takes the kernel of all score changes as well.  Its
-    // instances beyond 64 components keep 76 to 97 registers in scratch memory, and so do those of 128
-    // with score changes (14, with 8 bits 49) and of 256 in 8 bits with them (4): read back in the
-    // steps, behind the next tile's loads.
+    // A head dimension between the padded ones takes the kernel of all score changes as well.  Beyond 64
+    // components its instances keep 76 to 97 registers in scratch memory, over shared scales 105 to 123;
+    // those of all 128 with score changes 14 (fp8 49, MXFP4 50, MXFP8 119), of all 256 none (4, 25, 88), and
+    // of MXFP8 without them 43 and 53: read back in the steps, behind the next tile's loads.  (Behind
+    // shared prefixes a few more: 46 and 58.  A cap takes the four chunks above from 270 us to 370, fp8
+    // from 291 to 414, MXFP4 from 284 to 445, MXFP8 from 303 to 536.)
     auto of = [&](auto cache, auto dim) {
         using C = decltype(cache);
         using K = KvKernelArgs<A, C>;
